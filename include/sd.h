@@ -282,6 +282,118 @@ sd_status sd_self_spec_sample(sd_model *model, const int32_t *prompt, int32_t pr
 sd_status sd_autoregressive_sample(sd_model *model, const int32_t *prompt, int32_t prompt_len, int32_t max_new,
                                    const sd_sampling *sampling, int32_t *out_tokens, sd_stats *stats);
 
+/* Token trees.  Algorithm 2 verifies one chain of drafts; a verification that
+ * scores several continuations of one prefix at once takes a tree: node 0 is
+ * the last committed token, every other node a drafted token after its
+ * parent, and parents come before their children (parents[0] = -1,
+ * 0 <= parents[i] < i).  The keys and values of node i stand at position
+ * prefix + i of the cache, its rotary position is prefix + depth(i), and it
+ * attends to the prefix and to the nodes on its own path.  The greedy walk
+ * accepts the path of tokens that the model itself would have emitted, and
+ * the cache rows of that path are moved together.  A chain is the tree with
+ * parents[i] = i - 1.
+ *
+ * The operators below take DEVICE pointers on the current device, enqueue on
+ * hip_stream (NULL: the null stream) without waiting, allocate nothing and may
+ * be captured into a graph; sd_forward_tree and sd_verify_tree run a model on
+ * them.  A tree has at most SD_TREE_MAX nodes. */
+#define SD_TREE_MAX 1024
+
+/* One layer of a KV cache: the element (head g, position p, e) of K and of V is
+ * at g * head_stride + p * row_stride + e (strides in elements, multiples of
+ * 16 bytes; row_stride >= head_dim; rows do not overlap; k and v 16-byte
+ * aligned).  head_dim is a power of two in [16, 128], dtype an sd_dtype. */
+typedef struct {
+    void *k, *v;
+    int64_t head_stride, row_stride;
+    int32_t n_kv_heads, capacity, head_dim, dtype;
+} sd_kv_layer;
+
+/* Rotary position embedding: the first rotary_dim elements of a head (even, at
+ * least 2, at most head_dim) are turned in pairs, (i, i + rotary_dim / 2) or
+ * (2i, 2i + 1), by the angle position * f_i with f_i = base^(-2i / rotary_dim);
+ * the others pass unchanged.  Angles are taken in float64.  Scaling for
+ * contexts past the trained one (factor s >= 1):
+ *   LINEAR  f_i / s
+ *   NTK     base s^(rotary_dim / (rotary_dim - 2)) as the base (rotary_dim > 2)
+ *   YARN    by parts: with t_i = original_context f_i / (2 pi) turns in the
+ *           original context and g = (t_i - beta_slow) / (beta_fast -
+ *           beta_slow) clamped to [0, 1], f_i (g + (1 - g) / s); cosines and
+ *           sines times 0.1 ln s + 1.
+ * A gain other than 0 replaces the factor on cosines and sines (1 without
+ * YARN). */
+typedef enum { SD_ROPE_HALF = 0, SD_ROPE_INTERLEAVED = 1 } sd_rope_layout;
+typedef enum { SD_ROPE_UNSCALED = 0, SD_ROPE_LINEAR = 1, SD_ROPE_NTK = 2, SD_ROPE_YARN = 3 } sd_rope_scaling;
+typedef struct {
+    double base, factor, gain;
+    double beta_fast, beta_slow; /* YARN: beta_fast > beta_slow >= 0 */
+    int32_t rotary_dim, layout, scaling;
+    int32_t original_context;    /* YARN: >= 1 */
+} sd_rope;
+
+/* Depths and ancestor bits of a tree (HOST arrays, host code): depths[i] = 0
+ * for node 0, else depths[parents[i]] + 1; bit j % 64 of mask[i * ((n + 63) / 64)
+ * + j / 64] is set when node j is node i or one of its ancestors.  depths and
+ * mask may be NULL.  1 <= n <= SD_TREE_MAX.  Errors: INVALID_ARG. */
+sd_status sd_tree_layout(const int32_t *parents, int32_t n, int32_t *depths, uint64_t *mask);
+
+/* Rotates the queries and keys of a QKV product and stores keys and values:
+ * row r of qkv (float32, rows ld_qkv elements apart: n_heads query heads, then
+ * the layer's kv heads of K, then of V) at position positions[r] (int32), or
+ * pos0 + r when positions is NULL; the rotated queries to q_out [n][n_heads
+ * head_dim] (float32, rows ld_q apart, not overlapping qkv), K and V in the
+ * layer's dtype (rounded to nearest even) to position slot + r of the layer.
+ * Rows 16-byte aligned; 1 <= n <= 2^20, 0 <= slot, slot + n <= capacity.  Errors:
+ * INVALID_ARG, CAPACITY, DEVICE. */
+sd_status sd_rope_append(const sd_rope *rope, const float *qkv, int64_t ld_qkv, int32_t n, int32_t n_heads,
+                         const int32_t *positions, int32_t pos0, float *q_out, int64_t ld_q, const sd_kv_layer *kv,
+                         int32_t slot, void *hip_stream);
+
+/* Attention of the n nodes of a tree over the first prefix positions of a
+ * layer and over nodes of the tree (positions prefix .. prefix + n - 1): row r
+ * of q (float32 [n][n_heads head_dim], rows ld_q apart) sees every prefix
+ * position and the nodes j whose bit j is set in row r of mask (uint64 [n][(n +
+ * 63) / 64], as sd_tree_layout writes it; any bits, bits past n are ignored),
+ * or the nodes 0 .. r when mask is NULL.  Scores are scaled by scale (0: 1 /
+ * sqrt(head_dim)); sums are float32.  out [n][n_heads head_dim] (float32, rows
+ * ld_out apart, not overlapping q).  A row that sees nothing gives zeros; what
+ * a row does not see never touches its result, whatever it holds.  workspace
+ * (16-byte aligned) holds at least sd_tree_attention_workspace() bytes for these
+ * sizes and belongs to the call until it has run.  1 <= n <= SD_TREE_MAX, 0 <=
+ * prefix, prefix + n <= capacity.  The same inputs give the same bits.  Errors:
+ * INVALID_ARG, CAPACITY, DEVICE. */
+sd_status sd_tree_attention(const sd_kv_layer *kv, const float *q, int64_t ld_q, int32_t n_heads, int32_t n,
+                            int32_t prefix, const uint64_t *mask, float scale, float *out, int64_t ld_out,
+                            void *workspace, size_t workspace_bytes, void *hip_stream);
+/* Bytes of workspace for these sizes (0 where none is needed, or for sizes
+ * that sd_tree_attention refuses). */
+size_t sd_tree_attention_workspace(const sd_kv_layer *kv, int32_t n_heads, int32_t n, int32_t prefix);
+
+/* The greedy walk over a verified tree.  best[r] is the id of the largest of
+ * the vocab logits of row r (float32, rows ld apart; the lowest id on ties, a
+ * NaN never wins, 0 when nothing does); from node 0 the walk goes to the lowest child whose token is
+ * the best token of its parent, until there is none.  walk (int32 [2 + 2 n])
+ * receives the number of nodes on the path (at least 1), the best token of its
+ * last node, the path (then -1), and best.  tokens and parents: int32 [n]; an
+ * entry of parents outside [0, i) makes node i unreachable.  1 <= n <=
+ * SD_TREE_MAX, vocab >= 1.  workspace (16-byte aligned): at least
+ * sd_tree_accept_workspace() bytes.  Errors: INVALID_ARG, DEVICE. */
+sd_status sd_tree_accept(const float *logits, int64_t ld, int32_t vocab, const int32_t *tokens, const int32_t *parents,
+                         int32_t n, int32_t *walk, void *workspace, size_t workspace_bytes, void *hip_stream);
+size_t sd_tree_accept_workspace(int32_t n, int32_t vocab);
+
+/* Moves the cache rows of a walk together: in each of planes (1 to
+ * 2^24) planes (plane_stride bytes apart, a multiple of 16; rows of row_bytes bytes, a
+ * multiple of 16; kv 16-byte aligned; a cache of sd_kv_cache_create has
+ * n_layers * 2 * n_kv_heads planes of capacity rows) row base + path[i] goes to row base + i for i < count, with
+ * count = walk[0] and path = walk + 2 as sd_tree_accept leaves them for n nodes
+ * (a count outside [1, n] or a path that is not strictly ascending within [0,
+ * n) moves nothing).  Rows past base + count - 1 keep what
+ * they hold.  0 <= base, base + n <= capacity (rows of a plane), 1 <= n <=
+ * SD_TREE_MAX.  Errors: INVALID_ARG, CAPACITY, DEVICE. */
+sd_status sd_kv_keep(void *kv, int64_t planes, int64_t plane_stride, int32_t row_bytes, int32_t capacity, int32_t base,
+                     const int32_t *walk, int32_t n, void *hip_stream);
+
 /* Skip-set search (Sec. 3.3, Eq. 1): z* = argmin f(z) over sublayer masks
  * z in {0, 1}^L, by Bayesian optimisation for a fixed number of steps.
  * Host code; every evaluation of f is one call of the objective.

@@ -26,7 +26,8 @@ EXPORTS = (
     "sd_self_spec_generate", "sd_self_spec_generate_adaptive", "sd_autoregressive_generate",
     "sd_self_spec_sample", "sd_autoregressive_sample", "sd_search_skip_set_fn", "sd_search_skip_set",
     "sd_model_time_kernel", "sd_model_kernel_time", "sd_measure_read_bandwidth", "sd_model_quantize_draft",
-    "sd_model_draft_fp8",
+    "sd_model_draft_fp8", "sd_tree_layout", "sd_rope_append", "sd_tree_attention", "sd_tree_attention_workspace",
+    "sd_tree_accept", "sd_tree_accept_workspace", "sd_kv_keep",
     "sd_last_error", "sd_version",
 )
 
@@ -73,6 +74,20 @@ class sd_sampling(ctypes.Structure):
     _fields_ = [("temperature", ctypes.c_float), ("top_p", ctypes.c_float), ("seed", ctypes.c_uint64)]
 
 
+SD_TREE_MAX = 1024
+
+
+class sd_kv_layer(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("head_stride", ctypes.c_int64),
+                ("row_stride", ctypes.c_int64), ("n_kv_heads", ctypes.c_int32), ("capacity", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class sd_rope(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_double) for n in ("base", "factor", "gain", "beta_fast", "beta_slow")] + [
+        (n, ctypes.c_int32) for n in ("rotary_dim", "layout", "scaling", "original_context")]
+
+
 SD_SEARCH_MEASURED, SD_SEARCH_MODELED = 0, 1
 
 
@@ -115,7 +130,7 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     if not os.path.exists(path):
         raise RuntimeError(f"{path} is not built: run `python -m paper_2309_08168_amd.build` first")
     lib = ctypes.CDLL(path)
-    vp, i32, p = ctypes.c_void_p, ctypes.c_int32, ctypes.POINTER
+    vp, i32, i64, p = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.POINTER
     sig = {
         "sd_model_create": ([p(sd_config), p(sd_weights), vp, p(vp)], ctypes.c_int),
         "sd_model_destroy": ([vp], ctypes.c_int),
@@ -144,6 +159,14 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "sd_model_quantize_draft": ([vp, vp], ctypes.c_int),
         "sd_model_draft_fp8": ([vp, i32, i32, p(vp), p(vp)], ctypes.c_int),
         "sd_measure_read_bandwidth": ([vp, ctypes.c_size_t, i32, i32, i32, vp, vp, p(ctypes.c_double)], ctypes.c_int),
+        "sd_tree_layout": ([vp, i32, vp, vp], ctypes.c_int),
+        "sd_rope_append": ([p(sd_rope), vp, i64, i32, i32, vp, i32, vp, i64, p(sd_kv_layer), i32, vp], ctypes.c_int),
+        "sd_tree_attention": ([p(sd_kv_layer), vp, i64, i32, i32, i32, vp, ctypes.c_float, vp, i64, vp,
+                               ctypes.c_size_t, vp], ctypes.c_int),
+        "sd_tree_attention_workspace": ([p(sd_kv_layer), i32, i32, i32], ctypes.c_size_t),
+        "sd_tree_accept": ([vp, i64, i32, vp, vp, i32, vp, vp, ctypes.c_size_t, vp], ctypes.c_int),
+        "sd_tree_accept_workspace": ([i32, i32], ctypes.c_size_t),
+        "sd_kv_keep": ([vp, i64, i64, i32, i32, i32, vp, i32, vp], ctypes.c_int),
         "sd_last_error": ([], ctypes.c_char_p),
         "sd_version": ([], ctypes.c_char_p),
     }
@@ -400,6 +423,185 @@ def measure_read_bandwidth(buf, nbytes: int, wg_per_cu: int, iters: int, sink, s
                                            ctypes.c_void_p(sink.data_ptr()), ctypes.c_void_p(st.cuda_stream),
                                            ctypes.byref(ms)))
     return ms.value
+
+
+# ----------------------------------------------------------------------------
+# Token trees: operators on torch tensors, on the current stream of their device.
+
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
+
+
+def rope(base: float = 10000.0, rotary_dim: int = 128, layout: str = "half", scaling: str = "none",
+         factor: float = 1.0, original_context: int = 4096, beta_fast: float = 32.0, beta_slow: float = 1.0,
+         gain: float = 0.0) -> sd_rope:
+    """A rotary form (sd_rope): layout "half" or "interleaved", scaling "none",
+    "linear", "ntk" or "yarn"; gain 0 is the form's own."""
+    return sd_rope(base, factor, gain, beta_fast, beta_slow, rotary_dim, ROPE_LAYOUTS[layout], ROPE_SCALINGS[scaling],
+                   original_context)
+
+
+def tree_layout(parents):
+    """sd_tree_layout: (depths int32 [n], mask uint64 [n, (n + 63) // 64])."""
+    par = np.ascontiguousarray(parents, dtype=np.int32)
+    depths = np.empty(par.size, np.int32)
+    mask = np.empty((par.size, (par.size + 63) // 64), np.uint64)
+    check(load().sd_tree_layout(_ptr(par), par.size, _ptr(depths), _ptr(mask)))
+    return depths, mask
+
+
+def _refuse(message: str):
+    raise SDError(SD_ERR_INVALID_ARG, message)
+
+
+def _on(device, *tensors):
+    """Every tensor on the one GPU `device`."""
+    for t in tensors:
+        if t is not None and t.device != device:
+            _refuse(f"tensors on {device} and {t.device}")
+
+
+def _call(device, fn, *args):
+    """fn(..., stream) on the current stream of `device`, with that device current."""
+    import torch
+
+    if device.type != "cuda":
+        _refuse("the operators take tensors on a GPU")
+    if device.index == torch.cuda.current_device():
+        check(fn(*args, torch.cuda.current_stream(device).cuda_stream))
+    else:
+        with torch.cuda.device(device):
+            check(fn(*args, torch.cuda.current_stream(device).cuda_stream))
+
+
+def kv_layer(k, v) -> sd_kv_layer:
+    """sd_kv_layer over tensors [n_kv_heads, capacity, head_dim] (float32 or
+    bfloat16, elements of a row adjacent, the same strides)."""
+    import torch
+
+    if k.dim() != 3 or k.shape != v.shape or k.dtype != v.dtype or k.stride() != v.stride() or k.stride(2) != 1:
+        _refuse("k and v are [n_kv_heads, capacity, head_dim] of one type and one set of strides, rows contiguous")
+    if k.dtype == torch.bfloat16:
+        dtype = SD_BF16
+    elif k.dtype == torch.float32:
+        dtype = SD_F32
+    else:
+        _refuse("k and v are float32 or bfloat16")
+    return sd_kv_layer(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.shape[0], k.shape[1], k.shape[2], dtype)
+
+
+def _rows(t, what: str, shape=None):
+    """Row stride of a float32 tensor [n, ...] whose rows are contiguous."""
+    import torch
+
+    if t.dtype != torch.float32 or (shape is not None and tuple(t.shape) != tuple(shape)):
+        _refuse(f"{what} is float32" + ("" if shape is None else f" {list(shape)}"))
+    want = 1
+    for i in range(t.dim() - 1, 0, -1):
+        if t.stride(i) != want and t.shape[i] != 1:
+            _refuse(f"the rows of {what} are contiguous")
+        want *= t.shape[i]
+    return t.stride(0) if t.shape[0] > 1 else want
+
+
+def rope_append(form: sd_rope, qkv, k, v, slot: int, n_heads: int, positions=None, pos0: int = 0, q_out=None):
+    """sd_rope_append: qkv float32 [n, (n_heads + 2 n_kv_heads) head_dim], k and v
+    as in kv_layer, rows stored at slot ..; positions int32 [n] or None: pos0 ..
+    Returns the rotated queries, float32 [n, n_heads, head_dim]."""
+    import torch
+
+    layer = kv_layer(k, v)
+    n, d = qkv.shape[0], layer.head_dim
+    ld = _rows(qkv, "qkv", (n, (n_heads + 2 * layer.n_kv_heads) * d))
+    if positions is not None and (positions.dtype != torch.int32 or positions.shape != (n,) or
+                                  not positions.is_contiguous()):
+        _refuse("positions is a contiguous int32 [n]")
+    if q_out is None:
+        q_out = torch.empty((n, n_heads, d), dtype=torch.float32, device=qkv.device)
+    ldq = _rows(q_out, "q_out", (n, n_heads, d))
+    _on(qkv.device, k, v, positions, q_out)
+    _call(qkv.device, load().sd_rope_append, ctypes.byref(form), qkv.data_ptr(), ld, n, n_heads,
+          None if positions is None else positions.data_ptr(), pos0, q_out.data_ptr(), ldq, ctypes.byref(layer), slot)
+    return q_out
+
+
+def _workspace(workspace, nbytes: int, device):
+    import torch
+
+    if workspace is not None:
+        if not workspace.is_contiguous():
+            _refuse("workspace is contiguous")
+        return workspace, workspace.numel() * workspace.element_size()
+    return torch.empty(nbytes, dtype=torch.uint8, device=device), nbytes
+
+
+def tree_attention(q, k, v, prefix: int, mask=None, scale: float = 0.0, out=None, workspace=None):
+    """sd_tree_attention: q float32 [n, n_heads, head_dim], k and v as in
+    kv_layer, mask int64 or uint64 [n, (n + 63) // 64] or None (row r sees nodes
+    0 .. r), scale 0: 1 / sqrt(head_dim).  Returns out, like q; workspace: a tensor of
+    at least tree_attention_workspace() bytes (else one is allocated)."""
+    import torch
+
+    layer = kv_layer(k, v)
+    n, h = q.shape[0], q.shape[1]
+    shape = (n, h, layer.head_dim)
+    ld = _rows(q, "q", shape)
+    if mask is not None and (mask.dtype not in (torch.int64, torch.uint64) or
+                             mask.shape != (n, (n + 63) // 64) or not mask.is_contiguous()):
+        _refuse("mask is a contiguous int64 or uint64 [n, (n + 63) // 64]")
+    if out is None:
+        out = torch.empty(shape, dtype=torch.float32, device=q.device)
+    ldo = _rows(out, "out", shape)
+    ref = ctypes.byref(layer)
+    ws, nbytes = _workspace(workspace, load().sd_tree_attention_workspace(ref, h, n, prefix), q.device)
+    _on(q.device, k, v, mask, out, ws)
+    _call(q.device, load().sd_tree_attention, ref, q.data_ptr(), ld, h, n, prefix,
+          None if mask is None else mask.data_ptr(), scale, out.data_ptr(), ldo, ws.data_ptr(), nbytes)
+    return out
+
+
+def tree_attention_workspace(k, v, n_heads: int, n: int, prefix: int) -> int:
+    """Bytes of workspace tree_attention needs for these sizes."""
+    return int(load().sd_tree_attention_workspace(ctypes.byref(kv_layer(k, v)), n_heads, n, prefix))
+
+
+def tree_accept(logits, tokens, parents, walk=None, workspace=None):
+    """sd_tree_accept: logits float32 [n, vocab], tokens and parents int32 [n].
+    Returns walk, int32 [2 + 2 n]: nodes on the path, the next token, the path
+    (then -1), each node's best token."""
+    import torch
+
+    n, vocab = logits.shape
+    ld = _rows(logits, "logits")
+    for t in (tokens, parents):
+        if t.dtype != torch.int32 or t.shape != (n,) or not t.is_contiguous():
+            _refuse("tokens and parents are contiguous int32 [n]")
+    if walk is None:
+        walk = torch.empty(2 + 2 * n, dtype=torch.int32, device=logits.device)
+    if walk.dtype != torch.int32 or walk.shape != (2 + 2 * n,) or not walk.is_contiguous():
+        _refuse("walk is a contiguous int32 [2 + 2 n]")
+    ws, nbytes = _workspace(workspace, load().sd_tree_accept_workspace(n, vocab), logits.device)
+    _on(logits.device, tokens, parents, walk, ws)
+    _call(logits.device, load().sd_tree_accept, logits.data_ptr(), ld, vocab, tokens.data_ptr(), parents.data_ptr(), n,
+          walk.data_ptr(), ws.data_ptr(), nbytes)
+    return walk
+
+
+def kv_keep(kv, base: int, walk):
+    """sd_kv_keep over a contiguous tensor [..., capacity, head_dim] (every plane
+    of a cache), with a walk of tree_accept; returns kv."""
+    import torch
+
+    if kv.dim() < 2 or not kv.is_contiguous():
+        _refuse("kv is a contiguous [..., capacity, head_dim]")
+    n = (walk.numel() - 2) // 2
+    if walk.dtype != torch.int32 or walk.dim() != 1 or walk.numel() != 2 + 2 * n or not walk.is_contiguous():
+        _refuse("walk is a contiguous int32 [2 + 2 n]")
+    cap, row = kv.shape[-2], kv.shape[-1] * kv.element_size()
+    _on(kv.device, walk)
+    _call(kv.device, load().sd_kv_keep, kv.data_ptr(), kv.numel() // max(cap * kv.shape[-1], 1), cap * row, row, cap, base,
+          walk.data_ptr(), n)
+    return kv
 
 
 def _search_call(call, n_dims: int, objective: int, cost, params: dict) -> dict:

@@ -1621,15 +1621,6 @@ const Plan *find_plan(const sd_model *m, int kind, int regime) {
 // ---------------------------------------------------------------------------
 // C ABI
 
-#define SD_GUARD(body)                                                                                 \
-    try {                                                                                              \
-        body                                                                                           \
-    } catch (const std::bad_alloc &) {                                                                 \
-        return fail(SD_ERR_OOM, "host allocation failed");                                             \
-    } catch (...) {                                                                                    \
-        return fail(SD_ERR_DEVICE, "unexpected internal error");                                       \
-    }
-
 extern "C" {
 
 sd_status sd_model_create(const sd_config *config, const sd_weights *weights, void *hip_stream, sd_model **out) {
