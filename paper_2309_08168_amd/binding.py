@@ -454,85 +454,100 @@ def _refuse(message: str):
     raise SDError(SD_ERR_INVALID_ARG, message)
 
 
-def _on(device, *tensors):
-    """Every tensor on the one GPU `device`."""
-    for t in tensors:
-        if t is not None and t.device != device:
-            _refuse(f"tensors on {device} and {t.device}")
+_torch = None      # looked up once: the operators run for a few microseconds, and an
+_raw_stream = None  # import statement or a Stream object costs one or two of them
+_DTYPES: Dict = {}  # torch dtypes of a cache
 
 
-def _call(device, fn, *args):
-    """fn(..., stream) on the current stream of `device`, with that device current."""
-    import torch
+def _use_torch():
+    global _torch, _raw_stream
+    if _torch is None:
+        import torch
 
-    if device.type != "cuda":
+        _DTYPES.update({torch.float32: SD_F32, torch.bfloat16: SD_BF16})
+        _raw_stream = torch._C._cuda_getCurrentRawStream  # (device index) -> hipStream_t
+        _torch = torch
+    return _torch
+
+
+def _device(t, *others) -> int:
+    """The index of the GPU that every tensor is on."""
+    dev = t.get_device()
+    if dev < 0:
         _refuse("the operators take tensors on a GPU")
-    if device.index == torch.cuda.current_device():
-        check(fn(*args, torch.cuda.current_stream(device).cuda_stream))
+    for o in others:
+        if o is not None and o.get_device() != dev:
+            _refuse("the tensors are on different devices")
+    return dev
+
+
+def _call(dev: int, fn, *args):
+    """fn(..., stream) on the current stream of GPU dev, with that GPU current."""
+    if dev == _torch.cuda.current_device():
+        status = fn(*args, _raw_stream(dev))
     else:
-        with torch.cuda.device(device):
-            check(fn(*args, torch.cuda.current_stream(device).cuda_stream))
+        with _torch.cuda.device(dev):
+            status = fn(*args, _raw_stream(dev))
+    if status != SD_OK:
+        check(status)
 
 
 def kv_layer(k, v) -> sd_kv_layer:
     """sd_kv_layer over tensors [n_kv_heads, capacity, head_dim] (float32 or
     bfloat16, elements of a row adjacent, the same strides)."""
-    import torch
-
-    if k.dim() != 3 or k.shape != v.shape or k.dtype != v.dtype or k.stride() != v.stride() or k.stride(2) != 1:
-        _refuse("k and v are [n_kv_heads, capacity, head_dim] of one type and one set of strides, rows contiguous")
-    if k.dtype == torch.bfloat16:
-        dtype = SD_BF16
-    elif k.dtype == torch.float32:
-        dtype = SD_F32
-    else:
-        _refuse("k and v are float32 or bfloat16")
-    return sd_kv_layer(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.shape[0], k.shape[1], k.shape[2], dtype)
+    _use_torch()
+    dtype = _DTYPES.get(k.dtype)
+    shape, stride = k.shape, k.stride()
+    if dtype is None or len(shape) != 3 or stride[2] != 1 or v.dtype != k.dtype or v.shape != shape or \
+            v.stride() != stride:
+        _refuse("k and v are [n_kv_heads, capacity, head_dim], float32 or bfloat16, of one type and one set of strides, "
+                "rows contiguous")
+    return sd_kv_layer(k.data_ptr(), v.data_ptr(), stride[0], stride[1], shape[0], shape[1], shape[2], dtype)
 
 
-def _rows(t, what: str, shape=None):
-    """Row stride of a float32 tensor [n, ...] whose rows are contiguous."""
-    import torch
-
-    if t.dtype != torch.float32 or (shape is not None and tuple(t.shape) != tuple(shape)):
-        _refuse(f"{what} is float32" + ("" if shape is None else f" {list(shape)}"))
-    want = 1
-    for i in range(t.dim() - 1, 0, -1):
-        if t.stride(i) != want and t.shape[i] != 1:
+def _rows(t, shape, what: str) -> int:
+    """Row stride of a float32 tensor of that shape whose rows are contiguous."""
+    if t.dtype != _torch.float32 or t.shape != shape:
+        _refuse(f"{what} is float32 {list(shape)}")
+    stride, want = t.stride(), 1
+    for i in range(len(shape) - 1, 0, -1):
+        if stride[i] != want and shape[i] != 1:
             _refuse(f"the rows of {what} are contiguous")
-        want *= t.shape[i]
-    return t.stride(0) if t.shape[0] > 1 else want
+        want *= shape[i]
+    return stride[0] if shape[0] > 1 else want
+
+
+def _words(t, shape, what: str) -> int:
+    """Address of a contiguous int32 tensor of that shape."""
+    if t.dtype != _torch.int32 or t.shape != shape or not t.is_contiguous():
+        _refuse(f"{what} is a contiguous int32 {list(shape)}")
+    return t.data_ptr()
+
+
+def _space(workspace, nbytes: int, like):
+    """(tensor, bytes): the caller's workspace, or one of nbytes on the current stream."""
+    if workspace is None:
+        return like.new_empty(nbytes, dtype=_torch.uint8) if nbytes else None, nbytes
+    if not workspace.is_contiguous():
+        _refuse("workspace is contiguous")
+    return workspace, workspace.numel() * workspace.element_size()
 
 
 def rope_append(form: sd_rope, qkv, k, v, slot: int, n_heads: int, positions=None, pos0: int = 0, q_out=None):
     """sd_rope_append: qkv float32 [n, (n_heads + 2 n_kv_heads) head_dim], k and v
     as in kv_layer, rows stored at slot ..; positions int32 [n] or None: pos0 ..
     Returns the rotated queries, float32 [n, n_heads, head_dim]."""
-    import torch
-
     layer = kv_layer(k, v)
     n, d = qkv.shape[0], layer.head_dim
-    ld = _rows(qkv, "qkv", (n, (n_heads + 2 * layer.n_kv_heads) * d))
-    if positions is not None and (positions.dtype != torch.int32 or positions.shape != (n,) or
-                                  not positions.is_contiguous()):
-        _refuse("positions is a contiguous int32 [n]")
+    ld = _rows(qkv, (n, (n_heads + 2 * layer.n_kv_heads) * d), "qkv")
+    shape = (n, n_heads, d)
     if q_out is None:
-        q_out = torch.empty((n, n_heads, d), dtype=torch.float32, device=qkv.device)
-    ldq = _rows(q_out, "q_out", (n, n_heads, d))
-    _on(qkv.device, k, v, positions, q_out)
-    _call(qkv.device, load().sd_rope_append, ctypes.byref(form), qkv.data_ptr(), ld, n, n_heads,
-          None if positions is None else positions.data_ptr(), pos0, q_out.data_ptr(), ldq, ctypes.byref(layer), slot)
+        q_out, ldq = qkv.new_empty(shape), n_heads * d
+    else:
+        ldq = _rows(q_out, shape, "q_out")
+    _call(_device(qkv, k, v, positions, q_out), load().sd_rope_append, form, qkv.data_ptr(), ld, n, n_heads,
+          None if positions is None else _words(positions, (n,), "positions"), pos0, q_out.data_ptr(), ldq, layer, slot)
     return q_out
-
-
-def _workspace(workspace, nbytes: int, device):
-    import torch
-
-    if workspace is not None:
-        if not workspace.is_contiguous():
-            _refuse("workspace is contiguous")
-        return workspace, workspace.numel() * workspace.element_size()
-    return torch.empty(nbytes, dtype=torch.uint8, device=device), nbytes
 
 
 def tree_attention(q, k, v, prefix: int, mask=None, scale: float = 0.0, out=None, workspace=None):
@@ -540,67 +555,68 @@ def tree_attention(q, k, v, prefix: int, mask=None, scale: float = 0.0, out=None
     kv_layer, mask int64 or uint64 [n, (n + 63) // 64] or None (row r sees nodes
     0 .. r), scale 0: 1 / sqrt(head_dim).  Returns out, like q; workspace: a tensor of
     at least tree_attention_workspace() bytes (else one is allocated)."""
-    import torch
-
-    layer = kv_layer(k, v)
-    n, h = q.shape[0], q.shape[1]
-    shape = (n, h, layer.head_dim)
-    ld = _rows(q, "q", shape)
-    if mask is not None and (mask.dtype not in (torch.int64, torch.uint64) or
-                             mask.shape != (n, (n + 63) // 64) or not mask.is_contiguous()):
-        _refuse("mask is a contiguous int64 or uint64 [n, (n + 63) // 64]")
+    layer, lib = kv_layer(k, v), load()
+    n, h, d = shape = q.shape
+    if d != layer.head_dim:
+        _refuse("q and the layer have one head_dim")
+    ld = _rows(q, shape, "q")
+    if mask is None:
+        bits = None
+    else:
+        if mask.dtype not in (_torch.int64, _torch.uint64) or mask.shape != (n, (n + 63) // 64) or \
+                not mask.is_contiguous():
+            _refuse("mask is a contiguous int64 or uint64 [n, (n + 63) // 64]")
+        bits = mask.data_ptr()
     if out is None:
-        out = torch.empty(shape, dtype=torch.float32, device=q.device)
-    ldo = _rows(out, "out", shape)
-    ref = ctypes.byref(layer)
-    ws, nbytes = _workspace(workspace, load().sd_tree_attention_workspace(ref, h, n, prefix), q.device)
-    _on(q.device, k, v, mask, out, ws)
-    _call(q.device, load().sd_tree_attention, ref, q.data_ptr(), ld, h, n, prefix,
-          None if mask is None else mask.data_ptr(), scale, out.data_ptr(), ldo, ws.data_ptr(), nbytes)
+        out, ldo = q.new_empty(shape), h * d
+    else:
+        ldo = _rows(out, shape, "out")
+    ws, nbytes = _space(workspace, lib.sd_tree_attention_workspace(layer, h, n, prefix), q)
+    _call(_device(q, k, v, mask, out, ws), lib.sd_tree_attention, layer, q.data_ptr(), ld, h, n, prefix, bits, scale,
+          out.data_ptr(), ldo, None if ws is None else ws.data_ptr(), nbytes)
     return out
 
 
 def tree_attention_workspace(k, v, n_heads: int, n: int, prefix: int) -> int:
     """Bytes of workspace tree_attention needs for these sizes."""
-    return int(load().sd_tree_attention_workspace(ctypes.byref(kv_layer(k, v)), n_heads, n, prefix))
+    return int(load().sd_tree_attention_workspace(kv_layer(k, v), n_heads, n, prefix))
 
 
 def tree_accept(logits, tokens, parents, walk=None, workspace=None):
     """sd_tree_accept: logits float32 [n, vocab], tokens and parents int32 [n].
     Returns walk, int32 [2 + 2 n]: nodes on the path, the next token, the path
-    (then -1), each node's best token."""
-    import torch
-
-    n, vocab = logits.shape
-    ld = _rows(logits, "logits")
-    for t in (tokens, parents):
-        if t.dtype != torch.int32 or t.shape != (n,) or not t.is_contiguous():
-            _refuse("tokens and parents are contiguous int32 [n]")
+    (then -1), each node's best token; workspace: a tensor of at least
+    tree_accept_workspace() bytes (else one is allocated)."""
+    _use_torch()
+    lib = load()
+    n, vocab = shape = logits.shape
+    ld = _rows(logits, shape, "logits")
     if walk is None:
-        walk = torch.empty(2 + 2 * n, dtype=torch.int32, device=logits.device)
-    if walk.dtype != torch.int32 or walk.shape != (2 + 2 * n,) or not walk.is_contiguous():
-        _refuse("walk is a contiguous int32 [2 + 2 n]")
-    ws, nbytes = _workspace(workspace, load().sd_tree_accept_workspace(n, vocab), logits.device)
-    _on(logits.device, tokens, parents, walk, ws)
-    _call(logits.device, load().sd_tree_accept, logits.data_ptr(), ld, vocab, tokens.data_ptr(), parents.data_ptr(), n,
-          walk.data_ptr(), ws.data_ptr(), nbytes)
+        walk = tokens.new_empty(2 + 2 * n)
+    ws, nbytes = _space(workspace, lib.sd_tree_accept_workspace(n, vocab), logits)
+    _call(_device(logits, tokens, parents, walk, ws), lib.sd_tree_accept, logits.data_ptr(), ld, vocab,
+          _words(tokens, (n,), "tokens"), _words(parents, (n,), "parents"), n, _words(walk, (2 + 2 * n,), "walk"),
+          None if ws is None else ws.data_ptr(), nbytes)
     return walk
+
+
+def tree_accept_workspace(n: int, vocab: int) -> int:
+    """Bytes of workspace tree_accept needs for these sizes."""
+    return int(load().sd_tree_accept_workspace(n, vocab))
 
 
 def kv_keep(kv, base: int, walk):
     """sd_kv_keep over a contiguous tensor [..., capacity, head_dim] (every plane
     of a cache), with a walk of tree_accept; returns kv."""
-    import torch
-
-    if kv.dim() < 2 or not kv.is_contiguous():
+    _use_torch()
+    shape = kv.shape
+    if len(shape) < 2 or not kv.is_contiguous():
         _refuse("kv is a contiguous [..., capacity, head_dim]")
     n = (walk.numel() - 2) // 2
-    if walk.dtype != torch.int32 or walk.dim() != 1 or walk.numel() != 2 + 2 * n or not walk.is_contiguous():
-        _refuse("walk is a contiguous int32 [2 + 2 n]")
-    cap, row = kv.shape[-2], kv.shape[-1] * kv.element_size()
-    _on(kv.device, walk)
-    _call(kv.device, load().sd_kv_keep, kv.data_ptr(), kv.numel() // max(cap * kv.shape[-1], 1), cap * row, row, cap, base,
-          walk.data_ptr(), n)
+    at = _words(walk, (2 + 2 * n,), "walk")
+    cap, row = shape[-2], shape[-1] * kv.element_size()
+    _call(_device(kv, walk), load().sd_kv_keep, kv.data_ptr(), kv.numel() // max(cap * shape[-1], 1), cap * row, row, cap,
+          base, at, n)
     return kv
 
 

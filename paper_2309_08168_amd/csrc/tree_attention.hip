@@ -23,7 +23,14 @@ using namespace sdk;
 namespace {
 
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
 
 constexpr int KB = 64;  // keys of a block
 
@@ -39,6 +46,7 @@ struct TreeAttnArgs {
     float2 *part_ml;  // [splits][n H]: (maximum, sum), in units of log2
     float scale;      // of the scores, times log2(e)
     int32_t n, words, prefix, n_heads, n_kv_heads, G, rows, q_tiles;  // rows = n G
+    int32_t q_rows;                                                   // of a tile
     int32_t prefix_blocks, blocks, splits, per_split;                 // per_split: blocks of a share
 };
 
@@ -70,21 +78,7 @@ __device__ __forceinline__ uint64_t visible(const TreeAttnArgs &a, const Block &
     return last < 0 ? 0 : (last >= 63 ? ~0ull : (2ull << last) - 1) & all;
 }
 
-__device__ __forceinline__ void load4(const float *p, float (&x)[4]) {
-    const f32x4_t v = *reinterpret_cast<const f32x4_t *>(p);
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-        x[j] = v[j];
-}
-__device__ __forceinline__ void load4(const uint16_t *p, float (&x)[4]) {
-    const uint2 v = *reinterpret_cast<const uint2 *>(p);
-    x[0] = __uint_as_float(v.x << 16);
-    x[1] = __uint_as_float(v.x & 0xffff0000u);
-    x[2] = __uint_as_float(v.y << 16);
-    x[3] = __uint_as_float(v.y & 0xffff0000u);
-}
-__device__ __forceinline__ float load1(const float *p) { return *p; }
-__device__ __forceinline__ float load1(const uint16_t *p) { return __uint_as_float((uint32_t)*p << 16); }
+__device__ __forceinline__ f32x4_t load4(const float *p) { return *reinterpret_cast<const f32x4_t *>(p); }
 
 __device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
 
@@ -100,7 +94,7 @@ __device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0
 // at the end.
 constexpr int TA_WAVES = 4;
 
-template <typename TK, int D>
+template <int D>
 __global__ __launch_bounds__(TA_WAVES * 64) void k_tree_attn_f32(TreeAttnArgs a) {
     constexpr int ES = D / 16, OP = 17;
     __shared__ float tile[TA_WAVES][D * OP];
@@ -108,18 +102,14 @@ __global__ __launch_bounds__(TA_WAVES * 64) void k_tree_attn_f32(TreeAttnArgs a)
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane & 15, g4 = lane >> 4;
     const int qt = blockIdx.x % a.q_tiles, g = blockIdx.x / a.q_tiles, split = blockIdx.y;
     const int b0 = split * a.per_split, b1 = min(a.blocks, b0 + a.per_split);
-    const TK *K = static_cast<const TK *>(a.k) + (int64_t)g * a.head_stride;
-    const TK *V = static_cast<const TK *>(a.v) + (int64_t)g * a.head_stride;
+    const float *K = static_cast<const float *>(a.k) + (int64_t)g * a.head_stride;
+    const float *V = static_cast<const float *>(a.v) + (int64_t)g * a.head_stride;
     const int row = min(qt * 16 + c, a.rows - 1), node = row / a.G, head = g * a.G + row - node * a.G;
 
-    float qx[ES][4];
+    f32x4_t qx[ES];
 #pragma unroll
-    for (int j = 0; j < ES; ++j) {
-        load4(a.q + (int64_t)node * a.ld_q + (int64_t)head * D + 16 * j + 4 * g4, qx[j]);
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-            qx[j][u] *= a.scale;
-    }
+    for (int j = 0; j < ES; ++j)
+        qx[j] = load4(a.q + (int64_t)node * a.ld_q + (int64_t)head * D + 16 * j + 4 * g4) * a.scale;
     float m_run = -INFINITY, l_run = 0.0f;
     f32x4_t o[ES];
 #pragma unroll
@@ -131,12 +121,11 @@ __global__ __launch_bounds__(TA_WAVES * 64) void k_tree_attn_f32(TreeAttnArgs a)
         if (16 * wave >= k.len)
             continue;  // uniform over the wave
         // keys past the block read its last one; their scores are masked
-        const TK *kp = K + (int64_t)(k.first + min(16 * wave + c, k.len - 1)) * a.row_stride + 4 * g4;
+        const float *kp = K + (int64_t)(k.first + min(16 * wave + c, k.len - 1)) * a.row_stride + 4 * g4;
         f32x4_t s = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int j = 0; j < ES; ++j) {
-            float kx[4];
-            load4(kp + 16 * j, kx);
+            const f32x4_t kx = load4(kp + 16 * j);
 #pragma unroll
             for (int u = 0; u < 4; ++u)
                 s = __builtin_amdgcn_mfma_f32_16x16x4f32(kx[u], qx[j][u], s, 0, 0, 0);
@@ -159,7 +148,7 @@ __global__ __launch_bounds__(TA_WAVES * 64) void k_tree_attn_f32(TreeAttnArgs a)
             p[v] = __builtin_amdgcn_exp2f(s[v] - m_use);
         l_run += (p[0] + p[1]) + (p[2] + p[3]);
         m_run = m_new;
-        const TK *vp[4];
+        const float *vp[4];
         float vx[ES][4];
         bool odd = false;
 #pragma unroll
@@ -170,7 +159,7 @@ __global__ __launch_bounds__(TA_WAVES * 64) void k_tree_attn_f32(TreeAttnArgs a)
             o[t] *= sc;
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
-                vx[t][v] = load1(vp[v] + 16 * t + c);
+                vx[t][v] = vp[v][16 * t + c];
                 odd |= !finite(vx[t][v]);
             }
         }
@@ -185,7 +174,7 @@ __global__ __launch_bounds__(TA_WAVES * 64) void k_tree_attn_f32(TreeAttnArgs a)
             // see it must not add 0 times it.  Lane (c, g4) holds elements
             // 16 t + 4 g4 + u of row c.
             for (int key = 0; key < 16; ++key) {
-                const TK *vr = V + (int64_t)(k.first + min(16 * wave + key, k.len - 1)) * a.row_stride + 4 * g4;
+                const float *vr = V + (int64_t)(k.first + min(16 * wave + key, k.len - 1)) * a.row_stride + 4 * g4;
                 float pk = p[0];
 #pragma unroll
                 for (int v = 1; v < 4; ++v)
@@ -193,8 +182,7 @@ __global__ __launch_bounds__(TA_WAVES * 64) void k_tree_attn_f32(TreeAttnArgs a)
                 pk = __shfl(pk, 16 * (key >> 2) + c, 64);
 #pragma unroll
                 for (int t = 0; t < ES; ++t) {
-                    float w[4];
-                    load4(vr + 16 * t, w);
+                    const f32x4_t w = load4(vr + 16 * t);
 #pragma unroll
                     for (int u = 0; u < 4; ++u)
                         o[t][u] = pk != 0.0f ? fmaf(pk, w[u], o[t][u]) : o[t][u];
@@ -242,6 +230,324 @@ __global__ __launch_bounds__(TA_WAVES * 64) void k_tree_attn_f32(TreeAttnArgs a)
     }
 }
 
+// ---------------------------------------------------------------------------
+// bfloat16 caches: matrix cores.  q (times scale log2(e)) and the weights are
+// float32; each is held as three bfloat16 terms that add up to it exactly, so that
+// only the float32 sums round.  That issues three times the flops: 1.5 matrix
+// cycles a score and SIMD, next to about as many for its softmax and terms.
+//
+// NQ x NK waves take 32 NQ rows of a kv head; the K and V rows of a block come
+// straight into LDS one block ahead, and all waves read them there.  NK = 2 waves
+// share a block's keys where there are few rows.  32 keys at a time: scores S^T =
+// K q as 32x32x16 products leave lane (col, half) the keys 8 (v / 4) + 4 half +
+// v % 4, v = 0..15, of row col; values v = 8 j .. 8 j + 7 are the slots of the
+// j-th 16-key value product, so the weights stay in their lanes and V^T is read
+// to match, transposed on its way out of LDS.
+//
+// LDS lines are 256 bytes, 16 chunks of 16 bytes: 128 / D rows.  Chunk p of line s
+// lies at p ^ swz(s), which spreads the 16 rows of a K read and the four rows of a
+// V read over all banks; the loads permute the chunks of a line on the way in.
+
+__device__ __forceinline__ f32x16_t mfma32(u32x4_t a, u32x4_t b, f32x16_t c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c,
+                                                   0, 0, 0);
+}
+__device__ __forceinline__ uint32_t cvt_pk(float a, float b) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), bf16x2_t));
+}
+// The three terms of two values, packed.
+__device__ __forceinline__ void terms2(float a, float b, uint32_t (&t)[X_TERMS]) {
+    t[0] = cvt_pk(a, b);
+    const float a1 = a - __uint_as_float(t[0] << 16), b1 = b - __uint_as_float(t[0] & 0xffff0000u);
+    t[1] = cvt_pk(a1, b1);
+    t[2] = cvt_pk(a1 - __uint_as_float(t[1] << 16), b1 - __uint_as_float(t[1] & 0xffff0000u));
+}
+
+// Sixteen bytes per lane from g to LDS at l + 16 lane (l the same in every lane).
+// The compiler does not see these loads; the kernel waits for them itself.  They
+// have no register result; M0 holds the LDS address and needs one wait state.
+__device__ __forceinline__ void load_to_lds16(const uint16_t *g, uint16_t *l) {
+    const uint32_t off = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint16_t *)l;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(
+                     __builtin_amdgcn_readfirstlane(off)),
+                 "v"(g)
+                 : "memory", "m0");
+}
+
+template <int D>
+struct Lines {  // where a block's rows lie in LDS
+    static constexpr int C = D / 8, RPL = 16 / C;  // chunks of a row, rows of a line
+    __device__ static int swz(int s) {
+        return C == 16 ? ((s & 3) << 2) | ((s >> 2) & 3) : C == 8 ? ((s & 1) << 2) | ((s >> 1) & 3) : s & (RPL == 4 ? 3 : 1);
+    }
+    // element offset of chunk c of row r
+    __device__ static int at(int r, int c) {
+        const int s = r / RPL;
+        return s * 128 + 8 * (((r % RPL) * C + c) ^ swz(s));
+    }
+};
+
+template <int D, int NQ, int NK>
+__global__ __launch_bounds__(64 * NQ * NK, NQ * NK == 2 ? 1 : 2) void k_tree_attn_mfma(TreeAttnArgs a) {
+    constexpr int T = X_TERMS, NW = NQ * NK, ES = D / 16, ET = D < 32 ? 1 : D / 32;
+    constexpr int LOADS = 2 * (D / 8);  // 1 KB loads of a block's K and V
+    using L = Lines<D>;
+    __shared__ __attribute__((aligned(1024))) uint16_t kv[2][2][KB * D];  // [block % 2][K, V]
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+    const int wq = wave % NQ, wk = wave / NQ;
+    const int g = blockIdx.x % a.n_kv_heads, rest = blockIdx.x / a.n_kv_heads;
+    const int qt = rest % a.q_tiles, split = rest / a.q_tiles;
+    const int b0 = split * a.per_split, b1 = min(a.blocks, b0 + a.per_split);
+    const int r0 = (qt * NQ + wq) * 32;
+    const bool live = r0 < a.rows;  // uniform over the wave: a wave without rows loads and waits with the others
+    const int row = min(r0 + col, a.rows - 1), node = row / a.G, head = g * a.G + row - node * a.G;
+    const uint16_t *K = static_cast<const uint16_t *>(a.k) + (int64_t)g * a.head_stride;
+    const uint16_t *V = static_cast<const uint16_t *>(a.v) + (int64_t)g * a.head_stride;
+
+    auto load_block = [&](int b, int buf) {
+        const Block k = block_of(a, b);
+        // (fewer registers than with every address of the block at once)
+#pragma unroll 2
+        for (int t = wave; t < LOADS; t += NW) {
+            const int m = t / L::C, u = t % L::C;  // matrix, and 1 KB of it
+            const int s = 4 * u + (lane >> 4), p = (lane & 15) ^ L::swz(s);
+            const int r = min(s * L::RPL + p / L::C, k.len - 1);  // rows past the block: its last
+            load_to_lds16((m ? V : K) + (int64_t)(k.first + r) * a.row_stride + 8 * (p % L::C), &kv[buf][m][u * 512]);
+        }
+    };
+    load_block(b0, 0);
+
+    u32x4_t qf[ES][T];
+    {
+        const float *qs = a.q + (int64_t)node * a.ld_q + (int64_t)head * D + 8 * half;
+#pragma unroll
+        for (int s = 0; s < ES; ++s) {
+            const f32x4_t x0 = *reinterpret_cast<const f32x4_t *>(qs + 16 * s) * a.scale,
+                          x1 = *reinterpret_cast<const f32x4_t *>(qs + 16 * s + 4) * a.scale;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                uint32_t t0[T], t1[T];
+                terms2(x0[2 * j], x0[2 * j + 1], t0);
+                terms2(x1[2 * j], x1[2 * j + 1], t1);
+#pragma unroll
+                for (int i = 0; i < T; ++i) {
+                    qf[s][i][j] = t0[i];
+                    qf[s][i][2 + j] = t1[i];
+                }
+            }
+        }
+    }
+    // V^T reads: ds_read_b64_tr_b16 hands lane l of each 16-lane group element
+    // l % 4 of the 8 bytes that lanes l / 4 + 4 k (k = 0..3) point at, so lane l
+    // points at row 4 half + l / 4 % 4, columns 16 (l / 16 % 2) + 4 (l % 4) ...
+    // (head_dim 16: columns past it repeat the first, in output rows that
+    // nothing reads)
+    const int v_lane = 2 * (KB * D + L::at(4 * half + ((lane >> 2) & 3), (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) % L::C) +
+                            4 * (lane & 1));
+    const char *lds = reinterpret_cast<const char *>(kv);
+    float m_run = -INFINITY, l_run = 0.0f;
+    f32x16_t o[ET];
+#pragma unroll
+    for (int et = 0; et < ET; ++et)
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+            o[et][v] = 0.0f;
+
+    int buf = 0;
+    for (int b = b0; b < b1; ++b, buf ^= 1) {
+        const Block k = block_of(a, b);
+        // this wave's loads of the block have landed, then everyone's; every
+        // read of the other buffer has returned
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (b + 1 < b1)
+            load_block(b + 1, buf ^ 1);
+        uint16_t *vs = kv[buf][1];
+        bool odd = false;
+        if (k.node0 >= 0) {
+            // A row must not add 0 times an infinity or NaN of a node that it
+            // does not see: they are taken out of the nodes' values, and put
+            // where they belong beside the products.
+            for (int c = threadIdx.x; c < KB * D / 8; c += 64 * NW) {
+                u32x4_t x = reinterpret_cast<const u32x4_t *>(vs)[c];
+                bool hit = false;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if ((x[j] & 0x7f80u) == 0x7f80u) {
+                        x[j] &= 0xffff0000u;
+                        hit = true;
+                    }
+                    if ((x[j] & 0x7f800000u) == 0x7f800000u) {
+                        x[j] &= 0xffffu;
+                        hit = true;
+                    }
+                }
+                if (hit)
+                    reinterpret_cast<u32x4_t *>(vs)[c] = x;
+                odd |= hit;
+            }
+            odd = __syncthreads_or(odd);
+        }
+        const uint64_t see = visible(a, k, node);
+#pragma unroll 1
+        for (int h = wk; h < 2; h += NK) {
+            const uint32_t bits = h ? (uint32_t)(see >> 32) : (uint32_t)see;
+            if (!live || !__any(bits != 0))
+                continue;  // uniform over the wave: no row of it sees these keys
+            f32x16_t s;
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+                s[v] = 0.0f;
+            // byte addresses in LDS: rows 32 h + col, chunk 2 e + half at xk ^ 32 e.
+            // (Hidden from the compiler, which would keep every address of the
+            // loop in a register and spill.)
+            int xk = 2 * (buf * 2 * KB * D + 32 * h * D + L::at(col, half)), xv = 2 * (buf * 2 * KB * D + 32 * h * D) + v_lane;
+            asm volatile("" : "+v"(xk), "+v"(xv));
+#pragma unroll
+            for (int e = 0; e < ES; ++e) {
+                const u32x4_t kf = *reinterpret_cast<const u32x4_t *>(lds + (xk ^ (32 * e)));
+#pragma unroll
+                for (int i = 0; i < T; ++i)
+                    s = mfma32(kf, qf[e][i], s);
+            }
+            if (__any(bits != 0xffffffffu)) {
+                const uint32_t mine = bits >> (4 * half);
+#pragma unroll
+                for (int v = 0; v < 16; ++v)
+                    s[v] = (mine >> (8 * (v >> 2) + (v & 3))) & 1 ? s[v] : -INFINITY;
+            }
+            float mx = s[0];
+#pragma unroll
+            for (int v = 1; v < 16; ++v)
+                mx = fmaxf(mx, s[v]);
+            {
+                const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+                mx = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+            }
+            if (__any(mx > m_run)) {
+                // (a row that has seen no key yet keeps zeros)
+                const float m_new = fmaxf(m_run, mx);
+                const float sc = m_run == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run - m_new);
+                l_run *= sc;
+#pragma unroll
+                for (int et = 0; et < ET; ++et)
+                    o[et] *= sc;
+                m_run = m_new;
+            }
+            const float m_use = m_run == -INFINITY ? 0.0f : m_run;
+            // (the running sum is rounded once for the 16 weights)
+            float p[16], sum = 0.0f;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                p[v] = __builtin_amdgcn_exp2f(s[v] - m_use);
+                sum += p[v];
+            }
+            l_run += sum;
+            if (odd) {
+                // what was taken out, from memory: lane (col, half) holds
+                // elements 32 et + 8 (v / 4) + 4 half + v % 4 of row col
+#pragma unroll 1
+                for (int key = 0; key < 32; ++key) {
+                    float pk = 0.0f;
+                    const int mine = 4 * (key >> 3) + (key & 3);
+#pragma unroll
+                    for (int v = 0; v < 16; ++v)
+                        pk = v == mine ? p[v] : pk;
+                    pk = __shfl(pk, col + 32 * ((key >> 2) & 1), 64);
+                    const uint16_t *vr = V + (int64_t)(k.first + min(32 * h + key, k.len - 1)) * a.row_stride;
+#pragma unroll
+                    for (int et = 0; et < ET; ++et)
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) {
+                            const int e = 32 * et + 8 * (v >> 2) + 4 * half + (v & 3);
+                            const float x = e < D ? __uint_as_float((uint32_t)vr[e] << 16) : 0.0f;
+                            if (pk != 0.0f && !finite(x))
+                                o[et][v] = fmaf(pk, x, o[et][v]);
+                        }
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                u32x4_t pf[T];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    uint32_t t[T];
+                    terms2(p[8 * j + 2 * u], p[8 * j + 2 * u + 1], t);
+#pragma unroll
+                    for (int i = 0; i < T; ++i)
+                        pf[i][u] = t[i];
+                }
+                // A operand V^T: column 32 et + col of keys 16 j + 8 I + 4 half +
+                // 0..3, the row's chunks of et and I one exclusive or away
+#pragma unroll
+                for (int et = 0; et < ET; ++et) {
+                    u32x4_t vf;
+#pragma unroll
+                    for (int I = 0; I < 2; ++I) {
+                        const char *src = lds + (xv ^ (64 * et) ^ (I ? (D == 16 ? 16 : 32) : 0)) + 2 * (16 * j + 8 * I) * D;
+                        const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)src);
+                        const u32x2_t y = __builtin_bit_cast(u32x2_t, x);
+                        vf[2 * I] = y[0];
+                        vf[2 * I + 1] = y[1];
+                    }
+#pragma unroll
+                    for (int i = 0; i < T; ++i)
+                        o[et] = mfma32(vf, pf[i], o[et]);
+                }
+            }
+        }
+    }
+    {
+        const auto lr = __builtin_amdgcn_permlane32_swap(__float_as_uint(l_run), __float_as_uint(l_run), false, false);
+        l_run = __uint_as_float(lr[0]) + __uint_as_float(lr[1]);
+    }
+    if constexpr (NK == 2) {
+        // the second half of the keys joins the first: its states through LDS,
+        // 16 ET + 2 words a lane
+        static_assert(sizeof(kv) >= NQ * 64 * (16 * ET + 2) * 4 || D < 128, "LDS for the states");
+        __shared__ float st[D == 128 ? 1 : NQ * 64 * (16 * ET + 2)];
+        float *to = D == 128 ? reinterpret_cast<float *>(kv) : st;
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (wk == 1) {
+#pragma unroll
+            for (int et = 0; et < ET; ++et)
+#pragma unroll
+                for (int v = 0; v < 16; ++v)
+                    to[((16 * et + v) * NQ + wq) * 64 + lane] = o[et][v];
+            to[(16 * ET * NQ + wq) * 64 + lane] = m_run;
+            to[((16 * ET + 1) * NQ + wq) * 64 + lane] = l_run;
+        }
+        __syncthreads();
+        if (wk == 1)
+            return;
+        const float m2 = to[(16 * ET * NQ + wq) * 64 + lane], l2 = to[((16 * ET + 1) * NQ + wq) * 64 + lane];
+        const float m = fmaxf(m_run, m2), mu = m == -INFINITY ? 0.0f : m;
+        const float w1 = __builtin_amdgcn_exp2f(m_run - mu), w2 = __builtin_amdgcn_exp2f(m2 - mu);
+        m_run = m;
+        l_run = l_run * w1 + l2 * w2;
+#pragma unroll
+        for (int et = 0; et < ET; ++et)
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+                o[et][v] = o[et][v] * w1 + to[((16 * et + v) * NQ + wq) * 64 + lane] * w2;
+    }
+    if (r0 + col >= a.rows)
+        return;
+    const int64_t slot = ((int64_t)split * a.n + node) * a.n_heads + head;
+    float *to = a.splits == 1 ? a.out + (int64_t)node * a.ld_out + (int64_t)head * D : a.part_o + slot * D;
+    const float inv = a.splits > 1 ? 1.0f : l_run == 0.0f ? 0.0f : 1.0f / l_run;
+#pragma unroll
+    for (int et = 0; et < ET; ++et)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int e = 32 * et + 8 * q + 4 * half;
+            if (e < D)
+                *reinterpret_cast<f32x4_t *>(to + e) =
+                    f32x4_t{o[et][4 * q], o[et][4 * q + 1], o[et][4 * q + 2], o[et][4 * q + 3]} * inv;
+        }
+    if (a.splits > 1 && half == 0)
+        a.part_ml[slot] = make_float2(m_run, l_run);
+}
+
 // The shares of a (node, head) joined in order: D / 4 lanes, four elements each.
 __global__ __launch_bounds__(256) void k_tree_join(TreeAttnArgs a, int D, int lanes) {
     const int64_t slots = (int64_t)a.n * a.n_heads;
@@ -266,10 +572,13 @@ __global__ __launch_bounds__(256) void k_tree_join(TreeAttnArgs a, int D, int la
         L == 0.0f ? f32x4_t{0.0f, 0.0f, 0.0f, 0.0f} : O / L;
 }
 
-// Shares of the keys: about four work-groups per CU, at least two blocks each.
-constexpr int TA_GROUPS = 1024;
+// Rows of a tile and shares of the keys.  bfloat16: tiles of 32, 64, 96 or 128
+// rows, the fewest that hold a kv head's rows, and shares that give every CU
+// two work-groups.  float32: tiles of 16 rows, four work-groups per CU.
+constexpr int TA_GROUPS = 1024, TA_GROUPS_MFMA = 512;
 
 void plan(const sd_kv_layer *kv, int32_t n_heads, int32_t n, int32_t prefix, TreeAttnArgs *a) {
+    const bool bf16 = kv->dtype == SD_BF16;
     a->n = n;
     a->words = (n + 63) / 64;
     a->prefix = prefix;
@@ -277,11 +586,13 @@ void plan(const sd_kv_layer *kv, int32_t n_heads, int32_t n, int32_t prefix, Tre
     a->n_kv_heads = kv->n_kv_heads;
     a->G = n_heads / kv->n_kv_heads;
     a->rows = n * a->G;
-    a->q_tiles = (a->rows + 15) / 16;
+    a->q_rows = bf16 ? std::min(128, (a->rows + 31) / 32 * 32) : 16;
+    a->q_tiles = (a->rows + a->q_rows - 1) / a->q_rows;
     a->prefix_blocks = (prefix + KB - 1) / KB;
     a->blocks = a->prefix_blocks + a->words;
-    const int units = a->q_tiles * a->n_kv_heads;
-    const int want = std::max(1, std::min((a->blocks + 1) / 2, (TA_GROUPS + units - 1) / units));
+    const int units = a->q_tiles * a->n_kv_heads, groups = bf16 ? TA_GROUPS_MFMA : TA_GROUPS;
+    const int most = bf16 ? a->blocks : (a->blocks + 1) / 2;
+    const int want = std::max(1, std::min(most, (groups + units - 1) / units));
     a->per_split = (a->blocks + want - 1) / want;
     a->splits = (a->blocks + a->per_split - 1) / a->per_split;
 }
@@ -305,17 +616,29 @@ sd_status check_sizes(const sd_kv_layer *kv, int32_t n_heads, int32_t n, int32_t
     return SD_OK;
 }
 
-template <typename TK>
 void launch_f32(const TreeAttnArgs &a, int D, hipStream_t s) {
     const dim3 grid((unsigned)(a.q_tiles * a.n_kv_heads), (unsigned)a.splits), block(TA_WAVES * 64);
     if (D == 16)
-        hipLaunchKernelGGL((k_tree_attn_f32<TK, 16>), grid, block, 0, s, a);
+        hipLaunchKernelGGL(k_tree_attn_f32<16>, grid, block, 0, s, a);
     else if (D == 32)
-        hipLaunchKernelGGL((k_tree_attn_f32<TK, 32>), grid, block, 0, s, a);
+        hipLaunchKernelGGL(k_tree_attn_f32<32>, grid, block, 0, s, a);
     else if (D == 64)
-        hipLaunchKernelGGL((k_tree_attn_f32<TK, 64>), grid, block, 0, s, a);
+        hipLaunchKernelGGL(k_tree_attn_f32<64>, grid, block, 0, s, a);
     else
-        hipLaunchKernelGGL((k_tree_attn_f32<TK, 128>), grid, block, 0, s, a);
+        hipLaunchKernelGGL(k_tree_attn_f32<128>, grid, block, 0, s, a);
+}
+
+template <int D>
+void launch_mfma(const TreeAttnArgs &a, hipStream_t s) {
+    const dim3 grid((unsigned)(a.q_tiles * a.n_kv_heads * a.splits));
+    if (a.q_rows == 32)
+        hipLaunchKernelGGL((k_tree_attn_mfma<D, 1, 2>), grid, dim3(128), 0, s, a);
+    else if (a.q_rows == 64)
+        hipLaunchKernelGGL((k_tree_attn_mfma<D, 2, 2>), grid, dim3(256), 0, s, a);
+    else if (a.q_rows == 96)
+        hipLaunchKernelGGL((k_tree_attn_mfma<D, 3, 1>), grid, dim3(192), 0, s, a);
+    else
+        hipLaunchKernelGGL((k_tree_attn_mfma<D, 4, 1>), grid, dim3(256), 0, s, a);
 }
 
 sd_status tree_attention(const sd_kv_layer *kv, const float *q, int64_t ld_q, int32_t n_heads, int32_t n,
@@ -347,13 +670,21 @@ sd_status tree_attention(const sd_kv_layer *kv, const float *q, int64_t ld_q, in
     a.mask = mask;
     a.out = out;
     a.ld_out = ld_out;
-    a.part_o = static_cast<float *>(workspace);
-    a.part_ml = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + o_bytes(a, D));
+    if (need) {
+        a.part_o = static_cast<float *>(workspace);
+        a.part_ml = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + o_bytes(a, D));
+    }
     a.scale = (scale == 0.0f ? 1.0f / std::sqrt((float)D) : scale) * 1.4426950408889634f;
-    if (kv->dtype == SD_BF16)
-        launch_f32<uint16_t>(a, D, s);
+    if (kv->dtype != SD_BF16)
+        launch_f32(a, D, s);
+    else if (D == 16)
+        launch_mfma<16>(a, s);
+    else if (D == 32)
+        launch_mfma<32>(a, s);
+    else if (D == 64)
+        launch_mfma<64>(a, s);
     else
-        launch_f32<float>(a, D, s);
+        launch_mfma<128>(a, s);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && a.splits > 1) {
         const int lanes = D / 4, per = 256 / lanes;
