@@ -5,9 +5,9 @@
 // The query heads of a kv head and the nodes share its keys: the n G rows of a kv
 // head (G query heads each, row = node G + head) are one matrix of queries.
 //
-// Keys come in blocks of 64 (one word of the mask): first the prefix, its last
-// block cut off, then the nodes in blocks of their own, so that a block's visible
-// keys are one 64-bit word a row.  The blocks are split over work-groups,
+// Keys come in blocks of 32 or 64: first the prefix, its last block cut off, then
+// the nodes in blocks of their own, so that a block's visible keys are one word,
+// or half a word, of the mask a row.  The blocks are split over work-groups,
 // each leaving an unnormalised output with its maximum and sum, which a second
 // kernel joins in order; a single share is normalised at once.
 #include "tree.h"
@@ -32,7 +32,8 @@ typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
 
-constexpr int KB = 64;  // keys of a block
+constexpr int KB = 64;       // keys of a block
+constexpr int KB_FEW = 32;   // of the kernel for few rows
 
 struct TreeAttnArgs {
     const float *q;
@@ -50,20 +51,21 @@ struct TreeAttnArgs {
     int32_t prefix_blocks, blocks, splits, per_split;                 // per_split: blocks of a share
 };
 
-// Block b: its first key, how many keys it has, and whether they are nodes.
+// Block b of B keys: its first key, how many keys it has, and whether they are nodes.
 struct Block {
     int first, len, node0;  // node0: the first node, or -1
 };
+template <int B>
 __device__ __forceinline__ Block block_of(const TreeAttnArgs &a, int b) {
     Block k;
     if (b < a.prefix_blocks) {
-        k.first = KB * b;
-        k.len = min(KB, a.prefix - k.first);
+        k.first = B * b;
+        k.len = min(B, a.prefix - k.first);
         k.node0 = -1;
     } else {
-        k.node0 = KB * (b - a.prefix_blocks);
+        k.node0 = B * (b - a.prefix_blocks);
         k.first = a.prefix + k.node0;
-        k.len = min(KB, a.n - k.node0);
+        k.len = min(B, a.n - k.node0);
     }
     return k;
 }
@@ -73,7 +75,7 @@ __device__ __forceinline__ uint64_t visible(const TreeAttnArgs &a, const Block &
     if (k.node0 < 0)
         return all;
     if (a.mask)
-        return a.mask[(int64_t)node * a.words + (k.node0 >> 6)] & all;
+        return (a.mask[(int64_t)node * a.words + (k.node0 >> 6)] >> (k.node0 & 63)) & all;
     const int last = node - k.node0;
     return last < 0 ? 0 : (last >= 63 ? ~0ull : (2ull << last) - 1) & all;
 }
@@ -81,6 +83,46 @@ __device__ __forceinline__ uint64_t visible(const TreeAttnArgs &a, const Block &
 __device__ __forceinline__ f32x4_t load4(const float *p) { return *reinterpret_cast<const f32x4_t *>(p); }
 
 __device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
+
+// Two packed bfloat16 values, zero for those that are infinite or NaN.
+__device__ __forceinline__ uint32_t without_odd(uint32_t x) {
+    const bool lo = (x & 0x7f80u) == 0x7f80u, hi = (x & 0x7f800000u) == 0x7f800000u;
+    return x & (lo ? 0xffff0000u : ~0u) & (hi ? 0x0000ffffu : ~0u);
+}
+
+// The NW waves' states of ROWS rows from row0 on (o [wave][e OP + row], waves
+// `pitch` floats apart; (maximum, sum) [wave][row]) merged in wave order: the
+// result of a single share, or its part of several.
+template <int D, int NW, int OP, int ROWS>
+__device__ __forceinline__ void merge_waves(const TreeAttnArgs &a, const float *o, int pitch, const float2 *ml, int row0,
+                                            int g, int split) {
+    for (int i = threadIdx.x; i < ROWS * D; i += NW * 64) {
+        const int rc = i / D, e = i - rc * D, rr = row0 + rc;
+        if (rr >= a.rows)
+            break;  // i only grows
+        float m = -INFINITY, L = 0.0f, O = 0.0f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w)
+            m = fmaxf(m, ml[w * ROWS + rc].x);
+        const float mu = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            // (a wave without keys has weight zero, output zero)
+            const float wt = __builtin_amdgcn_exp2f(ml[w * ROWS + rc].x - mu);
+            L = fmaf(wt, ml[w * ROWS + rc].y, L);
+            O = fmaf(wt, o[w * pitch + e * OP + rc], O);
+        }
+        const int nd = rr / a.G, hd = g * a.G + rr - nd * a.G;
+        if (a.splits == 1) {
+            a.out[(int64_t)nd * a.ld_out + (int64_t)hd * D + e] = L == 0.0f ? 0.0f : O / L;
+        } else {
+            const int64_t slot = ((int64_t)split * a.n + nd) * a.n_heads + hd;
+            a.part_o[slot * D + e] = O;
+            if (e == 0)
+                a.part_ml[slot] = make_float2(m, L);
+        }
+    }
+}
 
 // ---------------------------------------------------------------------------
 // In float32: a work-group of four waves takes 16 rows of a kv head, each wave
@@ -117,7 +159,7 @@ __global__ __launch_bounds__(TA_WAVES * 64) void k_tree_attn_f32(TreeAttnArgs a)
         o[t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 
     for (int b = b0; b < b1; ++b) {
-        const Block k = block_of(a, b);
+        const Block k = block_of<KB>(a, b);
         if (16 * wave >= k.len)
             continue;  // uniform over the wave
         // keys past the block read its last one; their scores are masked
@@ -202,32 +244,7 @@ __global__ __launch_bounds__(TA_WAVES * 64) void k_tree_attn_f32(TreeAttnArgs a)
     if (g4 == 0)
         ml[wave][c] = make_float2(m_run, l_run);
     __syncthreads();
-    for (int i = threadIdx.x; i < 16 * D; i += TA_WAVES * 64) {
-        const int rc = i / D, e = i - rc * D, rr = qt * 16 + rc;
-        if (rr >= a.rows)
-            break;  // i only grows
-        float m = -INFINITY, L = 0.0f, O = 0.0f;
-#pragma unroll
-        for (int w = 0; w < TA_WAVES; ++w)
-            m = fmaxf(m, ml[w][rc].x);
-        const float mu = m == -INFINITY ? 0.0f : m;
-#pragma unroll
-        for (int w = 0; w < TA_WAVES; ++w) {
-            // (a wave without keys has weight zero, output zero)
-            const float wt = __builtin_amdgcn_exp2f(ml[w][rc].x - mu);
-            L = fmaf(wt, ml[w][rc].y, L);
-            O = fmaf(wt, tile[w][e * OP + rc], O);
-        }
-        const int nd = rr / a.G, hd = g * a.G + rr - nd * a.G;
-        if (a.splits == 1) {
-            a.out[(int64_t)nd * a.ld_out + (int64_t)hd * D + e] = L == 0.0f ? 0.0f : O / L;
-        } else {
-            const int64_t slot = ((int64_t)split * a.n + nd) * a.n_heads + hd;
-            a.part_o[slot * D + e] = O;
-            if (e == 0)
-                a.part_ml[slot] = make_float2(m, L);
-        }
-    }
+    merge_waves<D, TA_WAVES, OP, 16>(a, &tile[0][0], D * OP, &ml[0][0], qt * 16, g, split);
 }
 
 // ---------------------------------------------------------------------------
@@ -288,7 +305,7 @@ struct Lines {  // where a block's rows lie in LDS
 };
 
 template <int D, int NQ, int NK>
-__global__ __launch_bounds__(64 * NQ * NK, NQ * NK == 2 ? 1 : 2) void k_tree_attn_mfma(TreeAttnArgs a) {
+__global__ __launch_bounds__(64 * NQ * NK, 2) void k_tree_attn_mfma(TreeAttnArgs a) {
     constexpr int T = X_TERMS, NW = NQ * NK, ES = D / 16, ET = D < 32 ? 1 : D / 32;
     constexpr int LOADS = 2 * (D / 8);  // 1 KB loads of a block's K and V
     using L = Lines<D>;
@@ -305,7 +322,7 @@ __global__ __launch_bounds__(64 * NQ * NK, NQ * NK == 2 ? 1 : 2) void k_tree_att
     const uint16_t *V = static_cast<const uint16_t *>(a.v) + (int64_t)g * a.head_stride;
 
     auto load_block = [&](int b, int buf) {
-        const Block k = block_of(a, b);
+        const Block k = block_of<KB>(a, b);
         // (fewer registers than with every address of the block at once)
 #pragma unroll 2
         for (int t = wave; t < LOADS; t += NW) {
@@ -355,7 +372,7 @@ __global__ __launch_bounds__(64 * NQ * NK, NQ * NK == 2 ? 1 : 2) void k_tree_att
 
     int buf = 0;
     for (int b = b0; b < b1; ++b, buf ^= 1) {
-        const Block k = block_of(a, b);
+        const Block k = block_of<KB>(a, b);
         // this wave's loads of the block have landed, then everyone's; every
         // read of the other buffer has returned
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -372,14 +389,9 @@ __global__ __launch_bounds__(64 * NQ * NK, NQ * NK == 2 ? 1 : 2) void k_tree_att
                 bool hit = false;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    if ((x[j] & 0x7f80u) == 0x7f80u) {
-                        x[j] &= 0xffff0000u;
-                        hit = true;
-                    }
-                    if ((x[j] & 0x7f800000u) == 0x7f800000u) {
-                        x[j] &= 0xffffu;
-                        hit = true;
-                    }
+                    const uint32_t y = without_odd(x[j]);
+                    hit |= y != x[j];
+                    x[j] = y;
                 }
                 if (hit)
                     reinterpret_cast<u32x4_t *>(vs)[c] = x;
@@ -548,34 +560,306 @@ __global__ __launch_bounds__(64 * NQ * NK, NQ * NK == 2 ? 1 : 2) void k_tree_att
         a.part_ml[slot] = make_float2(m_run, l_run);
 }
 
-// The shares of a (node, head) joined in order: D / 4 lanes, four elements each.
-__global__ __launch_bounds__(256) void k_tree_join(TreeAttnArgs a, int D, int lanes) {
-    const int64_t slots = (int64_t)a.n * a.n_heads;
-    const int64_t slot = (int64_t)blockIdx.x * (256 / lanes) + threadIdx.x / lanes;
-    if (slot >= slots)
-        return;
-    const int e = 4 * (threadIdx.x % lanes);
-    float m = -INFINITY;
-    for (int s = 0; s < a.splits; ++s)
-        m = fmaxf(m, a.part_ml[s * slots + slot].x);
-    const float mu = m == -INFINITY ? 0.0f : m;
-    float L = 0.0f;
-    f32x4_t O = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int s = 0; s < a.splits; ++s) {
-        const float2 v = a.part_ml[s * slots + slot];
-        const float w = __builtin_amdgcn_exp2f(v.x - mu);
-        L = fmaf(w, v.y, L);
-        O += w * *reinterpret_cast<const f32x4_t *>(a.part_o + (s * slots + slot) * D + e);
-    }
-    const int nd = (int)(slot / a.n_heads), hd = (int)(slot - (int64_t)nd * a.n_heads);
-    *reinterpret_cast<f32x4_t *>(a.out + (int64_t)nd * a.ld_out + (int64_t)hd * D + e) =
-        L == 0.0f ? f32x4_t{0.0f, 0.0f, 0.0f, 0.0f} : O / L;
+// ---------------------------------------------------------------------------
+// The same for up to 32 rows of a kv head, where the read of the cache counts and
+// not the products: four waves, each with 32-key blocks of its own and no barrier
+// until the end.  K goes straight into registers as the A operand of 16x16x32
+// score products, V straight into the wave's LDS, both one block ahead.  Lane
+// (col, grp) receives the keys 16 t + 4 grp + v of row col, which are the slots
+// u = 4 t + v that the value products take from it.  LDS lines are permuted for
+// the reads here: eight rows, two adjacent chunks each.
+__device__ __forceinline__ f32x4_t mfma16(u32x4_t a, u32x4_t b, f32x4_t c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c,
+                                                   0, 0, 0);
 }
 
-// Rows of a tile and shares of the keys.  bfloat16: tiles of 32, 64, 96 or 128
-// rows, the fewest that hold a kv head's rows, and shares that give every CU
-// two work-groups.  float32: tiles of 16 rows, four work-groups per CU.
-constexpr int TA_GROUPS = 1024, TA_GROUPS_MFMA = 512;
+// Rows r .. of a wave's V block in LDS.
+template <int D>
+struct FewLines {
+    static constexpr int C = D / 8, RPL = 16 / C;
+    __device__ static int swz(int s) {
+        return C == 16 ? ((s & 3) << 2) | ((s >> 1) & 2) : C == 8 ? (s & 3) << 1 : C == 4 ? (s & 1) << 1 : 0;
+    }
+    __device__ static int at(int r, int c) {
+        const int s = r / RPL;
+        return s * 128 + 8 * (((r % RPL) * C + c) ^ swz(s));
+    }
+};
+
+template <int D, int QT>
+__global__ __launch_bounds__(256, QT == 1 || D < 128 ? 2 : 1) void k_tree_attn_few(TreeAttnArgs a) {
+    constexpr int T = X_TERMS, NW = 4, ES = D < 32 ? 1 : D / 32, ET = D / 16, ROWS = 16 * QT, OP = ROWS + 1;
+    using L = FewLines<D>;
+    constexpr int VB = KB_FEW * D;  // elements of a V block
+    constexpr int WORDS = 2 * VB / 2 > D * OP ? 2 * VB / 2 : D * OP;
+    __shared__ __attribute__((aligned(1024))) uint32_t tile[NW][WORDS];  // two V blocks, or the outputs
+    __shared__ float2 ml[NW][ROWS];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
+    const int g = blockIdx.x % a.n_kv_heads, split = blockIdx.x / a.n_kv_heads;
+    const int b1 = min(a.blocks, (split + 1) * a.per_split);
+    const uint16_t *K = static_cast<const uint16_t *>(a.k) + (int64_t)g * a.head_stride;
+    const uint16_t *V = static_cast<const uint16_t *>(a.v) + (int64_t)g * a.head_stride;
+    uint16_t *vt = reinterpret_cast<uint16_t *>(tile[wave]);
+
+    u32x4_t kf[2][ES];
+    auto load_k = [&](const Block &k) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            // keys past the block: its last, masked; head_dim 16: the upper slots are zeros of q
+            const uint16_t *kp = K + (int64_t)(k.first + min(16 * t + col, k.len - 1)) * a.row_stride + (8 * grp) % D;
+#pragma unroll
+            for (int s = 0; s < ES; ++s)
+                kf[t][s] = *reinterpret_cast<const u32x4_t *>(kp + 32 * s);
+        }
+    };
+    auto load_v = [&](const Block &k, int buf) {
+#pragma unroll
+        for (int u = 0; u < VB / 512; ++u) {
+            const int s = 4 * u + (lane >> 4), p = (lane & 15) ^ L::swz(s);
+            const int r = min(s * L::RPL + p / L::C, k.len - 1);
+            load_to_lds16(V + (int64_t)(k.first + r) * a.row_stride + 8 * (p % L::C), vt + buf * VB + u * 512);
+        }
+    };
+    int b = split * a.per_split + wave;
+    if (b < b1) {
+        const Block k = block_of<KB_FEW>(a, b);
+        load_k(k);
+        load_v(k, 0);
+    }
+    int node[QT];
+    u32x4_t qf[QT][ES][T];
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+        const int row = min(16 * i + col, a.rows - 1);
+        node[i] = row / a.G;
+        const float *qs = a.q + (int64_t)node[i] * a.ld_q + (int64_t)(g * a.G + row - node[i] * a.G) * D + (8 * grp) % D;
+        const float scale = D < 32 && grp >= 2 ? 0.0f : a.scale;
+#pragma unroll
+        for (int s = 0; s < ES; ++s) {
+            f32x4_t x0 = load4(qs + 32 * s), x1 = load4(qs + 32 * s + 4);
+            if (D < 32 && grp >= 2)  // (0 times an infinity is none)
+                x0 = x1 = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+            x0 *= scale;
+            x1 *= scale;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                uint32_t t0[T], t1[T];
+                terms2(x0[2 * j], x0[2 * j + 1], t0);
+                terms2(x1[2 * j], x1[2 * j + 1], t1);
+#pragma unroll
+                for (int w = 0; w < T; ++w) {
+                    qf[i][s][w][j] = t0[w];
+                    qf[i][s][w][2 + j] = t1[w];
+                }
+            }
+        }
+    }
+    float m_run[QT], l_run[QT];
+    f32x4_t o[QT][ET];
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+        m_run[i] = -INFINITY;
+        l_run[i] = 0.0f;
+#pragma unroll
+        for (int et = 0; et < ET; ++et)
+            o[i][et] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    const int v_lane = 2 * L::at(4 * grp + (col >> 2), (col & 3) >> 1) + 8 * (col & 1);
+    const char *vb = reinterpret_cast<const char *>(vt);
+
+    int buf = 0;
+    for (; b < b1; b += NW, buf ^= 1) {
+        const Block k = block_of<KB_FEW>(a, b);
+        f32x4_t s[QT][2];
+#pragma unroll
+        for (int i = 0; i < QT; ++i)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                s[i][t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int e = 0; e < ES; ++e)
+#pragma unroll
+                    for (int w = 0; w < T; ++w)
+                        s[i][t] = mfma16(kf[t][e], qf[i][e][w], s[i][t]);
+            }
+        // this block's V has landed (it was asked for before this block's K, or
+        // just after), then the next block's loads
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (b + NW < b1) {
+            const Block next = block_of<KB_FEW>(a, b + NW);
+            load_v(next, buf ^ 1);
+            load_k(next);
+        }
+        // Infinities and NaN among the nodes' values: a row must not add 0 times
+        // one that it does not see.  They are taken out here, and put where they
+        // belong beside the products.
+        bool odd = false;
+        if (k.node0 >= 0) {
+            u32x4_t *vw = reinterpret_cast<u32x4_t *>(vt + buf * VB);
+            for (int c = lane; c < VB / 8; c += 64) {
+                u32x4_t x = vw[c];
+                bool hit = false;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t y = without_odd(x[j]);
+                    hit |= y != x[j];
+                    x[j] = y;
+                }
+                if (hit)
+                    vw[c] = x;
+                odd |= hit;
+            }
+            odd = __any(odd);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
+        // (a tile's rows at a time: V again from LDS for the second costs less than
+        // the registers of both)
+#pragma unroll
+        for (int i = 0; i < QT; ++i) {
+            const uint32_t bits = (uint32_t)visible(a, k, node[i]);
+            float p[8], mx = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                p[u] = s[i][u >> 2][u & 3];
+                if (k.node0 >= 0 || k.len < KB_FEW)
+                    p[u] = (bits >> (16 * (u >> 2) + 4 * grp + (u & 3))) & 1 ? p[u] : -INFINITY;
+                mx = fmaxf(mx, p[u]);
+            }
+            mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+            if (__any(mx > m_run[i])) {
+                const float m_new = fmaxf(m_run[i], mx);
+                const float sc = m_run[i] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run[i] - m_new);
+                l_run[i] *= sc;
+#pragma unroll
+                for (int et = 0; et < ET; ++et)
+                    o[i][et] *= sc;
+                m_run[i] = m_new;
+            }
+            const float m_use = m_run[i] == -INFINITY ? 0.0f : m_run[i];
+            float sum = 0.0f;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                p[u] = __builtin_amdgcn_exp2f(p[u] - m_use);
+                sum += p[u];
+            }
+            l_run[i] += sum;
+            if (odd) {
+                // lane (col, grp) holds elements 16 et + 4 grp + u of row col
+#pragma unroll 1
+                for (int key = 0; key < KB_FEW; ++key) {
+                    float pk = 0.0f;
+                    const int mine = 4 * (key >> 4) + (key & 3);
+#pragma unroll
+                    for (int u = 0; u < 8; ++u)
+                        pk = u == mine ? p[u] : pk;
+                    pk = __shfl(pk, col + 16 * ((key >> 2) & 3), 64);
+                    const uint16_t *vr = V + (int64_t)(k.first + min(key, k.len - 1)) * a.row_stride + 4 * grp;
+#pragma unroll
+                    for (int et = 0; et < ET; ++et) {
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) {
+                            const float x = __uint_as_float((uint32_t)vr[16 * et + u] << 16);
+                            if (pk != 0.0f && !finite(x))
+                                o[i][et][u] = fmaf(pk, x, o[i][et][u]);
+                        }
+                        __builtin_amdgcn_sched_barrier(0);  // a few loads at a time: registers
+                    }
+                }
+            }
+            u32x4_t pf[T];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                uint32_t t[T];
+                terms2(p[2 * j], p[2 * j + 1], t);
+#pragma unroll
+                for (int w = 0; w < T; ++w)
+                    pf[w][j] = t[w];
+            }
+            // A operand V^T: column 16 et + col of keys 16 I + 4 grp + 0..3
+            int xv = v_lane + 2 * buf * VB;
+            asm volatile("" : "+v"(xv));
+#pragma unroll
+            for (int et = 0; et < ET; ++et) {
+                u32x4_t vf;
+#pragma unroll
+                for (int I = 0; I < 2; ++I) {
+                    const char *src = vb + (xv ^ (32 * et)) + 2 * 16 * I * D;
+                    const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)src);
+                    const u32x2_t y = __builtin_bit_cast(u32x2_t, x);
+                    vf[2 * I] = y[0];
+                    vf[2 * I + 1] = y[1];
+                }
+#pragma unroll
+                for (int w = 0; w < T; ++w)
+                    o[i][et] = mfma16(vf, pf[w], o[i][et]);
+            }
+        }
+        // (every read of this block has returned before its buffer is filled again)
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+    // the waves' states, merged in wave order
+    float *to = reinterpret_cast<float *>(tile[wave]);
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+        l_run[i] += __shfl_xor(l_run[i], 16, 64);
+        l_run[i] += __shfl_xor(l_run[i], 32, 64);
+#pragma unroll
+        for (int et = 0; et < ET; ++et)
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                to[(16 * et + 4 * grp + u) * OP + 16 * i + col] = o[i][et][u];
+        if (grp == 0)
+            ml[wave][16 * i + col] = make_float2(m_run[i], l_run[i]);
+    }
+    __syncthreads();
+    merge_waves<D, NW, OP, ROWS>(a, reinterpret_cast<const float *>(tile), WORDS, &ml[0][0], 0, g, split);
+}
+
+// The shares of a (node, head) joined: a work-group each.  Every wave takes the
+// shares' maxima and sums by itself; D / 4 lanes hold a row, the groups of lanes
+// take the shares in turn and add up in order.  (One thread per element walking
+// over the shares: 6.7 us for 520 rows of 10 shares, 33 us for 576 of 63.)
+constexpr int JOIN_THREADS = 256;
+template <int D>
+__global__ __launch_bounds__(JOIN_THREADS) void k_tree_join(TreeAttnArgs a) {
+    constexpr int LANES = D / 4, NG = JOIN_THREADS / LANES;
+    __shared__ f32x4_t red[NG][LANES];
+    const int64_t slots = (int64_t)a.n * a.n_heads, slot = blockIdx.x;
+    const int lane = threadIdx.x & 63, e = threadIdx.x % LANES, gi = threadIdx.x / LANES;
+    float m = -INFINITY;
+    for (int s = lane; s < a.splits; s += 64)
+        m = fmaxf(m, a.part_ml[s * slots + slot].x);
+    m = wave_max_all(m);
+    const float mu = m == -INFINITY ? 0.0f : m;
+    float sum = 0.0f;
+    for (int s = lane; s < a.splits; s += 64) {
+        const float2 v = a.part_ml[s * slots + slot];
+        sum = fmaf(__builtin_amdgcn_exp2f(v.x - mu), v.y, sum);
+    }
+    const float total = wave_sum_all(sum);
+    f32x4_t O = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (int s = gi; s < a.splits; s += NG)
+        O += __builtin_amdgcn_exp2f(a.part_ml[s * slots + slot].x - mu) *
+             load4(a.part_o + (s * slots + slot) * D + 4 * e);
+    red[gi][e] = O;
+    __syncthreads();
+    if (gi > 0)
+        return;
+#pragma unroll
+    for (int i = 1; i < NG; ++i)
+        O += red[i][e];
+    const int nd = (int)(slot / a.n_heads), hd = (int)(slot - (int64_t)nd * a.n_heads);
+    *reinterpret_cast<f32x4_t *>(a.out + (int64_t)nd * a.ld_out + (int64_t)hd * D + 4 * e) =
+        total == 0.0f ? f32x4_t{0.0f, 0.0f, 0.0f, 0.0f} : O / total;
+}
+
+// Rows of a tile and shares of the keys.  bfloat16: up to 32 rows on the kernel
+// for few, every wave of two work-groups per CU with keys of its own; else tiles of 64,
+// 96 or 128 rows, the fewest that hold a kv head's rows, in two work-groups per
+// CU.  float32: tiles of 16 rows, four work-groups per CU.
+constexpr int TA_GROUPS = 1024, TA_GROUPS_MFMA = 512, FEW_ROWS = 32;
 
 void plan(const sd_kv_layer *kv, int32_t n_heads, int32_t n, int32_t prefix, TreeAttnArgs *a) {
     const bool bf16 = kv->dtype == SD_BF16;
@@ -586,14 +870,15 @@ void plan(const sd_kv_layer *kv, int32_t n_heads, int32_t n, int32_t prefix, Tre
     a->n_kv_heads = kv->n_kv_heads;
     a->G = n_heads / kv->n_kv_heads;
     a->rows = n * a->G;
-    a->q_rows = bf16 ? std::min(128, (a->rows + 31) / 32 * 32) : 16;
+    const bool few = bf16 && a->rows <= FEW_ROWS;
+    a->q_rows = few ? (a->rows <= 16 ? 16 : 32) : bf16 ? std::min(128, std::max(64, (a->rows + 31) / 32 * 32)) : 16;
     a->q_tiles = (a->rows + a->q_rows - 1) / a->q_rows;
-    a->prefix_blocks = (prefix + KB - 1) / KB;
-    a->blocks = a->prefix_blocks + a->words;
+    const int kb = few ? KB_FEW : KB, step = few ? 4 : bf16 ? 1 : 2;  // step: blocks that a share has at least
+    a->prefix_blocks = (prefix + kb - 1) / kb;
+    a->blocks = a->prefix_blocks + (n + kb - 1) / kb;
     const int units = a->q_tiles * a->n_kv_heads, groups = bf16 ? TA_GROUPS_MFMA : TA_GROUPS;
-    const int most = bf16 ? a->blocks : (a->blocks + 1) / 2;
-    const int want = std::max(1, std::min(most, (groups + units - 1) / units));
-    a->per_split = (a->blocks + want - 1) / want;
+    const int want = std::max(1, std::min((a->blocks + step - 1) / step, (groups + units - 1) / units));
+    a->per_split = ((a->blocks + want - 1) / want + step - 1) / step * step;
     a->splits = (a->blocks + a->per_split - 1) / a->per_split;
 }
 
@@ -631,8 +916,10 @@ void launch_f32(const TreeAttnArgs &a, int D, hipStream_t s) {
 template <int D>
 void launch_mfma(const TreeAttnArgs &a, hipStream_t s) {
     const dim3 grid((unsigned)(a.q_tiles * a.n_kv_heads * a.splits));
-    if (a.q_rows == 32)
-        hipLaunchKernelGGL((k_tree_attn_mfma<D, 1, 2>), grid, dim3(128), 0, s, a);
+    if (a.q_rows == 16)
+        hipLaunchKernelGGL((k_tree_attn_few<D, 1>), grid, dim3(256), 0, s, a);
+    else if (a.q_rows == 32)
+        hipLaunchKernelGGL((k_tree_attn_few<D, 2>), grid, dim3(256), 0, s, a);
     else if (a.q_rows == 64)
         hipLaunchKernelGGL((k_tree_attn_mfma<D, 2, 2>), grid, dim3(256), 0, s, a);
     else if (a.q_rows == 96)
@@ -687,8 +974,8 @@ sd_status tree_attention(const sd_kv_layer *kv, const float *q, int64_t ld_q, in
         launch_mfma<128>(a, s);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && a.splits > 1) {
-        const int lanes = D / 4, per = 256 / lanes;
-        hipLaunchKernelGGL(k_tree_join, dim3((unsigned)((n * n_heads + per - 1) / per)), dim3(256), 0, s, a, D, lanes);
+        auto join = D == 16 ? k_tree_join<16> : D == 32 ? k_tree_join<32> : D == 64 ? k_tree_join<64> : k_tree_join<128>;
+        hipLaunchKernelGGL(join, dim3((unsigned)(n * n_heads)), dim3(JOIN_THREADS), 0, s, a);
         e = hipGetLastError();
     }
     return e == hipSuccess ? SD_OK : report(SD_ERR_DEVICE, std::string("tree attention: ") + hipGetErrorString(e));
