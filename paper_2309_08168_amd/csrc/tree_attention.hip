@@ -90,17 +90,19 @@ __device__ __forceinline__ uint32_t without_odd(uint32_t x) {
     return x & (lo ? 0xffff0000u : ~0u) & (hi ? 0x0000ffffu : ~0u);
 }
 
-// The NW waves' states of ROWS rows from row0 on (o [wave][e OP + row], waves
+// The NW waves' states of ROWS rows from row0 on (o [wave][row][D + 4], waves
 // `pitch` floats apart; (maximum, sum) [wave][row]) merged in wave order: the
 // result of a single share, or its part of several.
-template <int D, int NW, int OP, int ROWS>
+template <int D, int NW, int ROWS>
 __device__ __forceinline__ void merge_waves(const TreeAttnArgs &a, const float *o, int pitch, const float2 *ml, int row0,
                                             int g, int split) {
-    for (int i = threadIdx.x; i < ROWS * D; i += NW * 64) {
-        const int rc = i / D, e = i - rc * D, rr = row0 + rc;
+#pragma unroll
+    for (int i = threadIdx.x; i < ROWS * D / 4; i += NW * 64) {
+        const int rc = i / (D / 4), e = 4 * (i % (D / 4)), rr = row0 + rc;
         if (rr >= a.rows)
             break;  // i only grows
-        float m = -INFINITY, L = 0.0f, O = 0.0f;
+        float m = -INFINITY, L = 0.0f;
+        f32x4_t O = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int w = 0; w < NW; ++w)
             m = fmaxf(m, ml[w * ROWS + rc].x);
@@ -110,14 +112,15 @@ __device__ __forceinline__ void merge_waves(const TreeAttnArgs &a, const float *
             // (a wave without keys has weight zero, output zero)
             const float wt = __builtin_amdgcn_exp2f(ml[w * ROWS + rc].x - mu);
             L = fmaf(wt, ml[w * ROWS + rc].y, L);
-            O = fmaf(wt, o[w * pitch + e * OP + rc], O);
+            O += wt * load4(o + w * pitch + rc * (D + 4) + e);
         }
         const int nd = rr / a.G, hd = g * a.G + rr - nd * a.G;
         if (a.splits == 1) {
-            a.out[(int64_t)nd * a.ld_out + (int64_t)hd * D + e] = L == 0.0f ? 0.0f : O / L;
+            *reinterpret_cast<f32x4_t *>(a.out + (int64_t)nd * a.ld_out + (int64_t)hd * D + e) =
+                L == 0.0f ? f32x4_t{0.0f, 0.0f, 0.0f, 0.0f} : O / L;
         } else {
             const int64_t slot = ((int64_t)split * a.n + nd) * a.n_heads + hd;
-            a.part_o[slot * D + e] = O;
+            *reinterpret_cast<f32x4_t *>(a.part_o + slot * D + e) = O;
             if (e == 0)
                 a.part_ml[slot] = make_float2(m, L);
         }
@@ -138,8 +141,8 @@ constexpr int TA_WAVES = 4;
 
 template <int D>
 __global__ __launch_bounds__(TA_WAVES * 64) void k_tree_attn_f32(TreeAttnArgs a) {
-    constexpr int ES = D / 16, OP = 17;
-    __shared__ float tile[TA_WAVES][D * OP];
+    constexpr int ES = D / 16, OP = D + 4;
+    __shared__ __attribute__((aligned(16))) float tile[TA_WAVES][16 * OP];
     __shared__ float2 ml[TA_WAVES][16];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane & 15, g4 = lane >> 4;
     const int qt = blockIdx.x % a.q_tiles, g = blockIdx.x / a.q_tiles, split = blockIdx.y;
@@ -238,13 +241,11 @@ __global__ __launch_bounds__(TA_WAVES * 64) void k_tree_attn_f32(TreeAttnArgs a)
     float *to = tile[wave];
 #pragma unroll
     for (int t = 0; t < ES; ++t)
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-            to[(16 * t + 4 * g4 + u) * OP + c] = o[t][u];
+        *reinterpret_cast<f32x4_t *>(to + c * OP + 16 * t + 4 * g4) = o[t];
     if (g4 == 0)
         ml[wave][c] = make_float2(m_run, l_run);
     __syncthreads();
-    merge_waves<D, TA_WAVES, OP, 16>(a, &tile[0][0], D * OP, &ml[0][0], qt * 16, g, split);
+    merge_waves<D, TA_WAVES, 16>(a, &tile[0][0], 16 * OP, &ml[0][0], qt * 16, g, split);
 }
 
 // ---------------------------------------------------------------------------
@@ -264,6 +265,10 @@ __global__ __launch_bounds__(TA_WAVES * 64) void k_tree_attn_f32(TreeAttnArgs a)
 // LDS lines are 256 bytes, 16 chunks of 16 bytes: 128 / D rows.  Chunk p of line s
 // lies at p ^ swz(s), which spreads the 16 rows of a K read and the four rows of a
 // V read over all banks; the loads permute the chunks of a line on the way in.
+
+// A maximum that grows by no more than this (in log2) does not rescale the sums:
+// weights then reach 2^8 and not 1, which float32 sums do not mind.
+constexpr float SLACK = 8.0f;
 
 __device__ __forceinline__ f32x16_t mfma32(u32x4_t a, u32x4_t b, f32x16_t c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c,
@@ -399,11 +404,12 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_tree_attn_mfma(TreeAttnArgs
             }
             odd = __syncthreads_or(odd);
         }
-        const uint64_t see = visible(a, k, node);
+        const bool full = k.node0 < 0 && k.len == KB;  // every row sees every key
+        const uint64_t see = full ? ~0ull : visible(a, k, node);
 #pragma unroll 1
         for (int h = wk; h < 2; h += NK) {
             const uint32_t bits = h ? (uint32_t)(see >> 32) : (uint32_t)see;
-            if (!live || !__any(bits != 0))
+            if (!live || (!full && !__any(bits != 0)))
                 continue;  // uniform over the wave: no row of it sees these keys
             f32x16_t s;
 #pragma unroll
@@ -414,6 +420,9 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_tree_attn_mfma(TreeAttnArgs
             // loop in a register and spill.)
             int xk = 2 * (buf * 2 * KB * D + 32 * h * D + L::at(col, half)), xv = 2 * (buf * 2 * KB * D + 32 * h * D) + v_lane;
             asm volatile("" : "+v"(xk), "+v"(xv));
+            // (the wave in its products before the one in its softmax: 4% less time
+            // where the products bound it)
+            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int e = 0; e < ES; ++e) {
                 const u32x4_t kf = *reinterpret_cast<const u32x4_t *>(lds + (xk ^ (32 * e)));
@@ -421,8 +430,10 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_tree_attn_mfma(TreeAttnArgs
                 for (int i = 0; i < T; ++i)
                     s = mfma32(kf, qf[e][i], s);
             }
-            if (__any(bits != 0xffffffffu)) {
-                const uint32_t mine = bits >> (4 * half);
+            __builtin_amdgcn_s_setprio(0);
+            if (!full) {
+                uint32_t mine = bits >> (4 * half);
+                asm volatile("" : "+v"(mine));  // (a branch, and not selects in every block)
 #pragma unroll
                 for (int v = 0; v < 16; ++v)
                     s[v] = (mine >> (8 * (v >> 2) + (v & 3))) & 1 ? s[v] : -INFINITY;
@@ -435,7 +446,7 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_tree_attn_mfma(TreeAttnArgs
                 const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
                 mx = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
             }
-            if (__any(mx > m_run)) {
+            if (__any(mx > m_run + SLACK)) {
                 // (a row that has seen no key yet keeps zeros)
                 const float m_new = fmaxf(m_run, mx);
                 const float sc = m_run == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run - m_new);
@@ -477,6 +488,7 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_tree_attn_mfma(TreeAttnArgs
                         }
                 }
             }
+            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 u32x4_t pf[T];
@@ -506,6 +518,7 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_tree_attn_mfma(TreeAttnArgs
                         o[et] = mfma32(vf, pf[i], o[et]);
                 }
             }
+            __builtin_amdgcn_s_setprio(0);
         }
     }
     {
@@ -588,14 +601,15 @@ struct FewLines {
 
 template <int D, int QT>
 __global__ __launch_bounds__(256, QT == 1 || D < 128 ? 2 : 1) void k_tree_attn_few(TreeAttnArgs a) {
-    constexpr int T = X_TERMS, NW = 4, ES = D < 32 ? 1 : D / 32, ET = D / 16, ROWS = 16 * QT, OP = ROWS + 1;
+    constexpr int T = X_TERMS, NW = 4, ES = D < 32 ? 1 : D / 32, ET = D / 16, ROWS = 16 * QT, OP = D + 4;
     using L = FewLines<D>;
     constexpr int VB = KB_FEW * D;  // elements of a V block
-    constexpr int WORDS = 2 * VB / 2 > D * OP ? 2 * VB / 2 : D * OP;
+    constexpr int WORDS = VB > ROWS * OP ? VB : ROWS * OP;
     __shared__ __attribute__((aligned(1024))) uint32_t tile[NW][WORDS];  // two V blocks, or the outputs
     __shared__ float2 ml[NW][ROWS];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
-    const int g = blockIdx.x % a.n_kv_heads, split = blockIdx.x / a.n_kv_heads;
+    const int g = blockIdx.x % a.n_kv_heads, rest = blockIdx.x / a.n_kv_heads;
+    const int r0 = rest % a.q_tiles * ROWS, split = rest / a.q_tiles;
     const int b1 = min(a.blocks, (split + 1) * a.per_split);
     const uint16_t *K = static_cast<const uint16_t *>(a.k) + (int64_t)g * a.head_stride;
     const uint16_t *V = static_cast<const uint16_t *>(a.v) + (int64_t)g * a.head_stride;
@@ -630,7 +644,7 @@ __global__ __launch_bounds__(256, QT == 1 || D < 128 ? 2 : 1) void k_tree_attn_f
     u32x4_t qf[QT][ES][T];
 #pragma unroll
     for (int i = 0; i < QT; ++i) {
-        const int row = min(16 * i + col, a.rows - 1);
+        const int row = min(r0 + 16 * i + col, a.rows - 1);
         node[i] = row / a.G;
         const float *qs = a.q + (int64_t)node[i] * a.ld_q + (int64_t)(g * a.G + row - node[i] * a.G) * D + (8 * grp) % D;
         const float scale = D < 32 && grp >= 2 ? 0.0f : a.scale;
@@ -716,18 +730,23 @@ __global__ __launch_bounds__(256, QT == 1 || D < 128 ? 2 : 1) void k_tree_attn_f
         // the registers of both)
 #pragma unroll
         for (int i = 0; i < QT; ++i) {
-            const uint32_t bits = (uint32_t)visible(a, k, node[i]);
             float p[8], mx = -INFINITY;
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
+            for (int u = 0; u < 8; ++u)
                 p[u] = s[i][u >> 2][u & 3];
-                if (k.node0 >= 0 || k.len < KB_FEW)
-                    p[u] = (bits >> (16 * (u >> 2) + 4 * grp + (u & 3))) & 1 ? p[u] : -INFINITY;
-                mx = fmaxf(mx, p[u]);
+            if (k.node0 >= 0 || k.len < KB_FEW) {
+                uint32_t mine = (uint32_t)visible(a, k, node[i]) >> (4 * grp);
+                asm volatile("" : "+v"(mine));  // (a branch, and not selects in every block)
+#pragma unroll
+                for (int u = 0; u < 8; ++u)
+                    p[u] = (mine >> (16 * (u >> 2) + (u & 3))) & 1 ? p[u] : -INFINITY;
             }
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                mx = fmaxf(mx, p[u]);
             mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
             mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-            if (__any(mx > m_run[i])) {
+            if (__any(mx > m_run[i] + SLACK)) {
                 const float m_new = fmaxf(m_run[i], mx);
                 const float sc = m_run[i] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run[i] - m_new);
                 l_run[i] *= sc;
@@ -806,14 +825,12 @@ __global__ __launch_bounds__(256, QT == 1 || D < 128 ? 2 : 1) void k_tree_attn_f
         l_run[i] += __shfl_xor(l_run[i], 32, 64);
 #pragma unroll
         for (int et = 0; et < ET; ++et)
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-                to[(16 * et + 4 * grp + u) * OP + 16 * i + col] = o[i][et][u];
+            *reinterpret_cast<f32x4_t *>(to + (16 * i + col) * OP + 16 * et + 4 * grp) = o[i][et];
         if (grp == 0)
             ml[wave][16 * i + col] = make_float2(m_run[i], l_run[i]);
     }
     __syncthreads();
-    merge_waves<D, NW, OP, ROWS>(a, reinterpret_cast<const float *>(tile), WORDS, &ml[0][0], 0, g, split);
+    merge_waves<D, NW, ROWS>(a, reinterpret_cast<const float *>(tile), WORDS, &ml[0][0], r0, g, split);
 }
 
 // The shares of a (node, head) joined: a work-group each.  Every wave takes the
@@ -856,10 +873,12 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_tree_join(TreeAttnArgs a) {
 }
 
 // Rows of a tile and shares of the keys.  bfloat16: up to 32 rows on the kernel
-// for few, every wave of two work-groups per CU with keys of its own; else tiles of 64,
-// 96 or 128 rows, the fewest that hold a kv head's rows, in two work-groups per
-// CU.  float32: tiles of 16 rows, four work-groups per CU.
-constexpr int TA_GROUPS = 1024, TA_GROUPS_MFMA = 512, FEW_ROWS = 32;
+// for few, one work-group per CU (13 rows over 1200 keys, 40 heads: 10.3 us, 11.3
+// with two, which halves the keys of a share; one row over 60000 keys, 8
+// heads: 43 and 46); else tiles of 64, 96 or 128 rows, the fewest that hold a kv
+// head's rows, in two work-groups per CU (three: 24 -> 28 us for 61 rows over
+// 3001 keys, 32 heads).  float32: tiles of 16 rows, four work-groups per CU.
+constexpr int TA_GROUPS = 1024, TA_GROUPS_MFMA = 512, TA_GROUPS_FEW = 256, FEW_ROWS = 32;
 
 void plan(const sd_kv_layer *kv, int32_t n_heads, int32_t n, int32_t prefix, TreeAttnArgs *a) {
     const bool bf16 = kv->dtype == SD_BF16;
@@ -876,7 +895,7 @@ void plan(const sd_kv_layer *kv, int32_t n_heads, int32_t n, int32_t prefix, Tre
     const int kb = few ? KB_FEW : KB, step = few ? 4 : bf16 ? 1 : 2;  // step: blocks that a share has at least
     a->prefix_blocks = (prefix + kb - 1) / kb;
     a->blocks = a->prefix_blocks + (n + kb - 1) / kb;
-    const int units = a->q_tiles * a->n_kv_heads, groups = bf16 ? TA_GROUPS_MFMA : TA_GROUPS;
+    const int units = a->q_tiles * a->n_kv_heads, groups = few ? TA_GROUPS_FEW : bf16 ? TA_GROUPS_MFMA : TA_GROUPS;
     const int want = std::max(1, std::min((a->blocks + step - 1) / step, (groups + units - 1) / units));
     a->per_split = ((a->blocks + want - 1) / want + step - 1) / step * step;
     a->splits = (a->blocks + a->per_split - 1) / a->per_split;
