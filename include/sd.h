@@ -394,6 +394,41 @@ size_t sd_tree_accept_workspace(int32_t n, int32_t vocab);
 sd_status sd_kv_keep(void *kv, int64_t planes, int64_t plane_stride, int32_t row_bytes, int32_t capacity, int32_t base,
                      const int32_t *walk, int32_t n, void *hip_stream);
 
+/* sd_forward for the n nodes of a tree (tokens and parents HOST int32 [n], 1 <=
+ * n <= SD_TREE_MAX): node i at rotary position length + depth(i), its keys and
+ * values at position length + i, attending to the cache and its own ancestors.
+ * The cache's length stays: the nodes lie behind it until sd_kv_cache_keep
+ * takes some of them over or another forward overwrites them.  logits, when
+ * not NULL, is a DEVICE float32 [n, vocab].  Refuses a skip mask while the
+ * draft is quantized.  Errors: INVALID_ARG, CAPACITY (length + n above the
+ * capacity; nothing enqueued), OOM, DEVICE. */
+sd_status sd_forward_tree(sd_model *model, const int32_t *tokens, const int32_t *parents, int32_t n,
+                          const uint8_t *skip_mask, sd_kv_cache *cache, float *logits);
+/* Takes the nodes of a path (HOST, strictly ascending, 1 <= count) of the tree
+ * forward before over: their rows move to length, length + 1, ... and the
+ * length grows by count.  For a path from the root to one node, the cache is
+ * then the one that the path's tokens alone would have left.  Errors:
+ * INVALID_ARG (also without a tree forward since the last change), OOM, DEVICE. */
+sd_status sd_kv_cache_keep(sd_kv_cache *cache, const int32_t *path, int32_t count);
+
+/* The verification of a tree (Algorithm 2 for several chains at once): the
+ * full model's forward over its nodes, the greedy walk, and the cache left with
+ * the accepted path.  path (HOST int32 [n]) receives the nodes of the path, the
+ * root among them, count (HOST) their number, next (HOST) the model's own
+ * token after them: the tokens of the path past the root and next are those of
+ * greedy autoregressive decoding.  The length grows by count.  The root is the
+ * last committed token, which the cache does not hold yet.  Errors: as
+ * sd_forward_tree, and n * vocab above 2^31 (INVALID_ARG). */
+sd_status sd_verify_tree(sd_model *model, const int32_t *tokens, const int32_t *parents, int32_t n, sd_kv_cache *cache,
+                         int32_t *path, int32_t *count, int32_t *next);
+
+/* The rotary form of every forward of the model (NULL: the config's base,
+ * unscaled): for contexts past the trained one.  The forwards rotate whole heads
+ * in halves (layout SD_ROPE_HALF, rotary_dim head_dim; another form is
+ * UNIMPLEMENTED).  Every cache of the model must be empty.  Errors:
+ * INVALID_ARG, UNIMPLEMENTED, OOM, DEVICE. */
+sd_status sd_model_set_rope(sd_model *model, const sd_rope *rope);
+
 /* Skip-set search (Sec. 3.3, Eq. 1): z* = argmin f(z) over sublayer masks
  * z in {0, 1}^L, by Bayesian optimisation for a fixed number of steps.
  * Host code; every evaluation of f is one call of the objective.

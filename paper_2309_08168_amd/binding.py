@@ -27,7 +27,8 @@ EXPORTS = (
     "sd_self_spec_sample", "sd_autoregressive_sample", "sd_search_skip_set_fn", "sd_search_skip_set",
     "sd_model_time_kernel", "sd_model_kernel_time", "sd_measure_read_bandwidth", "sd_model_quantize_draft",
     "sd_model_draft_fp8", "sd_tree_layout", "sd_rope_append", "sd_tree_attention", "sd_tree_attention_workspace",
-    "sd_tree_accept", "sd_tree_accept_workspace", "sd_kv_keep",
+    "sd_tree_accept", "sd_tree_accept_workspace", "sd_kv_keep", "sd_forward_tree", "sd_kv_cache_keep", "sd_verify_tree",
+    "sd_model_set_rope",
     "sd_last_error", "sd_version",
 )
 
@@ -167,6 +168,10 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "sd_tree_accept": ([vp, i64, i32, vp, vp, i32, vp, vp, ctypes.c_size_t, vp], ctypes.c_int),
         "sd_tree_accept_workspace": ([i32, i32], ctypes.c_size_t),
         "sd_kv_keep": ([vp, i64, i64, i32, i32, i32, vp, i32, vp], ctypes.c_int),
+        "sd_forward_tree": ([vp, vp, vp, i32, vp, vp, vp], ctypes.c_int),
+        "sd_kv_cache_keep": ([vp, vp, i32], ctypes.c_int),
+        "sd_verify_tree": ([vp, vp, vp, i32, vp, vp, p(i32), p(i32)], ctypes.c_int),
+        "sd_model_set_rope": ([vp, p(sd_rope)], ctypes.c_int),
         "sd_last_error": ([], ctypes.c_char_p),
         "sd_version": ([], ctypes.c_char_p),
     }
@@ -298,6 +303,33 @@ class Model:
         lp = None if logits is None else ctypes.c_void_p(logits.data_ptr())
         check(load().sd_forward_static(self._h, _ptr(tok), tok.size, _ptr(sk), cache._h, lp))
         return logits
+
+    def forward_tree(self, tokens, parents, cache: "KVCache", skip=None, logits=None):
+        """sd_forward_tree; logits is an optional torch float32 cuda tensor [n, vocab]."""
+        tok = np.ascontiguousarray(tokens, dtype=np.int32)
+        par = np.ascontiguousarray(parents, dtype=np.int32)
+        if tok.shape != par.shape or tok.ndim != 1:
+            _refuse("tokens and parents are of one length")
+        sk = None if skip is None else np.ascontiguousarray(skip, dtype=np.uint8)
+        lp = None if logits is None else ctypes.c_void_p(logits.data_ptr())
+        check(load().sd_forward_tree(self._h, _ptr(tok), _ptr(par), tok.size, _ptr(sk), cache._h, lp))
+        return logits
+
+    def verify_tree(self, tokens, parents, cache: "KVCache"):
+        """sd_verify_tree: (path int32 [count], next token)."""
+        tok = np.ascontiguousarray(tokens, dtype=np.int32)
+        par = np.ascontiguousarray(parents, dtype=np.int32)
+        if tok.shape != par.shape or tok.ndim != 1:
+            _refuse("tokens and parents are of one length")
+        path = np.zeros(max(tok.size, 1), np.int32)
+        count, nxt = ctypes.c_int32(), ctypes.c_int32()
+        check(load().sd_verify_tree(self._h, _ptr(tok), _ptr(par), tok.size, cache._h, _ptr(path), ctypes.byref(count),
+                                    ctypes.byref(nxt)))
+        return path[:count.value].copy(), nxt.value
+
+    def set_rope(self, form: Optional[sd_rope]):
+        """sd_model_set_rope: the rotary form of every forward (None: the config's)."""
+        check(load().sd_model_set_rope(self._h, None if form is None else ctypes.byref(form)))
 
     def quantize_draft(self, skip):
         """sd_model_quantize_draft: FP8 copies of the weights of the sublayers
@@ -703,3 +735,8 @@ class KVCache:
 
     def set_length(self, n: int):
         check(load().sd_kv_cache_set_length(self._h, n))
+
+    def keep(self, path):
+        """sd_kv_cache_keep: takes a path of the last tree forward over."""
+        p = np.ascontiguousarray(path, dtype=np.int32)
+        check(load().sd_kv_cache_keep(self._h, _ptr(p), p.size))

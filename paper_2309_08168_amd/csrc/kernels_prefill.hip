@@ -797,6 +797,16 @@ __global__ __launch_bounds__(NT) void k_pf_norm_split(float *h, const float *par
     }
 }
 
+// Rows [M][K] (K a multiple of 8), ldx apart, as terms.
+__global__ __launch_bounds__(256) void k_pf_terms(const float *x, int64_t ldx, int K, PfTerms out) {
+    const int m = blockIdx.x;
+    for (int k = 8 * threadIdx.x; k < K; k += 2048) {
+        float v[8];
+        load8f(x + (int64_t)m * ldx + k, v);
+        store_terms8(out, m, k, K, v);
+    }
+}
+
 // ---------------------------------------------------------------------------
 // Causal attention, head_dim 128.  A work-group takes 128 query rows of one
 // head, 32 per wave, over one chunk of the keys, in stages of 64 keys whose K
@@ -1064,6 +1074,13 @@ __global__ __launch_bounds__(NT) void k_pf_attn_terms(PfAttnArgs a, PfTerms out)
 
 hipError_t launch_pf_embed(const uint16_t *emb, int d, const int32_t *tokens, int M, float *h, hipStream_t s) {
     hipLaunchKernelGGL(k_pf_embed, dim3(M, (d + 2047) / 2048), dim3(256), 0, s, emb, d, tokens, h);
+    return hipGetLastError();
+}
+
+hipError_t launch_pf_terms(const float *x, int64_t ldx, int K, int M, const PfTerms &t, hipStream_t s) {
+    if (K % 8 || (t.blocks && K % 32))
+        return hipErrorInvalidValue;
+    hipLaunchKernelGGL(k_pf_terms, dim3(M), dim3(256), 0, s, x, ldx, K, t);
     return hipGetLastError();
 }
 

@@ -4,6 +4,7 @@
 // self-speculative, Algorithm 2 with the static draft exit of Sec. 3.4).
 #include "sd.h"
 #include "sd_internal.h"
+#include "tree.h"
 
 #include <hip/hip_runtime.h>
 
@@ -101,6 +102,7 @@ struct sd_kv_cache {
     bool owns;
     int32_t cap;
     int32_t len;
+    int32_t nodes = 0;  // of the last tree forward, behind len
 };
 
 struct sd_model {
@@ -129,6 +131,15 @@ struct sd_model {
     int attn_splits_cap = 0;  // key chunks ws.attn_o / ws.attn_ml hold
     float2 *rope = nullptr;
     int rope_cap = 0;
+    sd_rope rope_spec{};  // the rotary form of every forward
+    // token trees: the tree on the device (see tree_upload) and what it was
+    // copied from, the QKV products of a tree forward's rows, the attention's
+    // workspace, and a verification's logits, walk and row maxima
+    uint64_t *d_tree = nullptr, *tree_keys = nullptr;
+    std::vector<uint64_t> h_tree;
+    float *tree_qkv = nullptr, *tree_ws = nullptr, *tree_logits = nullptr;
+    int32_t *tree_walk = nullptr;
+    int d_tree_cap = 0, tree_keys_cap = 0, tree_qkv_cap = 0, tree_ws_cap = 0, tree_logits_cap = 0, tree_walk_cap = 0;
     // large-M forward (bfloat16 models), PF_ROWS rows each: residual stream,
     // rotated queries, partial sums of residual updates (and the attention's
     // chunks), and the GEMM inputs as X_TERMS terms: normed rows and attention
@@ -322,18 +333,21 @@ void dev_free(void *p) {
         (void)hipFree(p);
 }
 
-// Rotary table for positions [0, cap): (cos, sin) of pos * base^(-2i/dh),
-// computed in double and rounded to float.
+// Rotary table for positions [0, cap): (cos, sin) of pos times the pair's
+// frequency (base^(-2i/dh) unless scaled), computed in double and rounded to float.
 sd_status ensure_rope(sd_model *m, int cap) {
     if (cap <= m->rope_cap)
         return SD_OK;
     const int half = m->cfg.head_dim / 2;
     std::vector<float2> tab((size_t)cap * half);
+    std::vector<double> theta(half);
+    for (int i = 0; i < half; ++i)
+        theta[i] = rope_frequency(m->rope_spec, i);
+    const double gain = rope_gain(m->rope_spec);
     for (int p = 0; p < cap; ++p)
         for (int i = 0; i < half; ++i) {
-            const double theta = std::pow((double)m->cfg.rope_base, -2.0 * (double)i / (double)m->cfg.head_dim);
-            const double ang = (double)p * theta;
-            tab[(size_t)p * half + i] = make_float2((float)std::cos(ang), (float)std::sin(ang));
+            const double ang = (double)p * theta[i];
+            tab[(size_t)p * half + i] = make_float2((float)(gain * std::cos(ang)), (float)(gain * std::sin(ang)));
         }
     SD_HIP(hipStreamSynchronize(m->stream));
     float2 *nt = nullptr;
@@ -488,14 +502,41 @@ struct HeadSpec {
 // to a bound; several calls continue one forward), forward_head.  max_rows
 // (known to the host) bounds the row count and picks the kernels; skip is a
 // host mask or null.
+struct TreeRows;
 struct ForwardCursor {
     const Plan *P = nullptr;
+    const TreeRows *tree = nullptr;  // rows of a token tree, or null
     int max_rows = 0;
     int ctx_max = 0;       // host bound on the positions after this forward
     int next_layer = 0;
     int pending = 0;       // split-K partials not yet folded into h
     bool guarded = false;  // launches may find the step cancelled (ctl->m = 0)
 };
+
+// The rows of one forward that are nodes row0 .. nodes - 1 of a token tree
+// behind `prefix` cache positions: their rotary positions and mask words (of
+// `nodes` bits) on the device.
+struct TreeRows {
+    int32_t prefix, row0, nodes;
+    const int32_t *positions;
+    const uint64_t *mask;
+};
+
+// The attention sublayer of a tree's rows between its products: qkv (nq wide)
+// rotated into q and the cache, then, with out set, the attention into out.
+sd_status tree_attend(sd_model *m, const TreeRows &t, void *kbase, void *vbase, int32_t cap, const float *qkv, float *q,
+                      float *out) {
+    const sd_config &c = m->cfg;
+    const int64_t hd = (int64_t)c.n_heads * c.head_dim, nq = hd + 2 * (int64_t)c.n_kv_heads * c.head_dim;
+    const int32_t rows = t.nodes - t.row0;
+    const sd_kv_layer kv{kbase, vbase, (int64_t)cap * c.head_dim, c.head_dim, c.n_kv_heads, cap, c.head_dim, c.dtype};
+    SD_TRY(sd_rope_append(&m->rope_spec, qkv, nq, rows, c.n_heads, t.positions, 0, q, hd, &kv, t.prefix + t.row0,
+                          m->stream));
+    if (!out)
+        return SD_OK;
+    return tree_attention(&kv, q, hd, c.n_heads, rows, t.nodes, t.prefix, t.mask, 0.0f, out, hd, m->tree_ws,
+                          sizeof(float) * (size_t)m->tree_ws_cap, m->stream);
+}
 
 // host_tokens: the max_rows tokens of a forward that ends at ctx_max, or null
 // when the control block on the device holds the step.
@@ -544,40 +585,55 @@ sd_status forward_layers(sd_model *m, const Workspace &w, void *kv, int32_t cap,
         if (!(skip && skip[2 * l])) {
             char *kbase = static_cast<char *>(kv) + (size_t)(2 * l) * c.n_kv_heads * head_stride * ksz;
             char *vbase = static_cast<char *>(kv) + (size_t)(2 * l + 1) * c.n_kv_heads * head_stride * ksz;
-            EpiArgs e{};
-            e.q = w.q;
-            e.ld_q = ldq;
-            e.kcache = kbase;
-            e.vcache = vbase;
-            e.kv_head_stride = head_stride;
-            e.rope = m->rope;
-            e.n_heads = c.n_heads;
-            e.n_kv_heads = c.n_kv_heads;
-            e.head_dim = c.head_dim;
-            e.ffn = c.ffn_dim;
-            SD_TRY(prep_norm(m, w, P[LK_QKV], m->attn_norm[l], pending));
-            SD_TRY(lin(LK_QKV, l, m->w_qkv[l], w.h, ldh, m->attn_norm[l], e, w.xa));
-            AttnArgs at{};
-            at.q = w.q;
-            at.ld_q = ldq;
-            at.kcache = kbase;
-            at.vcache = vbase;
-            at.kv_head_stride = head_stride;
-            at.part_o = w.attn_o;
-            at.part_ml = w.attn_ml;
-            at.out = w.o;
-            at.ld_out = ldq;
-            if (P[LK_O].path == PATH_MFMA) {
-                at.out_x = w.xa;
-                at.ld_out = w.xld;
+            if (cur->tree) {
+                EpiArgs e{};
+                e.out = m->tree_qkv;
+                e.ld_out = (int64_t)(c.n_heads + 2 * c.n_kv_heads) * c.head_dim;
+                Plan raw = P[LK_QKV];
+                raw.epi = EPI_STORE;
+                SD_TRY(prep_norm(m, w, raw, m->attn_norm[l], pending));
+                SD_TRY(run_linear(m, w, raw, max_rows, m->w_qkv[l], w.h, ldh, m->attn_norm[l], e, w.xa));
+                SD_TRY(tree_attend(m, *cur->tree, kbase, vbase, cap, m->tree_qkv, w.q, w.o));
+                if (P[LK_O].path == PATH_MFMA)
+                    SD_TRY(launch(launch_prep_norm(w.o, ldq, nullptr, m->bf16, P[LK_O].K, w.ctl, w.xa, nullptr, 0,
+                                                   nullptr, m->stream),
+                                  "attention output terms"));
+            } else {
+                EpiArgs e{};
+                e.q = w.q;
+                e.ld_q = ldq;
+                e.kcache = kbase;
+                e.vcache = vbase;
+                e.kv_head_stride = head_stride;
+                e.rope = m->rope;
+                e.n_heads = c.n_heads;
+                e.n_kv_heads = c.n_kv_heads;
+                e.head_dim = c.head_dim;
+                e.ffn = c.ffn_dim;
+                SD_TRY(prep_norm(m, w, P[LK_QKV], m->attn_norm[l], pending));
+                SD_TRY(lin(LK_QKV, l, m->w_qkv[l], w.h, ldh, m->attn_norm[l], e, w.xa));
+                AttnArgs at{};
+                at.q = w.q;
+                at.ld_q = ldq;
+                at.kcache = kbase;
+                at.vcache = vbase;
+                at.kv_head_stride = head_stride;
+                at.part_o = w.attn_o;
+                at.part_ml = w.attn_ml;
+                at.out = w.o;
+                at.ld_out = ldq;
+                if (P[LK_O].path == PATH_MFMA) {
+                    at.out_x = w.xa;
+                    at.ld_out = w.xld;
+                }
+                at.n_heads = c.n_heads;
+                at.n_kv_heads = c.n_kv_heads;
+                at.head_dim = c.head_dim;
+                at.cap = cap;
+                at.ctx_max = cur->ctx_max;
+                at.ctl = w.ctl;
+                SD_TRY(launch(launch_attention(at, m->bf16, max_rows, m->stream), "attention"));
             }
-            at.n_heads = c.n_heads;
-            at.n_kv_heads = c.n_kv_heads;
-            at.head_dim = c.head_dim;
-            at.cap = cap;
-            at.ctx_max = cur->ctx_max;
-            at.ctl = w.ctl;
-            SD_TRY(launch(launch_attention(at, m->bf16, max_rows, m->stream), "attention"));
             EpiArgs eo{};
             eo.out = w.h;
             eo.ld_out = ldh;
@@ -744,9 +800,9 @@ sd_status ensure_gen_cache(sd_model *m, int32_t cap) {
 // positions [start, start + M), matrix-core GEMMs over all rows at once;
 // logits (device [M][vocab]) when not null.  Without logits the forward ends
 // with the keys and values of the last attention sublayer: nothing reads what
-// would follow.
+// would follow.  tree: the rows are the nodes of a token tree, or null.
 sd_status enqueue_forward_large(sd_model *m, void *kv, int32_t cap, const uint8_t *skip, const int32_t *dev_tokens,
-                                int32_t M, int32_t start, float *logits) {
+                                int32_t M, int32_t start, float *logits, const TreeRows *tree = nullptr) {
     const sd_config &c = m->cfg;
     const int H = c.n_heads, KVH = c.n_kv_heads, dh = c.head_dim, d = c.d_model, F = c.ffn_dim;
     const int hd = H * dh, nq = (H + 2 * KVH) * dh;
@@ -810,26 +866,38 @@ sd_status enqueue_forward_large(sd_model *m, void *kv, int32_t cap, const uint8_
             uint16_t *kbase = reinterpret_cast<uint16_t *>(kv) + (size_t)(2 * l) * KVH * head_stride;
             uint16_t *vbase = reinterpret_cast<uint16_t *>(kv) + (size_t)(2 * l + 1) * KVH * head_stride;
             SD_TRY(norm(m->attn_norm[l]));
-            rope.kcache = kbase;
-            rope.vcache = vbase;
-            SD_TRY(product(m->w_qkv[l], nq, d, terms, m->pf_q, hd, EPI_QKV));
-            if (!logits && l == last_attn)
-                return SD_OK;
-            PfAttnArgs at{};
-            at.q = m->pf_q;
-            at.ldq = hd;
-            at.kcache = kbase;
-            at.vcache = vbase;
-            at.kv_head_stride = head_stride;
-            at.out = m->pf_part;
-            at.ldo = hd;
-            at.ml = m->pf_ml;
-            at.M = M;
-            at.start = start;
-            at.n_heads = H;
-            at.n_kv_heads = KVH;
-            at.head_dim = dh;
-            SD_TRY(launch(launch_pf_attention(at, terms, s), "prefill attention"));
+            if (tree) {
+                // the QKV product, and after it the attention's output, lie in
+                // pf_part, whose partial sums the norm has taken
+                static_assert(PF_PART_ROWS >= 3 * PF_ROWS && PF_ROWS >= SD_TREE_MAX, "rows of a QKV product fit");
+                SD_TRY(product(m->w_qkv[l], nq, d, terms, m->pf_part, nq, EPI_STORE));
+                const bool last = !logits && l == last_attn;
+                SD_TRY(tree_attend(m, *tree, kbase, vbase, cap, m->pf_part, m->pf_q, last ? nullptr : m->pf_part));
+                if (last)
+                    return SD_OK;
+                SD_TRY(launch(launch_pf_terms(m->pf_part, hd, hd, M, terms, s), "attention output terms"));
+            } else {
+                rope.kcache = kbase;
+                rope.vcache = vbase;
+                SD_TRY(product(m->w_qkv[l], nq, d, terms, m->pf_q, hd, EPI_QKV));
+                if (!logits && l == last_attn)
+                    return SD_OK;
+                PfAttnArgs at{};
+                at.q = m->pf_q;
+                at.ldq = hd;
+                at.kcache = kbase;
+                at.vcache = vbase;
+                at.kv_head_stride = head_stride;
+                at.out = m->pf_part;
+                at.ldo = hd;
+                at.ml = m->pf_ml;
+                at.M = M;
+                at.start = start;
+                at.n_heads = H;
+                at.n_kv_heads = KVH;
+                at.head_dim = dh;
+                SD_TRY(launch(launch_pf_attention(at, terms, s), "prefill attention"));
+            }
             SD_TRY(product(m->w_o[l], d, hd, terms, nullptr, d, EPI_RESID));
         }
         if (!(skip && skip[2 * l + 1])) {
@@ -1212,6 +1280,7 @@ sd_status forward(sd_model *m, const int32_t *tokens, int32_t n, const uint8_t *
         return fail(SD_ERR_CAPACITY, "cache of capacity " + std::to_string(kc->cap) + " holds " +
                                          std::to_string(kc->len) + " positions; " + std::to_string(n) +
                                          " more do not fit");
+    kc->nodes = 0;
     if (m->pf_ok && n > MAX_ROWS) {
         SD_TRY(ensure_buf(m, &m->d_tokens, &m->d_tokens_cap, n));
         SD_HIP(hipMemcpyAsync(m->d_tokens, tokens, sizeof(int32_t) * (size_t)n, hipMemcpyHostToDevice, m->stream));
@@ -1234,6 +1303,200 @@ sd_status forward(sd_model *m, const int32_t *tokens, int32_t n, const uint8_t *
     collect_timing(m);
     kc->len += n;
     return SD_OK;
+}
+
+// Checks a tree forward, copies the tree to the device and enqueues the
+// forward; *dev_tokens and *dev_parents receive the device copies.  The logits
+// (device [n][vocab], or null) and the cache rows are there once the stream has run.
+sd_status tree_forward(sd_model *m, const int32_t *tokens, const int32_t *parents, int32_t n, const uint8_t *skip,
+                       sd_kv_cache *kc, float *logits, const int32_t **dev_tokens, const int32_t **dev_parents) {
+    const int32_t words = (n + 63) / 64;
+    std::vector<int32_t> depth((size_t)n);
+    std::vector<uint64_t> mask((size_t)n * words);
+    SD_TRY(sd_tree_layout(parents, n, depth.data(), mask.data()));
+    SD_TRY(check_tokens(m, tokens, n, "tokens"));
+    SD_TRY(check_mask(m, skip));
+    if (skip && m->has_fp8)
+        return fail(SD_ERR_INVALID_ARG, "while the draft is quantized, tree forwards take no skip mask");
+    if ((int64_t)kc->len + n > kc->cap)
+        return fail(SD_ERR_CAPACITY, "cache of capacity " + std::to_string(kc->cap) + " holds " +
+                                         std::to_string(kc->len) + " positions; " + std::to_string(n) +
+                                         " nodes do not fit");
+    const sd_config &c = m->cfg;
+    // one forward of every node on the large-M path, or MAX_ROWS of them at a
+    // time: parents come first, so a node's ancestors are in its own rows or before
+    const bool large = m->pf_ok && n > MAX_ROWS;
+    const int32_t step = large ? n : MAX_ROWS;
+    // device copy: per forward the mask words of its rows, as many as its nodes
+    // need; then the positions, the parents and the tokens
+    std::vector<uint64_t> &h = m->h_tree;
+    h.clear();
+    std::vector<size_t> at;
+    size_t ws = 1;
+    const sd_kv_layer any{kc->buf, kc->buf, (int64_t)kc->cap * c.head_dim, c.head_dim, c.n_kv_heads, kc->cap,
+                          c.head_dim, c.dtype};
+    for (int32_t r0 = 0; r0 < n; r0 += step) {
+        const int32_t nodes = std::min(n, r0 + step), w = (nodes + 63) / 64;
+        at.push_back(h.size());
+        for (int32_t r = r0; r < nodes; ++r)
+            for (int32_t i = 0; i < w; ++i)
+                h.push_back(mask[(size_t)r * words + i]);
+        ws = std::max(ws, tree_attention_bytes(&any, c.n_heads, nodes - r0, nodes, kc->len));
+    }
+    const size_t ints = h.size();
+    h.resize(ints + (size_t)(3 * n + 1) / 2);
+    int32_t *hp = reinterpret_cast<int32_t *>(h.data() + ints);
+    for (int32_t i = 0; i < n; ++i) {
+        hp[i] = kc->len + depth[i];
+        hp[n + i] = parents[i];
+        hp[2 * n + i] = tokens[i];
+    }
+    SD_TRY(ensure_buf(m, &m->d_tree, &m->d_tree_cap, (int)h.size()));
+    SD_TRY(ensure_buf(m, &m->tree_ws, &m->tree_ws_cap, (int)((ws + 3) / 4)));
+    if (!large)
+        SD_TRY(ensure_buf(m, &m->tree_qkv, &m->tree_qkv_cap, MAX_ROWS * (c.n_heads + 2 * c.n_kv_heads) * c.head_dim));
+    SD_HIP(hipMemcpyAsync(m->d_tree, h.data(), sizeof(uint64_t) * h.size(), hipMemcpyHostToDevice, m->stream));
+    const int32_t *dp = reinterpret_cast<const int32_t *>(m->d_tree + ints);
+    *dev_parents = dp + n;
+    *dev_tokens = dp + 2 * n;
+    kc->nodes = 0;
+    for (int32_t r0 = 0, i = 0; r0 < n; r0 += step, ++i) {
+        const int32_t nodes = std::min(n, r0 + step), rows = nodes - r0;
+        const TreeRows tree{kc->len, r0, nodes, dp + r0, m->d_tree + at[i]};
+        float *lg = logits ? logits + (size_t)r0 * c.vocab : nullptr;
+        if (large) {
+            SD_TRY(enqueue_forward_large(m, kc->buf, kc->cap, skip, *dev_tokens, n, kc->len, lg, &tree));
+            continue;
+        }
+        // the measurement hook's events stay out of this path
+        const int timed = m->timed_kind;
+        m->timed_kind = -1;
+        HeadSpec hs;
+        hs.run = lg != nullptr;
+        hs.logits = lg;
+        ForwardCursor cur;
+        sd_status st = forward_begin(m, m->ws, rows, kc->len + nodes, &cur, tokens + r0);
+        cur.tree = &tree;
+        if (st == SD_OK)
+            st = forward_layers(m, m->ws, kc->buf, kc->cap, skip, &cur, c.n_layers);
+        if (st == SD_OK)
+            st = forward_head(m, m->ws, &cur, hs);
+        m->timed_kind = timed;
+        SD_TRY(st);
+    }
+    return SD_OK;
+}
+
+sd_status check_tree_call(sd_model *m, int32_t n, const sd_kv_cache *kc) {
+    if (!m || !kc)
+        return fail(SD_ERR_INVALID_ARG, "model or cache is null");
+    if (kc->model != m)
+        return fail(SD_ERR_INVALID_ARG, "cache belongs to another model");
+    if (n < 1 || n > SD_TREE_MAX)
+        return fail(SD_ERR_INVALID_ARG, "a tree has 1 to " + std::to_string(SD_TREE_MAX) + " nodes");
+    return SD_OK;
+}
+
+sd_status forward_tree(sd_model *m, const int32_t *tokens, const int32_t *parents, int32_t n, const uint8_t *skip,
+                       sd_kv_cache *kc, float *logits) {
+    SD_TRY(check_tree_call(m, n, kc));
+    const int32_t *dt = nullptr, *dp = nullptr;
+    SD_TRY(tree_forward(m, tokens, parents, n, skip, kc, logits, &dt, &dp));
+    SD_HIP(hipStreamSynchronize(m->stream));
+    kc->nodes = n;
+    return SD_OK;
+}
+
+// Moves the rows behind kc->len that walk (device, for n nodes) names together.
+sd_status enqueue_keep(sd_model *m, sd_kv_cache *kc, const int32_t *walk, int32_t n) {
+    const sd_config &c = m->cfg;
+    const int32_t row = (int32_t)(c.head_dim * m->wsize);
+    return sd_kv_keep(kc->buf, (int64_t)c.n_layers * 2 * c.n_kv_heads, (int64_t)kc->cap * row, row, kc->cap, kc->len, walk,
+                      n, m->stream);
+}
+
+sd_status cache_keep(sd_kv_cache *kc, const int32_t *path, int32_t count) {
+    if (!kc || !kc->model)
+        return fail(SD_ERR_INVALID_ARG, "cache is null or its model is gone");
+    if (!path || count < 1 || count > kc->nodes)
+        return fail(SD_ERR_INVALID_ARG, "a path has 1 to " + std::to_string(kc->nodes) +
+                                            " nodes of the tree forward before");
+    for (int32_t i = 0; i < count; ++i)
+        if (path[i] < 0 || path[i] >= kc->nodes || (i > 0 && path[i] <= path[i - 1]))
+            return fail(SD_ERR_INVALID_ARG, "a path ascends within the nodes of the tree");
+    sd_model *m = kc->model;
+    SD_TRY(ensure_buf(m, &m->tree_walk, &m->tree_walk_cap, 2 + 2 * kc->nodes));
+    m->h_tree.resize((size_t)count + 1);
+    int32_t *h = reinterpret_cast<int32_t *>(m->h_tree.data());
+    h[0] = count;
+    h[1] = 0;
+    std::copy(path, path + count, h + 2);
+    SD_HIP(hipMemcpyAsync(m->tree_walk, h, sizeof(int32_t) * (size_t)(count + 2), hipMemcpyHostToDevice, m->stream));
+    SD_TRY(enqueue_keep(m, kc, m->tree_walk, kc->nodes));
+    SD_HIP(hipStreamSynchronize(m->stream));
+    kc->len += count;
+    kc->nodes = 0;
+    return SD_OK;
+}
+
+sd_status verify_tree(sd_model *m, const int32_t *tokens, const int32_t *parents, int32_t n, sd_kv_cache *kc,
+                      int32_t *path, int32_t *count, int32_t *next) {
+    SD_TRY(check_tree_call(m, n, kc));
+    if (!path || !count || !next)
+        return fail(SD_ERR_INVALID_ARG, "path, count or next is null");
+    const int32_t vocab = m->cfg.vocab;
+    if ((int64_t)n * vocab > INT32_MAX)
+        return fail(SD_ERR_INVALID_ARG, "n * vocab is above 2^31");
+    const size_t keys = sd_tree_accept_workspace(n, vocab);
+    SD_TRY(ensure_buf(m, &m->tree_logits, &m->tree_logits_cap, n * vocab));
+    SD_TRY(ensure_buf(m, &m->tree_keys, &m->tree_keys_cap, (int)(keys / sizeof(uint64_t))));
+    SD_TRY(ensure_buf(m, &m->tree_walk, &m->tree_walk_cap, 2 + 2 * n));
+    const int32_t *dt = nullptr, *dp = nullptr;
+    SD_TRY(tree_forward(m, tokens, parents, n, nullptr, kc, m->tree_logits, &dt, &dp));
+    SD_TRY(sd_tree_accept(m->tree_logits, vocab, vocab, dt, dp, n, m->tree_walk, m->tree_keys, keys, m->stream));
+    SD_TRY(enqueue_keep(m, kc, m->tree_walk, n));
+    std::vector<int32_t> walk((size_t)n + 2);
+    SD_HIP(hipMemcpyAsync(walk.data(), m->tree_walk, sizeof(int32_t) * walk.size(), hipMemcpyDeviceToHost, m->stream));
+    SD_HIP(hipStreamSynchronize(m->stream));
+    if (walk[0] < 1 || walk[0] > n)
+        return fail(SD_ERR_DEVICE, "the walk left no path");
+    *count = walk[0];
+    *next = walk[1];
+    std::copy(walk.begin() + 2, walk.begin() + 2 + walk[0], path);
+    kc->len += walk[0];
+    return SD_OK;
+}
+
+sd_rope plain_rope(const sd_config &c) {
+    sd_rope r{};
+    r.base = c.rope_base;
+    r.factor = 1.0;
+    r.rotary_dim = c.head_dim;
+    r.layout = SD_ROPE_HALF;
+    r.scaling = SD_ROPE_UNSCALED;
+    return r;
+}
+
+sd_status set_rope(sd_model *m, const sd_rope *rope) {
+    if (!m)
+        return fail(SD_ERR_INVALID_ARG, "model is null");
+    const sd_rope spec = rope ? *rope : plain_rope(m->cfg);
+    SD_TRY(check_rope(&spec, m->cfg.head_dim));
+    if (spec.layout != SD_ROPE_HALF || spec.rotary_dim != m->cfg.head_dim)
+        return fail(SD_ERR_UNIMPLEMENTED, "a model's forwards rotate whole heads in halves");
+    for (const sd_kv_cache *c : m->caches)
+        if (c->len > 0 || c->nodes > 0)
+            return fail(SD_ERR_INVALID_ARG, "a cache holds keys rotated the old way: truncate it to 0 first");
+    const sd_rope old = m->rope_spec;
+    const int cap = m->rope_cap;
+    m->rope_spec = spec;
+    m->rope_cap = 0;
+    const sd_status st = cap > 0 ? ensure_rope(m, cap) : SD_OK;
+    if (st != SD_OK) {  // the old table is still there
+        m->rope_spec = old;
+        m->rope_cap = cap;
+    }
+    return st;
 }
 
 }  // namespace
@@ -1322,6 +1585,7 @@ sd_status forward_static(sd_model *m, const int32_t *tokens, int32_t n, const ui
         return fail(SD_ERR_CAPACITY, "cache of capacity " + std::to_string(kc->cap) + " holds " +
                                          std::to_string(kc->len) + " positions; " + std::to_string(n) +
                                          " more do not fit");
+    kc->nodes = 0;
     Workspace w;
     const size_t need = carve_workspace(m, kc->cap, nullptr, &w);
     if (need > STATIC_SCRATCH_BYTES)
@@ -1436,6 +1700,12 @@ void destroy_model(sd_model *m) {
     dev_free(m->ws.attn_o);
     dev_free(m->ws.attn_ml);
     dev_free(m->rope);
+    dev_free(m->d_tree);
+    dev_free(m->tree_keys);
+    dev_free(m->tree_qkv);
+    dev_free(m->tree_ws);
+    dev_free(m->tree_logits);
+    dev_free(m->tree_walk);
     dev_free(m->pf_h);
     dev_free(m->pf_q);
     dev_free(m->pf_part);
@@ -1494,6 +1764,7 @@ sd_status create_model(const sd_config *cfg, const sd_weights *w, void *stream, 
     m->fp8_q.assign(L, {nullptr, nullptr, nullptr, nullptr});
     m->fp8_e.assign(L, {nullptr, nullptr, nullptr, nullptr});
     m->stream = reinterpret_cast<hipStream_t>(stream);
+    m->rope_spec = plain_rope(*cfg);
 
     int max_head_tiles = 1;
     for (int k = 0; k < LK_COUNT; ++k) {
@@ -1655,6 +1926,7 @@ sd_status sd_kv_cache_truncate(sd_kv_cache *cache, int32_t len) {
     if (len < 0 || len > cache->len)
         return fail(SD_ERR_INVALID_ARG, "truncate length must be in [0, length]");
     cache->len = len;
+    cache->nodes = 0;
     return SD_OK;
 }
 
@@ -1664,6 +1936,7 @@ sd_status sd_kv_cache_set_length(sd_kv_cache *cache, int32_t len) {
     if (len < 0 || len > cache->cap)
         return fail(SD_ERR_CAPACITY, "length must be in [0, capacity]");
     cache->len = len;
+    cache->nodes = 0;
     return SD_OK;
 }
 
@@ -1676,6 +1949,22 @@ sd_status sd_forward_static(sd_model *model, const int32_t *tokens, int32_t n, c
                             sd_kv_cache *cache, float *logits) {
     SD_GUARD(return forward_static(model, tokens, n, skip_mask, cache, logits);)
 }
+
+sd_status sd_forward_tree(sd_model *model, const int32_t *tokens, const int32_t *parents, int32_t n,
+                          const uint8_t *skip_mask, sd_kv_cache *cache, float *logits) {
+    SD_GUARD(return forward_tree(model, tokens, parents, n, skip_mask, cache, logits);)
+}
+
+sd_status sd_kv_cache_keep(sd_kv_cache *cache, const int32_t *path, int32_t count) {
+    SD_GUARD(return cache_keep(cache, path, count);)
+}
+
+sd_status sd_verify_tree(sd_model *model, const int32_t *tokens, const int32_t *parents, int32_t n, sd_kv_cache *cache,
+                         int32_t *path, int32_t *count, int32_t *next) {
+    SD_GUARD(return verify_tree(model, tokens, parents, n, cache, path, count, next);)
+}
+
+sd_status sd_model_set_rope(sd_model *model, const sd_rope *rope) { SD_GUARD(return set_rope(model, rope);) }
 
 sd_status sd_model_quantize_draft(sd_model *model, const uint8_t *skip_mask) {
     SD_GUARD(return quantize_draft(model, skip_mask);)

@@ -361,6 +361,8 @@ hipError_t launch_pf_embed(const uint16_t *emb, int d, const int32_t *tokens, in
 // ([splits][M][K], in split order).
 hipError_t launch_pf_norm_split(float *h, const float *part, int splits, int K, int M, const uint16_t *gain, float eps,
                                 const PfTerms &t, hipStream_t s);
+// Rows x [M][K], ldx apart, as terms.
+hipError_t launch_pf_terms(const float *x, int64_t ldx, int K, int M, const PfTerms &t, hipStream_t s);
 // C = A W^T (EPI_STORE), the partial sums of a residual update into a.part
 // (EPI_RESID; *out receives their number, for launch_pf_norm_split), the SwiGLU
 // of a gate/up product as terms (EPI_SWIGLU), or the rotated q and the cache

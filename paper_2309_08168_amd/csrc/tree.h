@@ -1,5 +1,5 @@
-// The operators of token trees (tree_ops.hip, tree_attention.hip): arguments
-// and launchers.
+// What the operators of token trees (tree_ops.hip, tree_attention.hip) share
+// with each other and with the model's forwards.
 #pragma once
 
 #include "sd.h"
@@ -10,22 +10,18 @@ namespace sdk {
 // Refuses a layer that breaks the rules of sd_kv_layer.
 sd_status check_layer(const sd_kv_layer *kv);
 
-struct RopeArgs {
-    // frequency of pair i: f = exp2(i * step); YARN then weighs f and f / factor
-    double step, inv_factor, turns, beta_slow, inv_beta;
-    float gain;
-    int32_t half, interleaved, yarn;  // half: pairs of a head
-    const float *qkv;
-    int64_t ld_qkv;
-    const int32_t *positions;
-    int32_t pos0, n, n_heads, n_kv_heads, head_dim;
-    float *q;
-    int64_t ld_q;
-    void *k, *v;
-    int64_t head_stride, row_stride;
-    int32_t slot;
-};
-// Checks a rotary form for a head_dim and fills its part of RopeArgs.
-sd_status rope_form(const sd_rope *rope, int32_t head_dim, RopeArgs *out);
+// Refuses a rotary form for a head_dim.
+sd_status check_rope(const sd_rope *rope, int32_t head_dim);
+// Angle per position of pair i, and the factor on cosines and sines, of a
+// checked form (float64, on the host).
+double rope_frequency(const sd_rope &rope, int32_t i);
+double rope_gain(const sd_rope &rope);
+
+// sd_tree_attention for the last n rows of a tree of `nodes` (mask: the words
+// of those rows); sd_tree_attention itself has n = nodes.
+sd_status tree_attention(const sd_kv_layer *kv, const float *q, int64_t ld_q, int32_t n_heads, int32_t n, int32_t nodes,
+                         int32_t prefix, const uint64_t *mask, float scale, float *out, int64_t ld_out, void *workspace,
+                         size_t workspace_bytes, hipStream_t s);
+size_t tree_attention_bytes(const sd_kv_layer *kv, int32_t n_heads, int32_t n, int32_t nodes, int32_t prefix);
 
 }  // namespace sdk

@@ -40,12 +40,13 @@ struct TreeAttnArgs {
     int64_t ld_q;
     const void *k, *v;
     int64_t head_stride, row_stride;
-    const uint64_t *mask;  // [n][words], or null: row r sees nodes 0 .. r
+    const uint64_t *mask;  // [n][words], or null: row r sees nodes 0 .. row0 + r
     float *out;
     int64_t ld_out;
     float *part_o;    // [splits][n H][D] unnormalised outputs
     float2 *part_ml;  // [splits][n H]: (maximum, sum), in units of log2
     float scale;      // of the scores, times log2(e)
+    int32_t row0, nodes;  // the n rows are nodes row0 .. of that many
     int32_t n, words, prefix, n_heads, n_kv_heads, G, rows, q_tiles;  // rows = n G
     int32_t q_rows;                                                   // of a tile
     int32_t prefix_blocks, blocks, splits, per_split;                 // per_split: blocks of a share
@@ -65,7 +66,7 @@ __device__ __forceinline__ Block block_of(const TreeAttnArgs &a, int b) {
     } else {
         k.node0 = B * (b - a.prefix_blocks);
         k.first = a.prefix + k.node0;
-        k.len = min(B, a.n - k.node0);
+        k.len = min(B, a.nodes - k.node0);
     }
     return k;
 }
@@ -76,7 +77,7 @@ __device__ __forceinline__ uint64_t visible(const TreeAttnArgs &a, const Block &
         return all;
     if (a.mask)
         return (a.mask[(int64_t)node * a.words + (k.node0 >> 6)] >> (k.node0 & 63)) & all;
-    const int last = node - k.node0;
+    const int last = a.row0 + node - k.node0;
     return last < 0 ? 0 : (last >= 63 ? ~0ull : (2ull << last) - 1) & all;
 }
 
@@ -880,10 +881,12 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_tree_join(TreeAttnArgs a) {
 // 3001 keys, 32 heads).  float32: tiles of 16 rows, four work-groups per CU.
 constexpr int TA_GROUPS = 1024, TA_GROUPS_MFMA = 512, TA_GROUPS_FEW = 256, FEW_ROWS = 32;
 
-void plan(const sd_kv_layer *kv, int32_t n_heads, int32_t n, int32_t prefix, TreeAttnArgs *a) {
+void plan(const sd_kv_layer *kv, int32_t n_heads, int32_t n, int32_t nodes, int32_t prefix, TreeAttnArgs *a) {
     const bool bf16 = kv->dtype == SD_BF16;
     a->n = n;
-    a->words = (n + 63) / 64;
+    a->nodes = nodes;
+    a->row0 = nodes - n;
+    a->words = (nodes + 63) / 64;
     a->prefix = prefix;
     a->n_heads = n_heads;
     a->n_kv_heads = kv->n_kv_heads;
@@ -894,7 +897,7 @@ void plan(const sd_kv_layer *kv, int32_t n_heads, int32_t n, int32_t prefix, Tre
     a->q_tiles = (a->rows + a->q_rows - 1) / a->q_rows;
     const int kb = few ? KB_FEW : KB, step = few ? 4 : bf16 ? 1 : 2;  // step: blocks that a share has at least
     a->prefix_blocks = (prefix + kb - 1) / kb;
-    a->blocks = a->prefix_blocks + (n + kb - 1) / kb;
+    a->blocks = a->prefix_blocks + (nodes + kb - 1) / kb;
     const int units = a->q_tiles * a->n_kv_heads, groups = few ? TA_GROUPS_FEW : bf16 ? TA_GROUPS_MFMA : TA_GROUPS;
     const int want = std::max(1, std::min((a->blocks + step - 1) / step, (groups + units - 1) / units));
     a->per_split = ((a->blocks + want - 1) / want + step - 1) / step * step;
@@ -906,16 +909,16 @@ size_t workspace_of(const TreeAttnArgs &a, int D) {
     return a.splits == 1 ? 0 : o_bytes(a, D) + sizeof(float2) * (size_t)a.splits * a.n * a.n_heads;
 }
 
-sd_status check_sizes(const sd_kv_layer *kv, int32_t n_heads, int32_t n, int32_t prefix) {
+sd_status check_sizes(const sd_kv_layer *kv, int32_t n_heads, int32_t n, int32_t nodes, int32_t prefix) {
     const sd_status st = check_layer(kv);
     if (st != SD_OK)
         return st;
-    if (n < 1 || n > SD_TREE_MAX || n_heads < 1 || n_heads > 4096 || n_heads % kv->n_kv_heads)
+    if (n < 1 || nodes < n || nodes > SD_TREE_MAX || n_heads < 1 || n_heads > 4096 || n_heads % kv->n_kv_heads)
         return report(SD_ERR_INVALID_ARG, "a tree has 1 to " + std::to_string(SD_TREE_MAX) +
                                               " nodes; n_heads is a multiple of n_kv_heads, at most 4096");
-    if (prefix < 0 || (int64_t)prefix + n > kv->capacity)
+    if (prefix < 0 || (int64_t)prefix + nodes > kv->capacity)
         return report(SD_ERR_CAPACITY, "a layer of capacity " + std::to_string(kv->capacity) + " does not hold " +
-                                           std::to_string(n) + " nodes after " + std::to_string(prefix) +
+                                           std::to_string(nodes) + " nodes after " + std::to_string(prefix) +
                                            " positions");
     return SD_OK;
 }
@@ -947,10 +950,14 @@ void launch_mfma(const TreeAttnArgs &a, hipStream_t s) {
         hipLaunchKernelGGL((k_tree_attn_mfma<D, 4, 1>), grid, dim3(256), 0, s, a);
 }
 
+}  // namespace
+
+namespace sdk {
+
 sd_status tree_attention(const sd_kv_layer *kv, const float *q, int64_t ld_q, int32_t n_heads, int32_t n,
-                         int32_t prefix, const uint64_t *mask, float scale, float *out, int64_t ld_out,
+                         int32_t nodes, int32_t prefix, const uint64_t *mask, float scale, float *out, int64_t ld_out,
                          void *workspace, size_t workspace_bytes, hipStream_t s) {
-    const sd_status st = check_sizes(kv, n_heads, n, prefix);
+    const sd_status st = check_sizes(kv, n_heads, n, nodes, prefix);
     if (st != SD_OK)
         return st;
     const int D = kv->head_dim;
@@ -962,7 +969,7 @@ sd_status tree_attention(const sd_kv_layer *kv, const float *q, int64_t ld_q, in
     if (!std::isfinite(scale))
         return report(SD_ERR_INVALID_ARG, "scale must be finite");
     TreeAttnArgs a{};
-    plan(kv, n_heads, n, prefix, &a);
+    plan(kv, n_heads, n, nodes, prefix, &a);
     const size_t need = workspace_of(a, D);
     if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need))
         return report(SD_ERR_INVALID_ARG, "these sizes need " + std::to_string(need) +
@@ -1000,22 +1007,26 @@ sd_status tree_attention(const sd_kv_layer *kv, const float *q, int64_t ld_q, in
     return e == hipSuccess ? SD_OK : report(SD_ERR_DEVICE, std::string("tree attention: ") + hipGetErrorString(e));
 }
 
-}  // namespace
+size_t tree_attention_bytes(const sd_kv_layer *kv, int32_t n_heads, int32_t n, int32_t nodes, int32_t prefix) {
+    if (check_sizes(kv, n_heads, n, nodes, prefix) != SD_OK)
+        return 0;
+    TreeAttnArgs a{};
+    plan(kv, n_heads, n, nodes, prefix, &a);
+    return workspace_of(a, kv->head_dim);
+}
+
+}  // namespace sdk
 
 extern "C" {
 
 size_t sd_tree_attention_workspace(const sd_kv_layer *kv, int32_t n_heads, int32_t n, int32_t prefix) {
-    if (check_sizes(kv, n_heads, n, prefix) != SD_OK)
-        return 0;
-    TreeAttnArgs a{};
-    plan(kv, n_heads, n, prefix, &a);
-    return workspace_of(a, kv->head_dim);
+    return tree_attention_bytes(kv, n_heads, n, n, prefix);
 }
 
 sd_status sd_tree_attention(const sd_kv_layer *kv, const float *q, int64_t ld_q, int32_t n_heads, int32_t n,
                             int32_t prefix, const uint64_t *mask, float scale, float *out, int64_t ld_out,
                             void *workspace, size_t workspace_bytes, void *hip_stream) {
-    SD_GUARD(return tree_attention(kv, q, ld_q, n_heads, n, prefix, mask, scale, out, ld_out, workspace,
+    SD_GUARD(return tree_attention(kv, q, ld_q, n_heads, n, n, prefix, mask, scale, out, ld_out, workspace,
                                    workspace_bytes, reinterpret_cast<hipStream_t>(hip_stream));)
 }
 

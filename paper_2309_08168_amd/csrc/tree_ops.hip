@@ -43,6 +43,38 @@ sd_status launched(const char *what) {
 // loads are under way; a thread then handles units of eight elements: four pairs of a
 // rotated head, or eight elements that pass.
 
+struct RopeArgs {
+    // frequency of pair i: f = exp2(i * step), weighed for YARN, else times inv_factor
+    double step, inv_factor, turns, beta_slow, inv_beta;
+    float gain;
+    int32_t half, interleaved, yarn;  // half: pairs of a head
+    const float *qkv;
+    int64_t ld_qkv;
+    const int32_t *positions;
+    int32_t pos0, n, n_heads, n_kv_heads, head_dim;
+    float *q;
+    int64_t ld_q;
+    void *k, *v;
+    int64_t head_stride, row_stride;
+    int32_t slot;
+};
+
+// The rotary part of the arguments, for a checked form.
+void rope_form(const sd_rope &r, RopeArgs *out) {
+    double base = r.base;
+    if (r.scaling == SD_ROPE_NTK)
+        base *= std::pow(r.factor, (double)r.rotary_dim / (r.rotary_dim - 2));
+    out->step = -2.0 * std::log2(base) / r.rotary_dim;
+    out->yarn = r.scaling == SD_ROPE_YARN;
+    out->inv_factor = r.scaling == SD_ROPE_LINEAR || out->yarn ? 1.0 / r.factor : 1.0;
+    out->turns = r.original_context / 6.28318530717958647693;
+    out->beta_slow = r.beta_slow;
+    out->inv_beta = out->yarn ? 1.0 / (r.beta_fast - r.beta_slow) : 0.0;
+    out->gain = (float)rope_gain(r);
+    out->half = r.rotary_dim / 2;
+    out->interleaved = r.layout == SD_ROPE_INTERLEAVED;
+}
+
 __device__ __forceinline__ float2 rope_turn(const RopeArgs &a, int i, int pos) {
     double f = exp2(a.step * (double)i);
     if (a.yarn) {
@@ -363,9 +395,10 @@ sd_status rope_append(const sd_rope *rope, const float *qkv, int64_t ld_qkv, int
     if (st != SD_OK)
         return st;
     RopeArgs a{};
-    const sd_status rt = rope_form(rope, kv->head_dim, &a);
+    const sd_status rt = check_rope(rope, kv->head_dim);
     if (rt != SD_OK)
         return rt;
+    rope_form(*rope, &a);
     const int64_t D = kv->head_dim, KVH = kv->n_kv_heads;
     if (!qkv || !q_out || !aligned16(qkv) || !aligned16(q_out) || ((uintptr_t)positions & 3))
         return report(SD_ERR_INVALID_ARG, "qkv and q_out must be set and 16-byte aligned");
@@ -435,7 +468,7 @@ sd_status check_layer(const sd_kv_layer *kv) {
     return SD_OK;
 }
 
-sd_status rope_form(const sd_rope *r, int32_t head_dim, RopeArgs *out) {
+sd_status check_rope(const sd_rope *r, int32_t head_dim) {
     if (!r)
         return report(SD_ERR_INVALID_ARG, "rope is null");
     if (r->rotary_dim < 2 || r->rotary_dim % 2 || r->rotary_dim > head_dim)
@@ -453,19 +486,26 @@ sd_status rope_form(const sd_rope *r, int32_t head_dim, RopeArgs *out) {
     if (r->scaling == SD_ROPE_YARN && (!(r->beta_slow >= 0.0) || !(r->beta_fast > r->beta_slow) ||
                                        !std::isfinite(r->beta_fast) || r->original_context < 1))
         return report(SD_ERR_INVALID_ARG, "YARN needs beta_fast > beta_slow >= 0 and original_context >= 1");
-    double base = r->base;
-    if (r->scaling == SD_ROPE_NTK)
-        base *= std::pow(r->factor, (double)r->rotary_dim / (r->rotary_dim - 2));
-    out->step = -2.0 * std::log2(base) / r->rotary_dim;
-    out->yarn = r->scaling == SD_ROPE_YARN;
-    out->inv_factor = r->scaling == SD_ROPE_LINEAR || out->yarn ? 1.0 / r->factor : 1.0;
-    out->turns = r->original_context / 6.28318530717958647693;
-    out->beta_slow = r->beta_slow;
-    out->inv_beta = out->yarn ? 1.0 / (r->beta_fast - r->beta_slow) : 0.0;
-    out->gain = r->gain != 0.0 ? (float)r->gain : out->yarn ? (float)(0.1 * std::log(r->factor) + 1.0) : 1.0f;
-    out->half = r->rotary_dim / 2;
-    out->interleaved = r->layout == SD_ROPE_INTERLEAVED;
     return SD_OK;
+}
+
+double rope_frequency(const sd_rope &r, int32_t i) {
+    double base = r.base;
+    if (r.scaling == SD_ROPE_NTK)
+        base *= std::pow(r.factor, (double)r.rotary_dim / (r.rotary_dim - 2));
+    const double f = std::pow(base, -2.0 * (double)i / (double)r.rotary_dim);
+    if (r.scaling == SD_ROPE_LINEAR)
+        return f / r.factor;
+    if (r.scaling == SD_ROPE_YARN) {
+        const double turns = f * r.original_context / 6.28318530717958647693;
+        const double g = std::min(1.0, std::max(0.0, (turns - r.beta_slow) / (r.beta_fast - r.beta_slow)));
+        return f * (g + (1.0 - g) / r.factor);
+    }
+    return f;
+}
+
+double rope_gain(const sd_rope &r) {
+    return r.gain != 0.0 ? r.gain : r.scaling == SD_ROPE_YARN ? 0.1 * std::log(r.factor) + 1.0 : 1.0;
 }
 
 }  // namespace sdk

@@ -170,3 +170,12 @@ def test_tensor_shapes_types_and_strides_are_refused():
         with pytest.raises(binding.SDError) as e:
             bad()
         assert e.value.status == BAD
+
+
+def test_null_models_and_caches_are_refused():
+    lib, out = binding.load(), ctypes.c_int32()
+    assert lib.sd_forward_tree(None, P, P, 3, None, P, None) == BAD
+    assert lib.sd_verify_tree(None, P, P, 3, P, P, ctypes.byref(out), ctypes.byref(out)) == BAD
+    assert lib.sd_kv_cache_keep(None, P, 1) == BAD
+    assert lib.sd_model_set_rope(None, None) == BAD
+    assert b"model" in lib.sd_last_error()
