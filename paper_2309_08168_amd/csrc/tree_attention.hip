@@ -286,6 +286,21 @@ __device__ __forceinline__ void terms2(float a, float b, uint32_t (&t)[X_TERMS])
     t[2] = cvt_pk(a1 - __uint_as_float(t[1] << 16), b1 - __uint_as_float(t[1] & 0xffff0000u));
 }
 
+// The terms of eight values as MFMA operands.
+__device__ __forceinline__ void query_terms(f32x4_t x0, f32x4_t x1, u32x4_t (&q)[X_TERMS]) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        uint32_t t0[X_TERMS], t1[X_TERMS];
+        terms2(x0[2 * j], x0[2 * j + 1], t0);
+        terms2(x1[2 * j], x1[2 * j + 1], t1);
+#pragma unroll
+        for (int i = 0; i < X_TERMS; ++i) {
+            q[i][j] = t0[i];
+            q[i][2 + j] = t1[i];
+        }
+    }
+}
+
 // Sixteen bytes per lane from g to LDS at l + 16 lane (l the same in every lane).
 // The compiler does not see these loads; the kernel waits for them itself.  They
 // have no register result; M0 holds the LDS address and needs one wait state.
@@ -338,28 +353,23 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_tree_attn_mfma(TreeAttnArgs
             load_to_lds16((m ? V : K) + (int64_t)(k.first + r) * a.row_stride + 8 * (p % L::C), &kv[buf][m][u * 512]);
         }
     };
-    load_block(b0, 0);
-
-    u32x4_t qf[ES][T];
+    // The queries are asked for before the first block: loads return in order
+    // (100 rows over 2000 keys, 40 heads: 27.2 -> 26.4 us).
+    f32x4_t qx[ES][2];
     {
         const float *qs = a.q + (int64_t)node * a.ld_q + (int64_t)head * D + 8 * half;
 #pragma unroll
         for (int s = 0; s < ES; ++s) {
-            const f32x4_t x0 = *reinterpret_cast<const f32x4_t *>(qs + 16 * s) * a.scale,
-                          x1 = *reinterpret_cast<const f32x4_t *>(qs + 16 * s + 4) * a.scale;
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                uint32_t t0[T], t1[T];
-                terms2(x0[2 * j], x0[2 * j + 1], t0);
-                terms2(x1[2 * j], x1[2 * j + 1], t1);
-#pragma unroll
-                for (int i = 0; i < T; ++i) {
-                    qf[s][i][j] = t0[i];
-                    qf[s][i][2 + j] = t1[i];
-                }
-            }
+            qx[s][0] = load4(qs + 16 * s);
+            qx[s][1] = load4(qs + 16 * s + 4);
         }
     }
+    __builtin_amdgcn_sched_barrier(0);
+    load_block(b0, 0);
+    u32x4_t qf[ES][T];
+#pragma unroll
+    for (int s = 0; s < ES; ++s)
+        query_terms(qx[s][0] * a.scale, qx[s][1] * a.scale, qf[s]);
     // V^T reads: ds_read_b64_tr_b16 hands lane l of each 16-lane group element
     // l % 4 of the 8 bytes that lanes l / 4 + 4 k (k = 0..3) point at, so lane l
     // points at row 4 half + l / 4 % 4, columns 16 (l / 16 % 2) + 4 (l % 4) ...
@@ -648,25 +658,12 @@ __global__ __launch_bounds__(256, QT == 1 || D < 128 ? 2 : 1) void k_tree_attn_f
         const int row = min(r0 + 16 * i + col, a.rows - 1);
         node[i] = row / a.G;
         const float *qs = a.q + (int64_t)node[i] * a.ld_q + (int64_t)(g * a.G + row - node[i] * a.G) * D + (8 * grp) % D;
-        const float scale = D < 32 && grp >= 2 ? 0.0f : a.scale;
 #pragma unroll
         for (int s = 0; s < ES; ++s) {
-            f32x4_t x0 = load4(qs + 32 * s), x1 = load4(qs + 32 * s + 4);
-            if (D < 32 && grp >= 2)  // (0 times an infinity is none)
+            f32x4_t x0 = load4(qs + 32 * s) * a.scale, x1 = load4(qs + 32 * s + 4) * a.scale;
+            if (D < 32 && grp >= 2)  // head_dim 16: the upper half of the reduction
                 x0 = x1 = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-            x0 *= scale;
-            x1 *= scale;
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                uint32_t t0[T], t1[T];
-                terms2(x0[2 * j], x0[2 * j + 1], t0);
-                terms2(x1[2 * j], x1[2 * j + 1], t1);
-#pragma unroll
-                for (int w = 0; w < T; ++w) {
-                    qf[i][s][w][j] = t0[w];
-                    qf[i][s][w][2 + j] = t1[w];
-                }
-            }
+            query_terms(x0, x1, qf[i][s]);
         }
     }
     float m_run[QT], l_run[QT];
@@ -873,13 +870,35 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_tree_join(TreeAttnArgs a) {
         total == 0.0f ? f32x4_t{0.0f, 0.0f, 0.0f, 0.0f} : O / total;
 }
 
-// Rows of a tile and shares of the keys.  bfloat16: up to 32 rows on the kernel
-// for few, one work-group per CU (13 rows over 1200 keys, 40 heads: 10.3 us, 11.3
-// with two, which halves the keys of a share; one row over 60000 keys, 8
-// heads: 43 and 46); else tiles of 64, 96 or 128 rows, the fewest that hold a kv
-// head's rows, in two work-groups per CU (three: 24 -> 28 us for 61 rows over
-// 3001 keys, 32 heads).  float32: tiles of 16 rows, four work-groups per CU.
-constexpr int TA_GROUPS = 1024, TA_GROUPS_MFMA = 512, TA_GROUPS_FEW = 256, FEW_ROWS = 32;
+// Rows of a tile and shares of the keys.
+//   float32: tiles of 16 rows, four work-groups per CU, two blocks a share at least.
+//   bfloat16, up to 32 rows of a kv head: the kernel for few, one work-group per
+//   CU (13 rows over 1200 keys, 40 heads: 10.3 us, 11.3 with two, which halves
+//   the keys of a share; one row over 60000 keys, 8 heads: 43 and 46).
+//   More rows: tiles of 64, 96 or 128, the fewest that hold a kv head's rows, and
+//   one or two work-groups per CU (mfma_shares).
+constexpr int TA_GROUPS = 1024, TA_GROUPS_FEW = 256, TA_CUS = 256, FEW_ROWS = 32;
+
+// Two work-groups per CU hide a part of each other's softmax, about a seventh of
+// a long share; every work-group costs its start, its end and its part of the
+// join, about two blocks' time.  us, kernel and join, one and two per CU: 61
+// rows over 3001 keys (32 heads, 6 and 3 blocks a share) 26.3 and 27.4; 64 over
+// 8000 (8 heads, 4 and 2) 20.9 and 24.6; 512 over 16000 (8 heads, 32 and 16) 127
+// and 118.  Three per CU do not fit.
+int mfma_shares(int units, int blocks) {
+    int best = 1;
+    double least = INFINITY;
+    for (int groups = TA_CUS; groups <= 2 * TA_CUS; groups += TA_CUS) {
+        const int shares = std::max(1, std::min(blocks, groups / units));
+        const int per = (blocks + shares - 1) / shares, w = (units * shares + TA_CUS - 1) / TA_CUS;
+        const double cost = w * (per * (w == 1 ? 7.0 / 6.0 : 1.0) + 2.0);
+        if (cost < least) {
+            least = cost;
+            best = shares;
+        }
+    }
+    return best;
+}
 
 void plan(const sd_kv_layer *kv, int32_t n_heads, int32_t n, int32_t nodes, int32_t prefix, TreeAttnArgs *a) {
     const bool bf16 = kv->dtype == SD_BF16;
@@ -898,8 +917,9 @@ void plan(const sd_kv_layer *kv, int32_t n_heads, int32_t n, int32_t nodes, int3
     const int kb = few ? KB_FEW : KB, step = few ? 4 : bf16 ? 1 : 2;  // step: blocks that a share has at least
     a->prefix_blocks = (prefix + kb - 1) / kb;
     a->blocks = a->prefix_blocks + (nodes + kb - 1) / kb;
-    const int units = a->q_tiles * a->n_kv_heads, groups = few ? TA_GROUPS_FEW : bf16 ? TA_GROUPS_MFMA : TA_GROUPS;
-    const int want = std::max(1, std::min((a->blocks + step - 1) / step, (groups + units - 1) / units));
+    const int units = a->q_tiles * a->n_kv_heads, groups = few ? TA_GROUPS_FEW : TA_GROUPS;
+    const int want = bf16 && !few ? mfma_shares(units, a->blocks)
+                                  : std::max(1, std::min((a->blocks + step - 1) / step, (groups + units - 1) / units));
     a->per_split = ((a->blocks + want - 1) / want + step - 1) / step * step;
     a->splits = (a->blocks + a->per_split - 1) / a->per_split;
 }
