@@ -195,16 +195,12 @@ __global__ __launch_bounds__(ROPE_THREADS) void k_rope_append(RopeArgs a) {
 constexpr int ACC_THREADS = 256;
 constexpr int WALK_THREADS = 1024;
 
-// An order-preserving code of a float, high for large; NaN below everything.
-__device__ __forceinline__ uint32_t float_order(float x) {
-    const uint32_t u = __float_as_uint(x == 0.0f ? 0.0f : x);  // the zeros are equal
-    if (x != x)
-        return 0u;
-    return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-}
+// A (logit, id) pair as a key that orders like it: larger logits above, then
+// lower ids; 0 is below every pair.  (The zeros are equal.)
 __device__ __forceinline__ uint64_t best_key(float x, int id) {
-    const uint32_t o = float_order(x);
-    return o ? ((uint64_t)o << 32) | (uint32_t)(0x7fffffff - id) : 0ull;
+    const uint32_t u = __float_as_uint(x == 0.0f ? 0.0f : x);
+    const uint32_t o = (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+    return ((uint64_t)o << 32) | (uint32_t)(0x7fffffff - id);
 }
 __device__ __forceinline__ uint64_t max64(uint64_t a, uint64_t b) { return a > b ? a : b; }
 
@@ -226,35 +222,74 @@ struct AcceptArgs {
     int32_t vocab, n, slices, slice;
 };
 
+// A thread's ids ascend, so a logit wins only where it is larger than the one
+// before, which a NaN never is: a comparison and two selects a logit.  Four
+// loads of a thread are in flight (a load at a time: 21.3 us for 700 rows of
+// 32000, 4.2 TB/s).  A slice without a logit above minus infinity, which no
+// thread then reports, is looked through once more for its first one.
+constexpr int BEST_LOADS = 4;
 __global__ __launch_bounds__(ACC_THREADS) void k_row_best(AcceptArgs a) {
     __shared__ uint64_t red[ACC_THREADS / 64];
     const int r = blockIdx.y, tid = threadIdx.x;
     const int i0 = blockIdx.x * a.slice, i1 = min(a.vocab, i0 + a.slice);
     const float *x = a.logits + (int64_t)r * a.ld;
-    uint64_t best = 0;
+    float top = -INFINITY;
+    int id = -1;
+    auto take = [&](float v, int i) {
+        const bool wins = v > top;
+        top = wins ? v : top;
+        id = wins ? i : id;
+    };
     // (the head and the tail that are not whole 16-byte words one by one)
     const int lead = min(i1 - i0, (int)((4 - (((uintptr_t)(x + i0) >> 2) & 3)) & 3));
     if (tid < lead)
-        best = best_key(x[i0 + tid], i0 + tid);
+        take(x[i0 + tid], i0 + tid);
     const int w0 = i0 + lead, words = (i1 - w0) / 4, tail = w0 + 4 * words;
-    for (int w = tid; w < words; w += ACC_THREADS) {
-        const f32x4_t v = __builtin_nontemporal_load(reinterpret_cast<const f32x4_t *>(x + w0) + w);
+    const f32x4_t *xw = reinterpret_cast<const f32x4_t *>(x + w0);
+    int w = tid;
+    for (; w + (BEST_LOADS - 1) * ACC_THREADS < words; w += BEST_LOADS * ACC_THREADS) {
+        f32x4_t v[BEST_LOADS];
+#pragma unroll
+        for (int u = 0; u < BEST_LOADS; ++u)
+            v[u] = __builtin_nontemporal_load(xw + w + u * ACC_THREADS);
+#pragma unroll
+        for (int u = 0; u < BEST_LOADS; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                take(v[u][j], w0 + 4 * (w + u * ACC_THREADS) + j);
+    }
+    for (; w < words; w += ACC_THREADS) {
+        const f32x4_t v = __builtin_nontemporal_load(xw + w);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            best = max64(best, best_key(v[j], w0 + 4 * w + j));
+            take(v[j], w0 + 4 * w + j);
     }
     if (tid < i1 - tail)
-        best = max64(best, best_key(x[tail + tid], tail + tid));
-    best = wave_max64(best);
+        take(x[tail + tid], tail + tid);
+    uint64_t best = wave_max64(id >= 0 ? best_key(top, id) : 0);
     if ((tid & 63) == 0)
         red[tid >> 6] = best;
     __syncthreads();
-    if (tid == 0) {
+    best = red[0];
 #pragma unroll
-        for (int w = 1; w < ACC_THREADS / 64; ++w)
-            best = max64(best, red[w]);
-        a.keys[(int64_t)r * a.slices + blockIdx.x] = best;
+    for (int v = 1; v < ACC_THREADS / 64; ++v)
+        best = max64(best, red[v]);
+    if (best == 0) {  // uniform
+        for (int i = i0 + tid; i < i1 && id < 0; i += ACC_THREADS)
+            if (x[i] == -INFINITY)
+                id = i;
+        best = wave_max64(id >= 0 ? best_key(-INFINITY, id) : 0);
+        __syncthreads();
+        if ((tid & 63) == 0)
+            red[tid >> 6] = best;
+        __syncthreads();
+        best = red[0];
+#pragma unroll
+        for (int v = 1; v < ACC_THREADS / 64; ++v)
+            best = max64(best, red[v]);
     }
+    if (tid == 0)
+        a.keys[(int64_t)r * a.slices + blockIdx.x] = best;
 }
 
 // One work-group, a thread per node: best tokens, then the lowest matching child
@@ -326,29 +361,35 @@ constexpr int KEEP_WORDS = 4;  // 16-byte words in flight per lane
 
 __global__ __launch_bounds__(KEEP_THREADS) void k_kv_keep(KeepArgs a) {
     __shared__ int32_t path[SD_TREE_MAX];
-    __shared__ int32_t bad;
+    __shared__ int32_t first;  // of the path's rows that move
     const int tid = threadIdx.x, lane = tid & 63;
-    const int count = a.walk[0];
-    if (count < 1 || count > a.n)
-        return;  // uniform
+    // the count and the path in one round trip
     if (tid == 0)
-        bad = 0;
-    for (int i = tid; i < count; i += KEEP_THREADS)
-        path[i] = a.walk[2 + i];
-    __syncthreads();
-    for (int i = tid; i < count; i += KEEP_THREADS)
-        if (path[i] < 0 || path[i] >= a.n || (i > 0 && path[i] <= path[i - 1]))
-            bad = 1;
-    __syncthreads();
+        first = a.n;
+    const int count = a.walk[0];
+    bool bad = count < 1 || count > a.n;
+    int below = -1;
+    for (int i = tid; i < a.n; i += KEEP_THREADS) {
+        const int p = a.walk[2 + i], before = i > 0 ? a.walk[1 + i] : -1;
+        path[i] = p;
+        bad |= i < count && (p < 0 || p >= a.n || (i > 0 && p <= before));
+        if (i < count && p != i && below < 0)
+            below = i;
+    }
+    bad = __syncthreads_or(bad);
     if (bad)
         return;  // uniform
+    if (below >= 0)
+        atomicMin(&first, below);
+    __syncthreads();
     const int64_t plane = (int64_t)blockIdx.x * (KEEP_THREADS / 64) + (tid >> 6);
     if (plane >= a.planes)
         return;
     char *rows = a.kv + plane * a.plane_stride + (int64_t)a.base * a.row_bytes;
     const int wpr = a.row_bytes >> 4;
+    // the path leaves its nodes' numbers once: the rows before stay where they are
     const int words = count * wpr;
-    for (int w0 = 0; w0 < words; w0 += 64 * KEEP_WORDS) {
+    for (int w0 = first * wpr; w0 < words; w0 += 64 * KEEP_WORDS) {
         u32x4_t v[KEEP_WORDS];
 #pragma unroll
         for (int j = 0; j < KEEP_WORDS; ++j) {
@@ -361,7 +402,7 @@ __global__ __launch_bounds__(KEEP_THREADS) void k_kv_keep(KeepArgs a) {
 #pragma unroll
         for (int j = 0; j < KEEP_WORDS; ++j) {
             const int w = w0 + 64 * j + lane, i = w / wpr;
-            if (w < words && path[i] != i)
+            if (w < words)
                 *reinterpret_cast<u32x4_t *>(rows + (int64_t)i * a.row_bytes + 16 * (w - i * wpr)) = v[j];
         }
     }
