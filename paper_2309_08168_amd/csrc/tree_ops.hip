@@ -97,6 +97,7 @@ __device__ __forceinline__ float2 rope_turn(const RopeArgs &a, int i, int pos) {
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), bf16x2_t));
 }
+__device__ __forceinline__ f32x4_t load4(const float *p) { return *reinterpret_cast<const f32x4_t *>(p); }
 __device__ __forceinline__ void store4(float *p, f32x4_t x) { *reinterpret_cast<f32x4_t *>(p) = x; }
 __device__ __forceinline__ void store4(uint16_t *p, f32x4_t x) {
     *reinterpret_cast<u32x2_t *>(p) = u32x2_t{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
@@ -115,12 +116,31 @@ __global__ __launch_bounds__(ROPE_THREADS) void k_rope_append(RopeArgs a) {
     const int per = UNITS ? D / 8 : D, units = (H + 2 * KVH) * per;
     const int stride = gridDim.y * ROPE_THREADS;
     const float *x = a.qkv + (int64_t)r * a.ld_qkv;
+    const int u0 = blockIdx.y * ROPE_THREADS + threadIdx.x;
+    // unit w of a head: its two groups of four elements
+    auto first_of = [&](int head, int w, int &e1) {
+        if (head < H + KVH && 8 * w < R && !a.interleaved) {
+            e1 = 4 * w + a.half;
+            return 4 * w;
+        }
+        e1 = 8 * w + 4;
+        return 8 * w;
+    };
+    f32x4_t p = {}, q = {};
+    auto load = [&](int u) {
+        const int head = u / per, w = u - head * per;
+        int e1;
+        const int e0 = first_of(head, w, e1);
+        p = load4(x + (int64_t)head * D + e0);
+        q = load4(x + (int64_t)head * D + e1);
+    };
+    if (UNITS && u0 < units)
+        load(u0);
     if ((int)threadIdx.x < a.half)
         turn[threadIdx.x] = rope_turn(a, threadIdx.x, a.positions ? a.positions[r] : a.pos0 + r);
     __syncthreads();
-    for (int u = blockIdx.y * ROPE_THREADS + threadIdx.x; u < units; u += stride) {
+    for (int u = u0; u < units; u += stride) {
         const int head = u / per, w = u - head * per;
-        const float *xh = x + (int64_t)head * D;
         // where the head goes: queries to q, keys and values to the cache row
         float *qh = head < H ? a.q + (int64_t)r * a.ld_q + (int64_t)head * D : nullptr;
         TK *ch = nullptr;
@@ -131,18 +151,13 @@ __global__ __launch_bounds__(ROPE_THREADS) void k_rope_append(RopeArgs a) {
         }
         const bool turned = head < H + KVH;
         if constexpr (UNITS) {
-            int e0 = 8 * w, e1 = e0 + 4;
-            const bool rot = turned && e0 < R;
-            if (rot && !a.interleaved) {
-                e0 = 4 * w;
-                e1 = e0 + a.half;
-            }
-            f32x4_t p = *reinterpret_cast<const f32x4_t *>(xh + e0), q = *reinterpret_cast<const f32x4_t *>(xh + e1);
-            if (rot) {
+            int e1;
+            const int e0 = first_of(head, w, e1);
+            f32x4_t np = p, nq = q;
+            if (turned && 8 * w < R) {
                 const f32x4_t t0 = *reinterpret_cast<const f32x4_t *>(turn + 4 * w),
                               t1 = *reinterpret_cast<const f32x4_t *>(turn + 4 * w + 2);
                 const float c[4] = {t0[0], t0[2], t1[0], t1[2]}, s[4] = {t0[1], t0[3], t1[1], t1[3]};
-                f32x4_t np, nq;
                 if (a.interleaved) {
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
@@ -158,17 +173,18 @@ __global__ __launch_bounds__(ROPE_THREADS) void k_rope_append(RopeArgs a) {
                         nq[j] = q[j] * c[j] + p[j] * s[j];
                     }
                 }
-                p = np;
-                q = nq;
             }
+            if (u + stride < units)
+                load(u + stride);
             if (qh) {
-                store4(qh + e0, p);
-                store4(qh + e1, q);
+                store4(qh + e0, np);
+                store4(qh + e1, nq);
             } else {
-                store4(ch + e0, p);
-                store4(ch + e1, q);
+                store4(ch + e0, np);
+                store4(ch + e1, nq);
             }
         } else {
+            const float *xh = x + (int64_t)head * D;
             float y = xh[w];
             if (turned && w < R) {
                 const bool second = a.interleaved ? (w & 1) : w >= a.half;
