@@ -486,20 +486,26 @@ def _refuse(message: str):
     raise SDError(SD_ERR_INVALID_ARG, message)
 
 
-_torch = None      # looked up once: the operators run for a few microseconds, and an
-_raw_stream = None  # import statement or a Stream object costs one or two of them
-_DTYPES: Dict = {}  # torch dtypes of a cache
+# The operators run for a few microseconds, so their calls are short: torch, its
+# types and its stream are looked up once, and a tensor's attributes read once.
+_torch = _f32 = _bf16 = _i32 = _raw_stream = _current = None
 
 
 def _use_torch():
-    global _torch, _raw_stream
-    if _torch is None:
-        import torch
+    global _torch, _f32, _bf16, _i32, _raw_stream, _current
+    import torch
 
-        _DTYPES.update({torch.float32: SD_F32, torch.bfloat16: SD_BF16})
-        _raw_stream = torch._C._cuda_getCurrentRawStream  # (device index) -> hipStream_t
-        _torch = torch
-    return _torch
+    _f32, _bf16, _i32 = torch.float32, torch.bfloat16, torch.int32
+    _raw_stream = torch._C._cuda_getCurrentRawStream  # (device index) -> hipStream_t
+    _current = torch.cuda.current_device
+    load()
+    _torch = torch
+
+
+def _elsewhere(dev: int, fn, *args):
+    """fn(*args) with the GPU dev, which is not the current one, current."""
+    with _torch.cuda.device(dev):
+        return fn(*args)
 
 
 def _device(t, *others) -> int:
@@ -508,77 +514,85 @@ def _device(t, *others) -> int:
     if dev < 0:
         _refuse("the operators take tensors on a GPU")
     for o in others:
-        if o is not None and o.get_device() != dev:
+        if o.get_device() != dev:
             _refuse("the tensors are on different devices")
     return dev
 
 
-def _call(dev: int, fn, *args):
-    """fn(..., stream) on the current stream of GPU dev, with that GPU current."""
-    if dev == _torch.cuda.current_device():
-        status = fn(*args, _raw_stream(dev))
-    else:
-        with _torch.cuda.device(dev):
-            status = fn(*args, _raw_stream(dev))
-    if status != SD_OK:
-        check(status)
+def _layer(k, v):
+    """(sd_kv_layer, n_kv_heads, head_dim) of two tensors."""
+    if _torch is None:
+        _use_torch()
+    dtype, shape, stride = k.dtype, k.shape, k.stride()
+    if (dtype is not _bf16 and dtype is not _f32) or len(shape) != 3 or stride[2] != 1 or v.dtype is not dtype or \
+            v.shape != shape or v.stride() != stride:
+        _refuse("k and v are [n_kv_heads, capacity, head_dim], float32 or bfloat16, of one type and one set of strides, "
+                "rows contiguous")
+    heads, cap, d = shape
+    return sd_kv_layer(k.data_ptr(), v.data_ptr(), stride[0], stride[1], heads, cap, d,
+                       SD_BF16 if dtype is _bf16 else SD_F32), heads, d
 
 
 def kv_layer(k, v) -> sd_kv_layer:
     """sd_kv_layer over tensors [n_kv_heads, capacity, head_dim] (float32 or
     bfloat16, elements of a row adjacent, the same strides)."""
-    _use_torch()
-    dtype = _DTYPES.get(k.dtype)
-    shape, stride = k.shape, k.stride()
-    if dtype is None or len(shape) != 3 or stride[2] != 1 or v.dtype != k.dtype or v.shape != shape or \
-            v.stride() != stride:
-        _refuse("k and v are [n_kv_heads, capacity, head_dim], float32 or bfloat16, of one type and one set of strides, "
-                "rows contiguous")
-    return sd_kv_layer(k.data_ptr(), v.data_ptr(), stride[0], stride[1], shape[0], shape[1], shape[2], dtype)
+    return _layer(k, v)[0]
 
 
-def _rows(t, shape, what: str) -> int:
-    """Row stride of a float32 tensor of that shape whose rows are contiguous."""
-    if t.dtype != _torch.float32 or t.shape != shape:
-        _refuse(f"{what} is float32 {list(shape)}")
-    stride, want = t.stride(), 1
-    for i in range(len(shape) - 1, 0, -1):
-        if stride[i] != want and shape[i] != 1:
-            _refuse(f"the rows of {what} are contiguous")
-        want *= shape[i]
-    return stride[0] if shape[0] > 1 else want
+def _rows3(t, n: int, h: int, d: int, what: str) -> int:
+    """Row stride of a float32 tensor [n, h, d] whose rows are contiguous."""
+    stride = t.stride()
+    if t.dtype is not _f32 or t.shape != (n, h, d) or stride[2] != 1 or (stride[1] != d and h > 1):
+        _refuse(f"{what} is float32 [{n}, {h}, {d}], its rows contiguous")
+    return stride[0] if n > 1 else h * d
 
 
-def _words(t, shape, what: str) -> int:
-    """Address of a contiguous int32 tensor of that shape."""
-    if t.dtype != _torch.int32 or t.shape != shape or not t.is_contiguous():
-        _refuse(f"{what} is a contiguous int32 {list(shape)}")
+def _rows2(t, n: int, m: int, what: str) -> int:
+    """The same of [n, m]."""
+    stride = t.stride()
+    if t.dtype is not _f32 or t.shape != (n, m) or (stride[1] != 1 and m > 1):
+        _refuse(f"{what} is float32 [{n}, {m}], its rows contiguous")
+    return stride[0] if n > 1 else m
+
+
+def _words(t, n: int, what: str) -> int:
+    """Address of a contiguous int32 tensor [n]."""
+    if t.dtype is not _i32 or t.shape != (n,) or not t.is_contiguous():
+        _refuse(f"{what} is a contiguous int32 [{n}]")
     return t.data_ptr()
 
 
-def _space(workspace, nbytes: int, like):
-    """(tensor, bytes): the caller's workspace, or one of nbytes on the current stream."""
-    if workspace is None:
-        return like.new_empty(nbytes, dtype=_torch.uint8) if nbytes else None, nbytes
+def _space(workspace, like):
+    """(address, bytes) of a caller's workspace."""
     if not workspace.is_contiguous():
         _refuse("workspace is contiguous")
-    return workspace, workspace.numel() * workspace.element_size()
+    _device(like, workspace)
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 def rope_append(form: sd_rope, qkv, k, v, slot: int, n_heads: int, positions=None, pos0: int = 0, q_out=None):
     """sd_rope_append: qkv float32 [n, (n_heads + 2 n_kv_heads) head_dim], k and v
     as in kv_layer, rows stored at slot ..; positions int32 [n] or None: pos0 ..
     Returns the rotated queries, float32 [n, n_heads, head_dim]."""
-    layer = kv_layer(k, v)
-    n, d = qkv.shape[0], layer.head_dim
-    ld = _rows(qkv, (n, (n_heads + 2 * layer.n_kv_heads) * d), "qkv")
-    shape = (n, n_heads, d)
+    layer, kvh, d = _layer(k, v)
+    n = qkv.shape[0]
+    ld = _rows2(qkv, n, (n_heads + 2 * kvh) * d, "qkv")
+    dev = _device(qkv, k, v)
+    if dev != _current():
+        return _elsewhere(dev, rope_append, form, qkv, k, v, slot, n_heads, positions, pos0, q_out)
+    at = None
+    if positions is not None:
+        at = _words(positions, n, "positions")
+        _device(qkv, positions)
     if q_out is None:
-        q_out, ldq = qkv.new_empty(shape), n_heads * d
+        q_out, ldq = qkv.new_empty((n, n_heads, d)), n_heads * d
     else:
-        ldq = _rows(q_out, shape, "q_out")
-    _call(_device(qkv, k, v, positions, q_out), load().sd_rope_append, form, qkv.data_ptr(), ld, n, n_heads,
-          None if positions is None else _words(positions, (n,), "positions"), pos0, q_out.data_ptr(), ldq, layer, slot)
+        ldq = _rows3(q_out, n, n_heads, d, "q_out")
+        _device(qkv, q_out)
+    status = _lib.sd_rope_append(form, qkv.data_ptr(), ld, n, n_heads, at, pos0, q_out.data_ptr(), ldq, layer, slot,
+                                 _raw_stream(dev))
+    if status:
+        check(status)
     return q_out
 
 
@@ -587,25 +601,37 @@ def tree_attention(q, k, v, prefix: int, mask=None, scale: float = 0.0, out=None
     kv_layer, mask int64 or uint64 [n, (n + 63) // 64] or None (row r sees nodes
     0 .. r), scale 0: 1 / sqrt(head_dim).  Returns out, like q; workspace: a tensor of
     at least tree_attention_workspace() bytes (else one is allocated)."""
-    layer, lib = kv_layer(k, v), load()
-    n, h, d = shape = q.shape
-    if d != layer.head_dim:
-        _refuse("q and the layer have one head_dim")
-    ld = _rows(q, shape, "q")
-    if mask is None:
-        bits = None
-    else:
-        if mask.dtype not in (_torch.int64, _torch.uint64) or mask.shape != (n, (n + 63) // 64) or \
+    layer, _, d = _layer(k, v)
+    shape = q.shape
+    if len(shape) != 3:
+        _refuse("q is [n, n_heads, head_dim]")
+    n, h, _ = shape
+    ld = _rows3(q, n, h, d, "q")
+    dev = _device(q, k, v)
+    if dev != _current():
+        return _elsewhere(dev, tree_attention, q, k, v, prefix, mask, scale, out, workspace)
+    bits = None
+    if mask is not None:
+        if mask.element_size() != 8 or mask.is_floating_point() or mask.shape != (n, (n + 63) >> 6) or \
                 not mask.is_contiguous():
             _refuse("mask is a contiguous int64 or uint64 [n, (n + 63) // 64]")
+        _device(q, mask)
         bits = mask.data_ptr()
     if out is None:
         out, ldo = q.new_empty(shape), h * d
     else:
-        ldo = _rows(out, shape, "out")
-    ws, nbytes = _space(workspace, lib.sd_tree_attention_workspace(layer, h, n, prefix), q)
-    _call(_device(q, k, v, mask, out, ws), lib.sd_tree_attention, layer, q.data_ptr(), ld, h, n, prefix, bits, scale,
-          out.data_ptr(), ldo, None if ws is None else ws.data_ptr(), nbytes)
+        ldo = _rows3(out, n, h, d, "out")
+        _device(q, out)
+    if workspace is None:
+        nbytes = _lib.sd_tree_attention_workspace(layer, h, n, prefix)
+        ws = q.new_empty((nbytes + 3) >> 2) if nbytes else None
+        at = ws.data_ptr() if nbytes else None
+    else:
+        at, nbytes = _space(workspace, q)
+    status = _lib.sd_tree_attention(layer, q.data_ptr(), ld, h, n, prefix, bits, scale, out.data_ptr(), ldo, at, nbytes,
+                                    _raw_stream(dev))
+    if status:
+        check(status)
     return out
 
 
@@ -619,16 +645,32 @@ def tree_accept(logits, tokens, parents, walk=None, workspace=None):
     Returns walk, int32 [2 + 2 n]: nodes on the path, the next token, the path
     (then -1), each node's best token; workspace: a tensor of at least
     tree_accept_workspace() bytes (else one is allocated)."""
-    _use_torch()
-    lib = load()
-    n, vocab = shape = logits.shape
-    ld = _rows(logits, shape, "logits")
+    if _torch is None:
+        _use_torch()
+    shape = logits.shape
+    if len(shape) != 2:
+        _refuse("logits is [n, vocab]")
+    n, vocab = shape
+    ld = _rows2(logits, n, vocab, "logits")
+    tok, par = _words(tokens, n, "tokens"), _words(parents, n, "parents")
+    dev = _device(logits, tokens, parents)
+    if dev != _current():
+        return _elsewhere(dev, tree_accept, logits, tokens, parents, walk, workspace)
     if walk is None:
         walk = tokens.new_empty(2 + 2 * n)
-    ws, nbytes = _space(workspace, lib.sd_tree_accept_workspace(n, vocab), logits)
-    _call(_device(logits, tokens, parents, walk, ws), lib.sd_tree_accept, logits.data_ptr(), ld, vocab,
-          _words(tokens, (n,), "tokens"), _words(parents, (n,), "parents"), n, _words(walk, (2 + 2 * n,), "walk"),
-          None if ws is None else ws.data_ptr(), nbytes)
+        out = walk.data_ptr()
+    else:
+        out = _words(walk, 2 + 2 * n, "walk")
+        _device(logits, walk)
+    if workspace is None:
+        nbytes = _lib.sd_tree_accept_workspace(n, vocab)
+        ws = logits.new_empty((nbytes + 3) >> 2) if nbytes else None
+        at = ws.data_ptr() if nbytes else None
+    else:
+        at, nbytes = _space(workspace, logits)
+    status = _lib.sd_tree_accept(logits.data_ptr(), ld, vocab, tok, par, n, out, at, nbytes, _raw_stream(dev))
+    if status:
+        check(status)
     return walk
 
 
@@ -640,15 +682,21 @@ def tree_accept_workspace(n: int, vocab: int) -> int:
 def kv_keep(kv, base: int, walk):
     """sd_kv_keep over a contiguous tensor [..., capacity, head_dim] (every plane
     of a cache), with a walk of tree_accept; returns kv."""
-    _use_torch()
+    if _torch is None:
+        _use_torch()
     shape = kv.shape
     if len(shape) < 2 or not kv.is_contiguous():
         _refuse("kv is a contiguous [..., capacity, head_dim]")
-    n = (walk.numel() - 2) // 2
-    at = _words(walk, (2 + 2 * n,), "walk")
+    n = (walk.numel() - 2) >> 1
+    at = _words(walk, 2 + 2 * n, "walk")
+    dev = _device(kv, walk)
+    if dev != _current():
+        return _elsewhere(dev, kv_keep, kv, base, walk)
     cap, row = shape[-2], shape[-1] * kv.element_size()
-    _call(_device(kv, walk), load().sd_kv_keep, kv.data_ptr(), kv.numel() // max(cap * shape[-1], 1), cap * row, row, cap,
-          base, at, n)
+    planes = kv.numel() // (cap * shape[-1]) if kv.numel() else 0
+    status = _lib.sd_kv_keep(kv.data_ptr(), planes, cap * row, row, cap, base, at, n, _raw_stream(dev))
+    if status:
+        check(status)
     return kv
 
 
