@@ -312,6 +312,19 @@ __device__ __forceinline__ void load_to_lds16(const uint16_t *g, uint16_t *l) {
                  : "memory", "m0");
 }
 
+// The same from base (the same in every lane) + off bytes.
+__device__ __forceinline__ void load_to_lds16(const uint16_t *base, uint32_t off, uint16_t *l) {
+    const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint16_t *)l;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(
+                     __builtin_amdgcn_readfirstlane(to)),
+                 "v"(off), "s"(base)
+                 : "memory", "m0");
+}
+// Whether offsets within rows rows fit 32 bits.
+__device__ __forceinline__ bool near_rows(int64_t row_stride, int rows) {
+    return row_stride < (int64_t)1 << (30 - 6) || (rows <= 32 && row_stride < (int64_t)1 << (30 - 5));
+}
+
 template <int D>
 struct Lines {  // where a block's rows lie in LDS
     static constexpr int C = D / 8, RPL = 16 / C;  // chunks of a row, rows of a line
@@ -331,7 +344,8 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_tree_attn_mfma(TreeAttnArgs
     constexpr int LOADS = 2 * (D / 8);  // 1 KB loads of a block's K and V
     using L = Lines<D>;
     __shared__ __attribute__((aligned(1024))) uint16_t kv[2][2][KB * D];  // [block % 2][K, V]
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 31,
+              half = lane >> 5;
     const int wq = wave % NQ, wk = wave / NQ;
     const int g = blockIdx.x % a.n_kv_heads, rest = blockIdx.x / a.n_kv_heads;
     const int qt = rest % a.q_tiles, split = rest / a.q_tiles;
@@ -342,15 +356,35 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_tree_attn_mfma(TreeAttnArgs
     const uint16_t *K = static_cast<const uint16_t *>(a.k) + (int64_t)g * a.head_stride;
     const uint16_t *V = static_cast<const uint16_t *>(a.v) + (int64_t)g * a.head_stride;
 
+    // A wave takes every NW-th KB of K's and of V's rows.  Whole blocks: lane
+    // offsets that do not change, from the block's first row (with the addresses
+    // taken load by load, issuing them was a quarter of a block's time).
+    constexpr int NU = (L::C + NW - 1) / NW;
+    uint32_t off[NU];
+#pragma unroll
+    for (int i = 0; i < NU; ++i) {
+        const int s = 4 * (wave + NW * i) + (lane >> 4), p = (lane & 15) ^ L::swz(s);
+        off[i] = (uint32_t)(2 * ((int64_t)(s * L::RPL + p / L::C) * a.row_stride + 8 * (p % L::C)));
+    }
+    const bool near = near_rows(a.row_stride, KB);
     auto load_block = [&](int b, int buf) {
         const Block k = block_of<KB>(a, b);
-        // (fewer registers than with every address of the block at once)
-#pragma unroll 2
-        for (int t = wave; t < LOADS; t += NW) {
-            const int m = t / L::C, u = t % L::C;  // matrix, and 1 KB of it
-            const int s = 4 * u + (lane >> 4), p = (lane & 15) ^ L::swz(s);
-            const int r = min(s * L::RPL + p / L::C, k.len - 1);  // rows past the block: its last
-            load_to_lds16((m ? V : K) + (int64_t)(k.first + r) * a.row_stride + 8 * (p % L::C), &kv[buf][m][u * 512]);
+        if (k.len == KB && near) {
+            const int64_t first = (int64_t)k.first * a.row_stride;
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int i = 0; i < NU; ++i)
+                    if (L::C % NW == 0 || wave + NW * i < L::C)  // uniform over the wave
+                        load_to_lds16((m ? V : K) + first, off[i], &kv[buf][m][(wave + NW * i) * 512]);
+        } else {
+#pragma unroll 1
+            for (int t = wave; t < LOADS; t += NW) {
+                const int m = t / L::C, u = t % L::C;  // matrix, and 1 KB of it
+                const int s = 4 * u + (lane >> 4), p = (lane & 15) ^ L::swz(s);
+                const int r = min(s * L::RPL + p / L::C, k.len - 1);  // rows past the block: its last
+                load_to_lds16((m ? V : K) + (int64_t)(k.first + r) * a.row_stride + 8 * (p % L::C), &kv[buf][m][u * 512]);
+            }
         }
     };
     // The queries are asked for before the first block: loads return in order
@@ -618,7 +652,8 @@ __global__ __launch_bounds__(256, QT == 1 || D < 128 ? 2 : 1) void k_tree_attn_f
     constexpr int WORDS = VB > ROWS * OP ? VB : ROWS * OP;
     __shared__ __attribute__((aligned(1024))) uint32_t tile[NW][WORDS];  // two V blocks, or the outputs
     __shared__ float2 ml[NW][ROWS];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 15,
+              grp = lane >> 4;
     const int g = blockIdx.x % a.n_kv_heads, rest = blockIdx.x / a.n_kv_heads;
     const int r0 = rest % a.q_tiles * ROWS, split = rest / a.q_tiles;
     const int b1 = min(a.blocks, (split + 1) * a.per_split);
@@ -626,23 +661,42 @@ __global__ __launch_bounds__(256, QT == 1 || D < 128 ? 2 : 1) void k_tree_attn_f
     const uint16_t *V = static_cast<const uint16_t *>(a.v) + (int64_t)g * a.head_stride;
     uint16_t *vt = reinterpret_cast<uint16_t *>(tile[wave]);
 
+    // Whole blocks: lane offsets that do not change, from the block's first row.
+    // (Of V's loads u, only the lane's place in odd and even ones differs.)
+    const bool near = near_rows(a.row_stride, KB_FEW);
+    const uint32_t koff = (uint32_t)(2 * ((int64_t)col * a.row_stride + (8 * grp) % D));
+    uint32_t voff[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const int s = 4 * u + (lane >> 4), p = (lane & 15) ^ L::swz(s);
+        voff[u] = (uint32_t)(2 * ((int64_t)((lane >> 4) * L::RPL + p / L::C) * a.row_stride + 8 * (p % L::C)));
+    }
     u32x4_t kf[2][ES];
     auto load_k = [&](const Block &k) {
+        const bool whole = k.len == KB_FEW && near;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             // keys past the block: its last, masked; head_dim 16: the upper slots are zeros of q
-            const uint16_t *kp = K + (int64_t)(k.first + min(16 * t + col, k.len - 1)) * a.row_stride + (8 * grp) % D;
+            const char *kp = whole ? reinterpret_cast<const char *>(K + (int64_t)(k.first + 16 * t) * a.row_stride) + koff
+                                   : reinterpret_cast<const char *>(
+                                         K + (int64_t)(k.first + min(16 * t + col, k.len - 1)) * a.row_stride + (8 * grp) % D);
 #pragma unroll
             for (int s = 0; s < ES; ++s)
-                kf[t][s] = *reinterpret_cast<const u32x4_t *>(kp + 32 * s);
+                kf[t][s] = *reinterpret_cast<const u32x4_t *>(kp + 64 * s);
         }
     };
     auto load_v = [&](const Block &k, int buf) {
+        if (k.len == KB_FEW && near) {
 #pragma unroll
-        for (int u = 0; u < VB / 512; ++u) {
-            const int s = 4 * u + (lane >> 4), p = (lane & 15) ^ L::swz(s);
-            const int r = min(s * L::RPL + p / L::C, k.len - 1);
-            load_to_lds16(V + (int64_t)(k.first + r) * a.row_stride + 8 * (p % L::C), vt + buf * VB + u * 512);
+            for (int u = 0; u < VB / 512; ++u)
+                load_to_lds16(V + (int64_t)(k.first + 4 * u * L::RPL) * a.row_stride, voff[u & 1], vt + buf * VB + u * 512);
+        } else {
+#pragma unroll 1
+            for (int u = 0; u < VB / 512; ++u) {
+                const int s = 4 * u + (lane >> 4), p = (lane & 15) ^ L::swz(s);
+                const int r = min(s * L::RPL + p / L::C, k.len - 1);
+                load_to_lds16(V + (int64_t)(k.first + r) * a.row_stride + 8 * (p % L::C), vt + buf * VB + u * 512);
+            }
         }
     };
     int b = split * a.per_split + wave;
