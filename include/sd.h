@@ -302,7 +302,8 @@ sd_status sd_autoregressive_sample(sd_model *model, const int32_t *prompt, int32
 /* One layer of a KV cache: the element (head g, position p, e) of K and of V is
  * at g * head_stride + p * row_stride + e (strides in elements, multiples of
  * 16 bytes; row_stride >= head_dim; rows do not overlap; k and v 16-byte
- * aligned).  head_dim is a power of two in [16, 128], dtype an sd_dtype. */
+ * aligned).  head_dim is a power of two in [16, 128], capacity at most 2^30,
+ * dtype an sd_dtype; the operators take up to 4096 query heads. */
 typedef struct {
     void *k, *v;
     int64_t head_stride, row_stride;

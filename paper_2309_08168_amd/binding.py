@@ -488,14 +488,14 @@ def _refuse(message: str):
 
 # The operators run for a few microseconds, so their calls are short: torch, its
 # types and its stream are looked up once, and a tensor's attributes read once.
-_torch = _f32 = _bf16 = _i32 = _raw_stream = _current = None
+_torch = _f32 = _bf16 = _i32 = _bits = _raw_stream = _current = None
 
 
 def _use_torch():
-    global _torch, _f32, _bf16, _i32, _raw_stream, _current
+    global _torch, _f32, _bf16, _i32, _bits, _raw_stream, _current
     import torch
 
-    _f32, _bf16, _i32 = torch.float32, torch.bfloat16, torch.int32
+    _f32, _bf16, _i32, _bits = torch.float32, torch.bfloat16, torch.int32, (torch.int64, torch.uint64)
     _raw_stream = torch._C._cuda_getCurrentRawStream  # (device index) -> hipStream_t
     _current = torch.cuda.current_device
     load()
@@ -562,6 +562,12 @@ def _words(t, n: int, what: str) -> int:
     return t.data_ptr()
 
 
+def _int32(value: int, what: str):
+    """Refuses what ctypes would cut to 32 bits."""
+    if not -0x80000000 <= value <= 0x7fffffff:
+        _refuse(f"{what} {value} is outside the 32-bit integers")
+
+
 def _space(workspace, like):
     """(address, bytes) of a caller's workspace."""
     if not workspace.is_contiguous():
@@ -575,6 +581,10 @@ def rope_append(form: sd_rope, qkv, k, v, slot: int, n_heads: int, positions=Non
     as in kv_layer, rows stored at slot ..; positions int32 [n] or None: pos0 ..
     Returns the rotated queries, float32 [n, n_heads, head_dim]."""
     layer, kvh, d = _layer(k, v)
+    _int32(slot, "slot")
+    _int32(pos0, "pos0")
+    if qkv.dim() != 2:
+        _refuse("qkv is [n, (n_heads + 2 n_kv_heads) head_dim]")
     n = qkv.shape[0]
     ld = _rows2(qkv, n, (n_heads + 2 * kvh) * d, "qkv")
     dev = _device(qkv, k, v)
@@ -602,6 +612,7 @@ def tree_attention(q, k, v, prefix: int, mask=None, scale: float = 0.0, out=None
     0 .. r), scale 0: 1 / sqrt(head_dim).  Returns out, like q; workspace: a tensor of
     at least tree_attention_workspace() bytes (else one is allocated)."""
     layer, _, d = _layer(k, v)
+    _int32(prefix, "prefix")
     shape = q.shape
     if len(shape) != 3:
         _refuse("q is [n, n_heads, head_dim]")
@@ -612,7 +623,7 @@ def tree_attention(q, k, v, prefix: int, mask=None, scale: float = 0.0, out=None
         return _elsewhere(dev, tree_attention, q, k, v, prefix, mask, scale, out, workspace)
     bits = None
     if mask is not None:
-        if mask.element_size() != 8 or mask.is_floating_point() or mask.shape != (n, (n + 63) >> 6) or \
+        if mask.dtype not in _bits or mask.shape != (n, (n + 63) >> 6) or \
                 not mask.is_contiguous():
             _refuse("mask is a contiguous int64 or uint64 [n, (n + 63) // 64]")
         _device(q, mask)
@@ -692,6 +703,7 @@ def kv_keep(kv, base: int, walk):
     dev = _device(kv, walk)
     if dev != _current():
         return _elsewhere(dev, kv_keep, kv, base, walk)
+    _int32(base, "base")
     cap, row = shape[-2], shape[-1] * kv.element_size()
     planes = kv.numel() // (cap * shape[-1]) if kv.numel() else 0
     status = _lib.sd_kv_keep(kv.data_ptr(), planes, cap * row, row, cap, base, at, n, _raw_stream(dev))

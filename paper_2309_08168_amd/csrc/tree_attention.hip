@@ -320,10 +320,8 @@ __device__ __forceinline__ void load_to_lds16(const uint16_t *base, uint32_t off
                  "v"(off), "s"(base)
                  : "memory", "m0");
 }
-// Whether offsets within rows rows fit 32 bits.
-__device__ __forceinline__ bool near_rows(int64_t row_stride, int rows) {
-    return row_stride < (int64_t)1 << (30 - 6) || (rows <= 32 && row_stride < (int64_t)1 << (30 - 5));
-}
+// Whether a block's offsets in bytes fit 32 bits.
+__device__ __forceinline__ bool near_rows(int64_t row_stride) { return row_stride < (int64_t)1 << 24; }
 
 template <int D>
 struct Lines {  // where a block's rows lie in LDS
@@ -366,7 +364,7 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_tree_attn_mfma(TreeAttnArgs
         const int s = 4 * (wave + NW * i) + (lane >> 4), p = (lane & 15) ^ L::swz(s);
         off[i] = (uint32_t)(2 * ((int64_t)(s * L::RPL + p / L::C) * a.row_stride + 8 * (p % L::C)));
     }
-    const bool near = near_rows(a.row_stride, KB);
+    const bool near = near_rows(a.row_stride);
     auto load_block = [&](int b, int buf) {
         const Block k = block_of<KB>(a, b);
         if (k.len == KB && near) {
@@ -663,7 +661,7 @@ __global__ __launch_bounds__(256, QT == 1 || D < 128 ? 2 : 1) void k_tree_attn_f
 
     // Whole blocks: lane offsets that do not change, from the block's first row.
     // (Of V's loads u, only the lane's place in odd and even ones differs.)
-    const bool near = near_rows(a.row_stride, KB_FEW);
+    const bool near = near_rows(a.row_stride);
     const uint32_t koff = (uint32_t)(2 * ((int64_t)col * a.row_stride + (8 * grp) % D));
     uint32_t voff[2];
 #pragma unroll

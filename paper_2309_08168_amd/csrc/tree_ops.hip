@@ -459,8 +459,8 @@ sd_status rope_append(const sd_rope *rope, const float *qkv, int64_t ld_qkv, int
     const int64_t D = kv->head_dim, KVH = kv->n_kv_heads;
     if (!qkv || !q_out || !aligned16(qkv) || !aligned16(q_out) || ((uintptr_t)positions & 3))
         return report(SD_ERR_INVALID_ARG, "qkv and q_out must be set and 16-byte aligned");
-    if (n < 1 || n > 1 << 20 || n_heads < 1 || n_heads % KVH)
-        return report(SD_ERR_INVALID_ARG, "n must be in [1, 2^20] and n_heads a multiple of n_kv_heads");
+    if (n < 1 || n > 1 << 20 || n_heads < 1 || n_heads > 4096 || n_heads % KVH)
+        return report(SD_ERR_INVALID_ARG, "n must be in [1, 2^20], n_heads a multiple of n_kv_heads and at most 4096");
     if (ld_qkv % 4 || ld_q % 4 || ld_qkv < (n_heads + 2 * KVH) * D || ld_q < n_heads * D)
         return report(SD_ERR_INVALID_ARG, "ld_qkv and ld_q must hold a row and be multiples of 4");
     if (!positions && (int64_t)pos0 + n - 1 > INT32_MAX)
@@ -509,8 +509,10 @@ sd_status check_layer(const sd_kv_layer *kv) {
     if (kv->dtype != SD_F32 && kv->dtype != SD_BF16)
         return report(SD_ERR_INVALID_ARG, "dtype must be SD_F32 or SD_BF16");
     const int32_t D = kv->head_dim, unit = kv->dtype == SD_BF16 ? 8 : 4;
-    if (D < 16 || D > MAX_HEAD_DIM || (D & (D - 1)) || kv->n_kv_heads < 1 || kv->capacity < 1)
-        return report(SD_ERR_INVALID_ARG, "head_dim must be a power of two in [16, 128], n_kv_heads and capacity >= 1");
+    if (D < 16 || D > MAX_HEAD_DIM || (D & (D - 1)) || kv->n_kv_heads < 1 || kv->capacity < 1 ||
+        kv->capacity > 1 << 30)
+        return report(SD_ERR_INVALID_ARG, "head_dim must be a power of two in [16, 128], n_kv_heads >= 1 and capacity in "
+                                          "[1, 2^30]");
     const int64_t hs = kv->head_stride, rs = kv->row_stride, most = (int64_t)1 << 40;
     if (rs < D || rs % unit || hs < 0 || hs % unit || rs > most || hs > most)
         return report(SD_ERR_INVALID_ARG, "strides must be multiples of 16 bytes, row_stride at least head_dim");

@@ -38,7 +38,7 @@ def layer(**change):
 
 
 BAD_LAYERS = [dict(k=None), dict(v=None), dict(k=P + 8), dict(v=P + 2), dict(dtype=2), dict(head_dim=96),
-              dict(head_dim=8), dict(head_dim=256), dict(n_kv_heads=0), dict(capacity=0), dict(row_stride=64),
+              dict(head_dim=8), dict(head_dim=256), dict(n_kv_heads=0), dict(capacity=0), dict(capacity=(1 << 30) + 1, head_stride=1 << 39), dict(row_stride=64),
               dict(row_stride=132), dict(head_stride=-128), dict(head_stride=12), dict(head_stride=0), dict(head_stride=128),
               dict(head_stride=63 * 128), dict(head_stride=128, row_stride=128 + 64)]
 
@@ -69,7 +69,7 @@ def test_bad_layers(change):
 
 @pytest.mark.parametrize("change,status", [
     (dict(qkv=None), BAD), (dict(qkv=P + 4), BAD), (dict(q=None), BAD), (dict(q=P + 8), BAD), (dict(positions=P + 2), BAD),
-    (dict(n=0), BAD), (dict(n=(1 << 20) + 1), BAD), (dict(n_heads=3), BAD), (dict(n_heads=0), BAD), (dict(ld_qkv=1020), BAD),
+    (dict(n=0), BAD), (dict(n=(1 << 20) + 1), BAD), (dict(n_heads=3), BAD), (dict(n_heads=0), BAD), (dict(n_heads=4098, ld_qkv=1 << 22, ld_q=1 << 22), BAD), (dict(ld_qkv=1020), BAD),
     (dict(ld_qkv=1026), BAD), (dict(ld_q=508), BAD), (dict(ld_q=514), BAD), (dict(slot=-1), FULL), (dict(slot=61), FULL),
     (dict(n=65), FULL), (dict(positions=None, pos0=2**31 - 3), BAD)], ids=str)
 def test_rope_append_refuses(change, status):
@@ -162,6 +162,13 @@ def test_tensor_shapes_types_and_strides_are_refused():
                 lambda: binding.tree_attention(q.half(), k, k, 0), lambda: binding.tree_attention(q[:, :, :32], k, k, 0),
                 lambda: binding.tree_attention(q, k, k, 0, mask=torch.zeros(3, 2, dtype=torch.int64)),
                 lambda: binding.tree_attention(q, k, k, 0, mask=torch.zeros(3, 1)),
+                lambda: binding.tree_attention(q, k, k, 0, mask=torch.zeros(3, 1, dtype=torch.complex64)),
+                lambda: binding.tree_attention(q, k, k, 1 << 32),
+                lambda: binding.tree_attention(q[0], k, k, 0),
+                lambda: binding.rope_append(binding.rope(rotary_dim=64), torch.zeros(3, 8 * 64), k, k, 1 << 32, 4),
+                lambda: binding.rope_append(binding.rope(rotary_dim=64), torch.zeros(3, 8, 64), k, k, 0, 4),
+                lambda: binding.kv_keep(k, 1 << 32, torch.zeros(8, dtype=torch.int32)),
+                lambda: binding.kv_keep(k, 0, torch.zeros(9, dtype=torch.int32)),
                 lambda: binding.tree_attention(q.transpose(0, 1), k, k, 0),
                 lambda: binding.tree_accept(torch.zeros(3, 10), torch.zeros(3), torch.zeros(3)),
                 lambda: binding.kv_keep(k.transpose(0, 1), 0, torch.zeros(8, dtype=torch.int32)),
