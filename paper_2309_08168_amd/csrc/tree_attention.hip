@@ -885,31 +885,46 @@ __global__ __launch_bounds__(256, QT == 1 || D < 128 ? 2 : 1) void k_tree_attn_f
 
 // The shares of a (node, head) joined: a work-group each.  Every wave takes the
 // shares' maxima and sums by itself; D / 4 lanes hold a row, the groups of lanes
-// take the shares in turn and add up in order.  (One thread per element walking
+// take the shares in turn and add up in order.  The first J shares of a group
+// and the first 64 maxima are asked for at once.  (One thread per element walking
 // over the shares: 6.7 us for 520 rows of 10 shares, 33 us for 576 of 63.)
 constexpr int JOIN_THREADS = 256;
-template <int D>
+template <int D, int J>
 __global__ __launch_bounds__(JOIN_THREADS) void k_tree_join(TreeAttnArgs a) {
     constexpr int LANES = D / 4, NG = JOIN_THREADS / LANES;
     __shared__ f32x4_t red[NG][LANES];
     const int64_t slots = (int64_t)a.n * a.n_heads, slot = blockIdx.x;
     const int lane = threadIdx.x & 63, e = threadIdx.x % LANES, gi = threadIdx.x / LANES;
-    float m = -INFINITY;
-    for (int s = lane; s < a.splits; s += 64)
-        m = fmaxf(m, a.part_ml[s * slots + slot].x);
+    const float *po = a.part_o + slot * D + 4 * e;
+    const float2 *pm = a.part_ml + slot;
+    f32x4_t x[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+        x[j] = load4(po + min(gi + j * NG, a.splits - 1) * slots * D);
+    const float2 first = pm[min(lane, a.splits - 1) * slots];
+    float m = first.x;
+    for (int s = lane + 64; s < a.splits; s += 64)
+        m = fmaxf(m, pm[s * slots].x);
     m = wave_max_all(m);
     const float mu = m == -INFINITY ? 0.0f : m;
-    float sum = 0.0f;
-    for (int s = lane; s < a.splits; s += 64) {
-        const float2 v = a.part_ml[s * slots + slot];
+    const float w0 = __builtin_amdgcn_exp2f(first.x - mu);  // of share `lane`
+    float sum = lane < a.splits ? w0 * first.y : 0.0f;
+    for (int s = lane + 64; s < a.splits; s += 64) {
+        const float2 v = pm[s * slots];
         sum = fmaf(__builtin_amdgcn_exp2f(v.x - mu), v.y, sum);
     }
     const float total = wave_sum_all(sum);
     f32x4_t O = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        const int s = gi + j * NG;
+        const float w = s < 64 ? __shfl(w0, s & 63, 64) : __builtin_amdgcn_exp2f(pm[min(s, a.splits - 1) * slots].x - mu);
+        if (s < a.splits)
+            O += w * x[j];
+    }
 #pragma unroll 4
-    for (int s = gi; s < a.splits; s += NG)
-        O += __builtin_amdgcn_exp2f(a.part_ml[s * slots + slot].x - mu) *
-             load4(a.part_o + (s * slots + slot) * D + 4 * e);
+    for (int s = gi + J * NG; s < a.splits; s += NG)
+        O += __builtin_amdgcn_exp2f(pm[s * slots].x - mu) * load4(po + s * slots * D);
     red[gi][e] = O;
     __syncthreads();
     if (gi > 0)
@@ -920,6 +935,13 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_tree_join(TreeAttnArgs a) {
     const int nd = (int)(slot / a.n_heads), hd = (int)(slot - (int64_t)nd * a.n_heads);
     *reinterpret_cast<f32x4_t *>(a.out + (int64_t)nd * a.ld_out + (int64_t)hd * D + 4 * e) =
         total == 0.0f ? f32x4_t{0.0f, 0.0f, 0.0f, 0.0f} : O / total;
+}
+
+template <int D>
+void launch_join(const TreeAttnArgs &a, hipStream_t s) {
+    constexpr int NG = JOIN_THREADS / (D / 4);
+    auto join = a.splits <= NG ? k_tree_join<D, 1> : a.splits <= 2 * NG ? k_tree_join<D, 2> : k_tree_join<D, 4>;
+    hipLaunchKernelGGL(join, dim3((unsigned)(a.n * a.n_heads)), dim3(JOIN_THREADS), 0, s, a);
 }
 
 // Rows of a tile and shares of the keys.
@@ -1072,8 +1094,14 @@ sd_status tree_attention(const sd_kv_layer *kv, const float *q, int64_t ld_q, in
         launch_mfma<128>(a, s);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && a.splits > 1) {
-        auto join = D == 16 ? k_tree_join<16> : D == 32 ? k_tree_join<32> : D == 64 ? k_tree_join<64> : k_tree_join<128>;
-        hipLaunchKernelGGL(join, dim3((unsigned)(n * n_heads)), dim3(JOIN_THREADS), 0, s, a);
+        if (D == 16)
+            launch_join<16>(a, s);
+        else if (D == 32)
+            launch_join<32>(a, s);
+        else if (D == 64)
+            launch_join<64>(a, s);
+        else
+            launch_join<128>(a, s);
         e = hipGetLastError();
     }
     return e == hipSuccess ? SD_OK : report(SD_ERR_DEVICE, std::string("tree attention: ") + hipGetErrorString(e));
