@@ -595,7 +595,7 @@ def rope_append(form: sd_rope, qkv, k, v, slot: int, n_heads: int, positions=Non
         at = _words(positions, n, "positions")
         _device(qkv, positions)
     if q_out is None:
-        q_out, ldq = qkv.new_empty((n, n_heads, d)), n_heads * d
+        q_out, ldq = qkv.new_empty(n, n_heads, d), n_heads * d
     else:
         ldq = _rows3(q_out, n, n_heads, d, "q_out")
         _device(qkv, q_out)
@@ -629,7 +629,7 @@ def tree_attention(q, k, v, prefix: int, mask=None, scale: float = 0.0, out=None
         _device(q, mask)
         bits = mask.data_ptr()
     if out is None:
-        out, ldo = q.new_empty(shape), h * d
+        out, ldo = q.new_empty(n, h, d), h * d
     else:
         ldo = _rows3(out, n, h, d, "out")
         _device(q, out)

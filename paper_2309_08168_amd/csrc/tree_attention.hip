@@ -945,27 +945,37 @@ void launch_join(const TreeAttnArgs &a, hipStream_t s) {
 }
 
 // Rows of a tile and shares of the keys.
-//   float32: tiles of 16 rows, four work-groups per CU, two blocks a share at least.
+//   float32: tiles of 16 rows, two work-groups per CU (128 rows over 4000 keys, 4
+//   heads of 64: 18.0 us, 21.1 with four).
 //   bfloat16, up to 32 rows of a kv head: the kernel for few, one work-group per
-//   CU (13 rows over 1200 keys, 40 heads: 10.3 us, 11.3 with two, which halves
-//   the keys of a share; one row over 60000 keys, 8 heads: 43 and 46).
+//   CU, four blocks (one a wave) a share at least (13 rows over 1200 keys, 40
+//   heads: 10.3 us, 11.3 with two per CU, which halves the keys of a share; one
+//   row over 60000 keys, 8 heads: 43 and 46).
 //   More rows: tiles of 64, 96 or 128, the fewest that hold a kv head's rows, and
 //   one or two work-groups per CU (mfma_shares).
-constexpr int TA_GROUPS = 1024, TA_GROUPS_FEW = 256, TA_CUS = 256, FEW_ROWS = 32;
+// A single share needs no join, which takes a launch: the few-row and float32
+// kernels keep short contexts whole.  us a call, whole and split, among others
+// and alone: 13 rows over 200 keys (40 heads) 8.6 and 24.2, 12.5 and 26.3; over
+// 400 11.1 and 26.9, 12.4 and 26.2; 32 rows over 300 14.2 and 30.0, 12.5 and
+// 28.4; float32, head_dim 64, 5 rows over 300 9.5 and 25.3, 12.7 and 24.9;
+// head_dim 128 over 300 18.8 and 34.5, 12.3 and 27.8.
+constexpr int TA_GROUPS = 512, TA_GROUPS_FEW = 256, TA_CUS = 256, FEW_ROWS = 32;
+constexpr int whole_blocks(int q_rows) { return q_rows == 16 ? 12 : 6; }  // few rows: blocks of 32 keys
+constexpr int WHOLE_F32 = 6 * 64;                                         // float32: blocks of 64 times head_dim
 
-// Two work-groups per CU hide a part of each other's softmax, about a seventh of
-// a long share; every work-group costs its start, its end and its part of the
-// join, about two blocks' time.  us, kernel and join, one and two per CU: 61
-// rows over 3001 keys (32 heads, 6 and 3 blocks a share) 26.3 and 27.4; 64 over
-// 8000 (8 heads, 4 and 2) 20.9 and 24.6; 512 over 16000 (8 heads, 32 and 16) 127
-// and 118.  Three per CU do not fit.
+// Shares of the tiles of more rows.  Two work-groups per CU hide a part of each
+// other's softmax, about a seventh of a long share; every work-group costs its
+// start and its end, about two blocks' time, and a join is about 1.7.  us, kernel
+// and join, with one and two per CU: 61 rows over 3001 keys (32 heads, 6 and 3
+// blocks a share) 24.2 and 27.5; 64 over 8000 (8 heads, 4 and 2) 19 and 24.8; 512
+// over 16000 (8 heads, 32 and 16) 112 and 105.  Three per CU do not fit.
 int mfma_shares(int units, int blocks) {
     int best = 1;
     double least = INFINITY;
-    for (int groups = TA_CUS; groups <= 2 * TA_CUS; groups += TA_CUS) {
+    for (int groups = 0; groups <= 2 * TA_CUS; groups += TA_CUS) {
         const int shares = std::max(1, std::min(blocks, groups / units));
         const int per = (blocks + shares - 1) / shares, w = (units * shares + TA_CUS - 1) / TA_CUS;
-        const double cost = w * (per * (w == 1 ? 7.0 / 6.0 : 1.0) + 2.0);
+        const double cost = w * (per * (w == 1 ? 7.0 / 6.0 : 1.0) + 2.0) + (shares > 1 ? 1.7 : 0.0);
         if (cost < least) {
             least = cost;
             best = shares;
@@ -988,12 +998,17 @@ void plan(const sd_kv_layer *kv, int32_t n_heads, int32_t n, int32_t nodes, int3
     const bool few = bf16 && a->rows <= FEW_ROWS;
     a->q_rows = few ? (a->rows <= 16 ? 16 : 32) : bf16 ? std::min(128, std::max(64, (a->rows + 31) / 32 * 32)) : 16;
     a->q_tiles = (a->rows + a->q_rows - 1) / a->q_rows;
-    const int kb = few ? KB_FEW : KB, step = few ? 4 : bf16 ? 1 : 2;  // step: blocks that a share has at least
+    const int kb = few ? KB_FEW : KB, step = few ? 4 : 1;
     a->prefix_blocks = (prefix + kb - 1) / kb;
     a->blocks = a->prefix_blocks + (nodes + kb - 1) / kb;
     const int units = a->q_tiles * a->n_kv_heads, groups = few ? TA_GROUPS_FEW : TA_GROUPS;
-    const int want = bf16 && !few ? mfma_shares(units, a->blocks)
-                                  : std::max(1, std::min((a->blocks + step - 1) / step, (groups + units - 1) / units));
+    int want;
+    if (few ? a->blocks <= whole_blocks(a->q_rows) : !bf16 && (int64_t)a->blocks * kv->head_dim <= WHOLE_F32)
+        want = 1;
+    else if (bf16 && !few)
+        want = mfma_shares(units, a->blocks);
+    else
+        want = std::max(1, std::min((a->blocks + step - 1) / step, (groups + units - 1) / units));
     a->per_split = ((a->blocks + want - 1) / want + step - 1) / step * step;
     a->splits = (a->blocks + a->per_split - 1) / a->per_split;
 }
