@@ -412,3 +412,73 @@ def test_a_layer_of_a_verification(dtype):
     want, size = T.attention(f64(cq), k64, v64, prefix, np.tril(np.ones((m, m), bool)), 1 / math.sqrt(d))
     tol = T.attention_tol(d, prefix + m, size, np.abs(v64).max())
     assert np.abs(f64(chain) - want).max() <= tol and np.abs(f64(out[rows]) - want).max() <= tol
+
+
+def test_a_layer_captured_and_replayed():
+    """The four operators in one graph, replayed with new inputs in the same
+    buffers; every replay against the eager calls, on a cache of its own, with
+    eager work between the replays."""
+    rng = np.random.default_rng(8)
+    heads, kvh, d, prefix, n, vocab = 8, 4, 128, 700, 19, 1000
+    parents = T.random_parents(n, rng, 3)
+    depth, see = T.layout(parents)
+    form = binding.rope(rotary_dim=d)
+    pos = torch.tensor(prefix + depth, dtype=torch.int32, device="cuda")
+    mask = torch.tensor(T.pack(see).astype(np.int64), device="cuda")
+    par = torch.tensor(parents, device="cuda")
+    start = torch.randn(2, kvh, prefix + n, d, device="cuda").to(torch.bfloat16)
+
+    def layer(qkv, kv, logits, tokens):
+        q = binding.rope_append(form, qkv, kv[0], kv[1], prefix, heads, positions=pos)
+        out = binding.tree_attention(q, kv[0], kv[1], prefix, mask=mask)
+        walk = binding.tree_accept(logits, tokens, par)
+        binding.kv_keep(kv, prefix, walk)
+        return q, out, walk
+
+    def inputs(i):
+        r = np.random.default_rng(100 + i)
+        logits = r.standard_normal((n, vocab)).astype(np.float32)
+        best = logits.argmax(axis=1)
+        tokens = [0] + [int(best[p]) if r.random() < 0.7 else 5 for p in parents[1:]]
+        qkv = r.standard_normal((n, (heads + 2 * kvh) * d))
+        return (torch.tensor(qkv, dtype=torch.float32, device="cuda"), torch.tensor(logits, device="cuda"),
+                torch.tensor(tokens, dtype=torch.int32, device="cuda"))
+
+    qkv, logits, tokens = inputs(0)
+    kv = start.clone()
+    layer(qkv, kv, logits, tokens)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        outs = layer(qkv, kv, logits, tokens)
+    for i in range(5):
+        new = inputs(i)
+        for to, x in zip((qkv, logits, tokens), new):
+            to.copy_(x)
+        kv.copy_(start)
+        g.replay()
+        mine = start.clone()
+        want = layer(new[0], mine, new[1], new[2])
+        torch.cuda.synchronize()
+        assert torch.equal(kv, mine) and all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+def test_calls_on_two_streams_at_once():
+    rng = np.random.default_rng(2)
+    work = []
+    for i in range(2):
+        k, v = layers(rng, 4, 2100, 128, "bf16")
+        q = torch.randn(9 + 20 * i, 8, 128, device="cuda")
+        logits = torch.randn(64, 32000, device="cuda")
+        par = torch.tensor(T.random_parents(64, rng), device="cuda")
+        tok = torch.zeros(64, dtype=torch.int32, device="cuda")
+        want = binding.tree_attention(q, k, v, 2000), binding.tree_accept(logits, tok, par)
+        work.append((torch.cuda.Stream(), q, k, v, logits, tok, par, want, []))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for s, q, k, v, logits, tok, par, _, got in work:
+            with torch.cuda.stream(s):
+                got.append((binding.tree_attention(q, k, v, 2000), binding.tree_accept(logits, tok, par)))
+    torch.cuda.synchronize()
+    for *_, want, got in work:
+        assert all(torch.equal(a, b) for pair in got for a, b in zip(pair, want))
