@@ -137,7 +137,8 @@ __device__ __forceinline__ void merge_waves(const TreeAttnArgs &a, const float *
 // of row c.  The value products O^T[e][row] += V^T P^T take the reduction slots
 // (step v, slot g) as key 4 g + v, so weights stay in their lanes and a V operand
 // is one element of row 4 g + v.  The waves keep states of their own and merge
-// at the end.
+// at the end.  Bound by the chain of loads, products and softmax of a block where
+// there are few: 5 rows over 30 keys, 4 heads of 64, 5.2 us.
 constexpr int TA_WAVES = 4;
 
 template <int D>
@@ -266,6 +267,10 @@ __global__ __launch_bounds__(TA_WAVES * 64) void k_tree_attn_f32(TreeAttnArgs a)
 // LDS lines are 256 bytes, 16 chunks of 16 bytes: 128 / D rows.  Chunk p of line s
 // lies at p ^ swz(s), which spreads the 16 rows of a K read and the four rows of a
 // V read over all banks; the loads permute the chunks of a line on the way in.
+//
+// Heads of 128, with their join: 64 rows of 8 over 16000 keys, 8 kv heads (four
+// tiles of 128) 91 + 8 us, 1.1 PFLOP/s issued; 9 rows of 8 over 60000 keys, 8 kv heads (96)
+// 83 + 6 us, 3.0 TB/s; 61 rows over 3001 keys, 32 heads (64) 21 + 4 us.
 
 // A maximum that grows by no more than this (in log2) does not rescale the sums:
 // weights then reach 2^8 and not 1, which float32 sums do not mind.
@@ -623,7 +628,9 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_tree_attn_mfma(TreeAttnArgs
 // score products, V straight into the wave's LDS, both one block ahead.  Lane
 // (col, grp) receives the keys 16 t + 4 grp + v of row col, which are the slots
 // u = 4 t + v that the value products take from it.  LDS lines are permuted for
-// the reads here: eight rows, two adjacent chunks each.
+// the reads here: eight rows, two adjacent chunks each.  13 rows over 1200 keys, 40
+// heads of 128: 10.6 us (2.4 TB/s) and the join's 3.9, most of which is a
+// launch's; one row over 60000 keys, 8 heads: 43 us, 5.7 TB/s.
 __device__ __forceinline__ f32x4_t mfma16(u32x4_t a, u32x4_t b, f32x4_t c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c,
                                                    0, 0, 0);
