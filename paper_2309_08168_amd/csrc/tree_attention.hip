@@ -268,9 +268,10 @@ __global__ __launch_bounds__(TA_WAVES * 64) void k_tree_attn_f32(TreeAttnArgs a)
 // lies at p ^ swz(s), which spreads the 16 rows of a K read and the four rows of a
 // V read over all banks; the loads permute the chunks of a line on the way in.
 //
-// Heads of 128, with their join: 64 rows of 8 over 16000 keys, 8 kv heads (four
-// tiles of 128) 91 + 8 us, 1.1 PFLOP/s issued; 9 rows of 8 over 60000 keys, 8 kv heads (96)
-// 83 + 6 us, 3.0 TB/s; 61 rows over 3001 keys, 32 heads (64) 21 + 4 us.
+// Heads of 128, with their join: 64 rows of 8 over 16000 keys, 8 kv heads (tiles
+// of 128) 91 + 8 us, 1.1 PFLOP/s issued; 9 rows of 8 over 60000 keys, 8 kv heads
+// 76 + 6 us, 3.2 TB/s (the read alone takes 50, and power holds the clock at 1.7
+// GHz); 61 rows over 3001 keys, 32 heads (64) 21 + 4 us.
 
 // A maximum that grows by no more than this (in log2) does not rescale the sums:
 // weights then reach 2^8 and not 1, which float32 sums do not mind.
@@ -403,10 +404,13 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_tree_attn_mfma(TreeAttnArgs
     }
     __builtin_amdgcn_sched_barrier(0);
     load_block(b0, 0);
+    // Rows past the last are zeros, which draw less power than copies of it (9 rows
+    // of 8 over 60000 keys: 80.3 -> 79.8 us with the join).
+    const float scale = r0 + col < a.rows ? a.scale : 0.0f;
     u32x4_t qf[ES][T];
 #pragma unroll
     for (int s = 0; s < ES; ++s)
-        query_terms(qx[s][0] * a.scale, qx[s][1] * a.scale, qf[s]);
+        query_terms(qx[s][0] * scale, qx[s][1] * scale, qf[s]);
     // V^T reads: ds_read_b64_tr_b16 hands lane l of each 16-lane group element
     // l % 4 of the 8 bytes that lanes l / 4 + 4 k (k = 0..3) point at, so lane l
     // points at row 4 half + l / 4 % 4, columns 16 (l / 16 % 2) + 4 (l % 4) ...
@@ -958,8 +962,9 @@ void launch_join(const TreeAttnArgs &a, hipStream_t s) {
 //   CU, four blocks (one a wave) a share at least (13 rows over 1200 keys, 40
 //   heads: 10.3 us, 11.3 with two per CU, which halves the keys of a share; one
 //   row over 60000 keys, 8 heads: 43 and 46).
-//   More rows: tiles of 64, 96 or 128, the fewest that hold a kv head's rows, and
-//   one or two work-groups per CU (mfma_shares).
+//   More rows: tiles of 64, or of 128 above that (for 72 rows a tile of three waves
+//   took 82.4 us where four, one of which only loads, take 80.3), and one or two
+//   work-groups per CU (mfma_shares).
 // A single share needs no join, which takes a launch: the few-row and float32
 // kernels keep short contexts whole.  us a call, whole and split, among others
 // and alone: 13 rows over 200 keys (40 heads) 8.6 and 24.2, 12.5 and 26.3; over
@@ -1003,7 +1008,7 @@ void plan(const sd_kv_layer *kv, int32_t n_heads, int32_t n, int32_t nodes, int3
     a->G = n_heads / kv->n_kv_heads;
     a->rows = n * a->G;
     const bool few = bf16 && a->rows <= FEW_ROWS;
-    a->q_rows = few ? (a->rows <= 16 ? 16 : 32) : bf16 ? std::min(128, std::max(64, (a->rows + 31) / 32 * 32)) : 16;
+    a->q_rows = few ? (a->rows <= 16 ? 16 : 32) : bf16 ? (a->rows <= 64 ? 64 : 128) : 16;
     a->q_tiles = (a->rows + a->q_rows - 1) / a->q_rows;
     const int kb = few ? KB_FEW : KB, step = few ? 4 : 1;
     a->prefix_blocks = (prefix + kb - 1) / kb;
@@ -1060,8 +1065,6 @@ void launch_mfma(const TreeAttnArgs &a, hipStream_t s) {
         hipLaunchKernelGGL((k_tree_attn_few<D, 2>), grid, dim3(256), 0, s, a);
     else if (a.q_rows == 64)
         hipLaunchKernelGGL((k_tree_attn_mfma<D, 2, 2>), grid, dim3(256), 0, s, a);
-    else if (a.q_rows == 96)
-        hipLaunchKernelGGL((k_tree_attn_mfma<D, 3, 1>), grid, dim3(192), 0, s, a);
     else
         hipLaunchKernelGGL((k_tree_attn_mfma<D, 4, 1>), grid, dim3(256), 0, s, a);
 }
