@@ -497,7 +497,7 @@ def _use_torch():
 
     _f32, _bf16, _i32, _bits = torch.float32, torch.bfloat16, torch.int32, (torch.int64, torch.uint64)
     _raw_stream = torch._C._cuda_getCurrentRawStream  # (device index) -> hipStream_t
-    _current = torch.cuda.current_device
+    _current = torch._C._cuda_getDevice  # (every call holds a tensor on a GPU)
     load()
     _torch = torch
 
@@ -562,10 +562,11 @@ def _words(t, n: int, what: str) -> int:
     return t.data_ptr()
 
 
-def _int32(value: int, what: str):
+def _int32(*values: int):
     """Refuses what ctypes would cut to 32 bits."""
-    if not -0x80000000 <= value <= 0x7fffffff:
-        _refuse(f"{what} {value} is outside the 32-bit integers")
+    for value in values:
+        if not -0x80000000 <= value <= 0x7fffffff:
+            _refuse(f"{value} is outside the 32-bit integers")
 
 
 def _space(workspace, like):
@@ -581,19 +582,17 @@ def rope_append(form: sd_rope, qkv, k, v, slot: int, n_heads: int, positions=Non
     as in kv_layer, rows stored at slot ..; positions int32 [n] or None: pos0 ..
     Returns the rotated queries, float32 [n, n_heads, head_dim]."""
     layer, kvh, d = _layer(k, v)
-    _int32(slot, "slot")
-    _int32(pos0, "pos0")
-    if qkv.dim() != 2:
+    _int32(slot, pos0)
+    if qkv.ndim != 2:
         _refuse("qkv is [n, (n_heads + 2 n_kv_heads) head_dim]")
     n = qkv.shape[0]
     ld = _rows2(qkv, n, (n_heads + 2 * kvh) * d, "qkv")
-    dev = _device(qkv, k, v)
+    if positions is None:
+        at, dev = None, _device(qkv, k, v)
+    else:
+        at, dev = _words(positions, n, "positions"), _device(qkv, k, v, positions)
     if dev != _current():
         return _elsewhere(dev, rope_append, form, qkv, k, v, slot, n_heads, positions, pos0, q_out)
-    at = None
-    if positions is not None:
-        at = _words(positions, n, "positions")
-        _device(qkv, positions)
     if q_out is None:
         q_out, ldq = qkv.new_empty(n, n_heads, d), n_heads * d
     else:
@@ -612,22 +611,20 @@ def tree_attention(q, k, v, prefix: int, mask=None, scale: float = 0.0, out=None
     0 .. r), scale 0: 1 / sqrt(head_dim).  Returns out, like q; workspace: a tensor of
     at least tree_attention_workspace() bytes (else one is allocated)."""
     layer, _, d = _layer(k, v)
-    _int32(prefix, "prefix")
+    _int32(prefix)
     shape = q.shape
     if len(shape) != 3:
         _refuse("q is [n, n_heads, head_dim]")
     n, h, _ = shape
     ld = _rows3(q, n, h, d, "q")
-    dev = _device(q, k, v)
+    if mask is None:
+        bits, dev = None, _device(q, k, v)
+    else:
+        if mask.dtype not in _bits or mask.shape != (n, (n + 63) >> 6) or not mask.is_contiguous():
+            _refuse("mask is a contiguous int64 or uint64 [n, (n + 63) // 64]")
+        bits, dev = mask.data_ptr(), _device(q, k, v, mask)
     if dev != _current():
         return _elsewhere(dev, tree_attention, q, k, v, prefix, mask, scale, out, workspace)
-    bits = None
-    if mask is not None:
-        if mask.dtype not in _bits or mask.shape != (n, (n + 63) >> 6) or \
-                not mask.is_contiguous():
-            _refuse("mask is a contiguous int64 or uint64 [n, (n + 63) // 64]")
-        _device(q, mask)
-        bits = mask.data_ptr()
     if out is None:
         out, ldo = q.new_empty(n, h, d), h * d
     else:
@@ -703,7 +700,7 @@ def kv_keep(kv, base: int, walk):
     dev = _device(kv, walk)
     if dev != _current():
         return _elsewhere(dev, kv_keep, kv, base, walk)
-    _int32(base, "base")
+    _int32(base)
     cap, row = shape[-2], shape[-1] * kv.element_size()
     planes = kv.numel() // (cap * shape[-1]) if kv.numel() else 0
     status = _lib.sd_kv_keep(kv.data_ptr(), planes, cap * row, row, cap, base, at, n, _raw_stream(dev))
