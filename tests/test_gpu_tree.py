@@ -172,6 +172,65 @@ def test_attention_long(dtype, n):
     check_attention(n, 2, 1, 128, dtype, 5000 if n < 1024 else 50, tree(n, back=30))
 
 
+@pytest.mark.parametrize("d,dtype,n", [(16, "f32", 1), (128, "f32", 3), (32, "bf16", 2), (128, "bf16", 1), (128, "bf16", 40)])
+def test_attention_many_shares(d, dtype, n):
+    """More shares than the join takes at once: hundreds for one kv head."""
+    prefix = 35001
+    k = torch.empty(1, prefix + n, d, dtype=TYPES[dtype], device="cuda")
+    assert binding.tree_attention_workspace(k, k, 1, n, prefix) > 100 * n * 4 * (d + 2)
+    check_attention(n, 1, 1, d, dtype, prefix, tree(n))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,heads", [(5, 4), (40, 4)])
+@pytest.mark.parametrize("gap", [2**24 - 8, 2**24 + 8])
+def test_a_layer_past_32_bits(dtype, n, heads, gap):
+    """Rows so far apart that offsets pass 2^31 elements and 2^32 bytes, with
+    row strides on both sides of where a block's offsets fit 32 bits."""
+    kvh, d, cap = 2, 128, 132
+    size = (cap - 1) * gap + 2 * kvh * d
+    assert size > 2**31
+    # k and v interleaved in one buffer: heads of k, then of v, in each row
+    buf = torch.empty(size, dtype=TYPES[dtype], device="cuda")
+    k, v = (torch.as_strided(buf, (kvh, cap, d), (d, gap, 1), i * kvh * d) for i in range(2))
+    rng = np.random.default_rng(n)
+    near_k, near_v = layers(rng, kvh, cap, d, dtype)
+    k.copy_(near_k)
+    v.copy_(near_v)
+    prefix = cap - n
+    qkv = torch.tensor(rng.standard_normal((n, (heads + 2 * kvh) * d)), dtype=torch.float32, device="cuda")
+    form = binding.rope(rotary_dim=d)
+    q = binding.rope_append(form, qkv, k, v, prefix, heads, pos0=prefix)
+    near_q = binding.rope_append(form, qkv, near_k, near_v, prefix, heads, pos0=prefix)
+    assert torch.equal(q, near_q) and torch.equal(k, near_k) and torch.equal(v, near_v)
+    mask = torch.tensor(T.pack(tree(n)).astype(np.int64), device="cuda")
+    assert torch.equal(binding.tree_attention(q, k, v, prefix, mask=mask),
+                       binding.tree_attention(q, near_k, near_v, prefix, mask=mask))
+
+
+def test_walk_and_move_past_32_bits():
+    n, ld, vocab = 600, 2**21, 500
+    rng = np.random.default_rng(1)
+    parents = T.random_parents(n, rng)
+    logits = rng.standard_normal((n, vocab)).astype(np.float32)
+    best = logits.argmax(axis=1)
+    tokens = [0] + [int(best[p]) for p in parents[1:]]
+    x = torch.empty(n, ld, device="cuda")[:, :vocab]
+    x.copy_(torch.tensor(logits))
+    walk = binding.tree_accept(x, torch.tensor(tokens, dtype=torch.int32, device="cuda"), torch.tensor(parents, device="cuda"))
+    del x
+    w = walk.cpu().numpy()
+    assert np.array_equal(w, T.walk(logits, tokens, parents))
+    planes, d, cap = 2, 128, 9_000_000  # a plane of 2.3 GB
+    base = cap - n
+    kv = torch.empty(planes, cap, d, dtype=torch.bfloat16, device="cuda")
+    kv[:, base:] = torch.randn(planes, n, d, device="cuda")
+    kv[:, :n] = 1.0
+    want = T.keep(f64(kv[:, base:]), 0, w[2:2 + w[0]])
+    binding.kv_keep(kv, base, walk)
+    assert np.array_equal(f64(kv[:, base:]), want) and (kv[:, :n] == 1.0).all()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("prefix", [0, 70])
 def test_attention_any_mask(dtype, prefix):
