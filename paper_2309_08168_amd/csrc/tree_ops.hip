@@ -368,7 +368,8 @@ int accept_slices(int32_t n, int32_t vocab, int32_t *slice) {
 // written after every row path[j], j <= i, has been read and is no later row's
 // source (path[j] >= j > i): batches of rows may follow one another in place,
 // each read whole before it is written.  17 rows of 256 bytes in 3200 planes
-// 7.4 us (3.6 TB/s: a wave's reads, then its writes), 4 rows in 1280 planes 3.5.
+// 7.3 us (3.7 TB/s: a wave's reads, then its writes), 4 rows in 1280 planes 3.3
+// (7.6 and 3.7 with half the words in flight and none passed over).
 
 struct KeepArgs {
     char *kv;
@@ -377,7 +378,7 @@ struct KeepArgs {
     const int32_t *walk;
 };
 constexpr int KEEP_THREADS = 256;
-constexpr int KEEP_WORDS = 4;  // 16-byte words in flight per lane
+constexpr int KEEP_WORDS = 8;  // 16-byte words in flight per lane
 
 __global__ __launch_bounds__(KEEP_THREADS) void k_kv_keep(KeepArgs a) {
     __shared__ int32_t path[SD_TREE_MAX];
@@ -413,6 +414,8 @@ __global__ __launch_bounds__(KEEP_THREADS) void k_kv_keep(KeepArgs a) {
         u32x4_t v[KEEP_WORDS];
 #pragma unroll
         for (int j = 0; j < KEEP_WORDS; ++j) {
+            if (w0 + 64 * j >= words)  // uniform
+                break;
             const int w = min(w0 + 64 * j + lane, words - 1), i = w / wpr;
             v[j] = *reinterpret_cast<const u32x4_t *>(rows + (int64_t)path[i] * a.row_bytes + 16 * (w - i * wpr));
         }
