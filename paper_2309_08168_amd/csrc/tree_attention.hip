@@ -135,15 +135,21 @@ __device__ __forceinline__ void merge_waves(const TreeAttnArgs &a, const float *
 // elements 16 j + 4 g + u of key c and of row c in step (j, u), so both come by
 // 16-byte loads straight from memory, and receives the keys 4 g + v, v = 0..3,
 // of row c.  The value products O^T[e][row] += V^T P^T take the reduction slots
-// (step v, slot g) as key 4 g + v, so weights stay in their lanes and a V operand
-// is one element of row 4 g + v.  The waves keep states of their own and merge
-// at the end.  Bound by the chain of loads, products and softmax of a block where
-// there are few: 5 rows over 30 keys, 4 heads of 64, 5.2 us.
+// (step v, slot g) as key 4 g + v, so weights stay in their lanes; tile t's row i is
+// element 64 (t / 4) + 4 i + t % 4, so 16 bytes of row 4 g + v are a lane's operands
+// of four tiles.  V is asked for before the scores and the next block's K after
+// them.  The waves keep states of their own and merge at the end.
+//
+// Bound by the read of the cache, 4 rows over 4000 keys, 40 heads of 128: 34.2 us,
+// 4.8 TB/s (43 with V by single elements and no load ahead); by the chain of loads,
+// products and softmax of a block where there are few, 5 rows over 30 keys, 4
+// heads of 64: 4.9 us.
 constexpr int TA_WAVES = 4;
 
 template <int D>
-__global__ __launch_bounds__(TA_WAVES * 64) void k_tree_attn_f32(TreeAttnArgs a) {
-    constexpr int ES = D / 16, OP = D + 4;
+__global__ __launch_bounds__(TA_WAVES * 64, 2) void k_tree_attn_f32(TreeAttnArgs a) {
+    constexpr int ES = D / 16, OP = D + 4, W = ES < 4 ? ES : 4;  // W: elements of a load of V
+    typedef float vec_t __attribute__((ext_vector_type(W)));
     __shared__ __attribute__((aligned(16))) float tile[TA_WAVES][16 * OP];
     __shared__ float2 ml[TA_WAVES][16];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane & 15, g4 = lane >> 4;
@@ -157,26 +163,49 @@ __global__ __launch_bounds__(TA_WAVES * 64) void k_tree_attn_f32(TreeAttnArgs a)
 #pragma unroll
     for (int j = 0; j < ES; ++j)
         qx[j] = load4(a.q + (int64_t)node * a.ld_q + (int64_t)head * D + 16 * j + 4 * g4) * a.scale;
+    // o[t][u]: this element of row c
+    auto element = [&](int t, int u) { return 16 * W * (t / W) + W * (4 * g4 + u) + t % W; };
     float m_run = -INFINITY, l_run = 0.0f;
     f32x4_t o[ES];
 #pragma unroll
     for (int t = 0; t < ES; ++t)
         o[t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 
+    // keys past a block read its last one; their scores are masked
+    f32x4_t kx[ES];
+    auto load_k = [&](const Block &k) {
+        const float *kp = K + (int64_t)(k.first + min(16 * wave + c, k.len - 1)) * a.row_stride + 4 * g4;
+#pragma unroll
+        for (int j = 0; j < ES; ++j)
+            kx[j] = load4(kp + 16 * j);
+    };
+    if (b0 < b1)
+        load_k(block_of<KB>(a, b0));
     for (int b = b0; b < b1; ++b) {
         const Block k = block_of<KB>(a, b);
-        if (16 * wave >= k.len)
-            continue;  // uniform over the wave
-        // keys past the block read its last one; their scores are masked
-        const float *kp = K + (int64_t)(k.first + min(16 * wave + c, k.len - 1)) * a.row_stride + 4 * g4;
+        const bool some = 16 * wave < k.len;  // uniform over the wave
         f32x4_t s = {0.0f, 0.0f, 0.0f, 0.0f};
+        vec_t vx[4][ES / W];
+        if (some) {
 #pragma unroll
-        for (int j = 0; j < ES; ++j) {
-            const f32x4_t kx = load4(kp + 16 * j);
+            for (int v = 0; v < 4; ++v) {
+                const float *vp = V + (int64_t)(k.first + min(16 * wave + 4 * g4 + v, k.len - 1)) * a.row_stride + W * c;
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-                s = __builtin_amdgcn_mfma_f32_16x16x4f32(kx[u], qx[j][u], s, 0, 0, 0);
+                for (int t = 0; t < ES / W; ++t)
+                    vx[v][t] = *reinterpret_cast<const vec_t *>(vp + 16 * W * t);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < ES; ++j)
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    s = __builtin_amdgcn_mfma_f32_16x16x4f32(kx[j][u], qx[j][u], s, 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
         }
+        if (b + 1 < b1)
+            load_k(block_of<KB>(a, b + 1));
+        if (!some)
+            continue;
         const uint32_t see = (uint32_t)(visible(a, k, node) >> (16 * wave + 4 * g4)) & 15u;
         float mx = -INFINITY;
 #pragma unroll
@@ -195,45 +224,38 @@ __global__ __launch_bounds__(TA_WAVES * 64) void k_tree_attn_f32(TreeAttnArgs a)
             p[v] = __builtin_amdgcn_exp2f(s[v] - m_use);
         l_run += (p[0] + p[1]) + (p[2] + p[3]);
         m_run = m_new;
-        const float *vp[4];
-        float vx[ES][4];
-        bool odd = false;
 #pragma unroll
-        for (int v = 0; v < 4; ++v)
-            vp[v] = V + (int64_t)(k.first + min(16 * wave + 4 * g4 + v, k.len - 1)) * a.row_stride;
-#pragma unroll
-        for (int t = 0; t < ES; ++t) {
+        for (int t = 0; t < ES; ++t)
             o[t] *= sc;
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                vx[t][v] = vp[v][16 * t + c];
-                odd |= !finite(vx[t][v]);
-            }
-        }
-        if (k.node0 < 0 || !__any(odd)) {
+        bool odd = false;
+        if (k.node0 >= 0) {
 #pragma unroll
             for (int v = 0; v < 4; ++v)
 #pragma unroll
                 for (int t = 0; t < ES; ++t)
-                    o[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(vx[t][v], p[v], o[t], 0, 0, 0);
+                    odd |= !finite(vx[v][t / W][t % W]);
+        }
+        if (!__any(odd)) {
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+#pragma unroll
+                for (int t = 0; t < ES; ++t)
+                    o[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(vx[v][t / W][t % W], p[v], o[t], 0, 0, 0);
         } else {
             // an infinity or NaN among the nodes' values: a row that does not
-            // see it must not add 0 times it.  Lane (c, g4) holds elements
-            // 16 t + 4 g4 + u of row c.
+            // see it must not add 0 times it.
             for (int key = 0; key < 16; ++key) {
-                const float *vr = V + (int64_t)(k.first + min(16 * wave + key, k.len - 1)) * a.row_stride + 4 * g4;
+                const float *vr = V + (int64_t)(k.first + min(16 * wave + key, k.len - 1)) * a.row_stride;
                 float pk = p[0];
 #pragma unroll
                 for (int v = 1; v < 4; ++v)
                     pk = (key & 3) == v ? p[v] : pk;
                 pk = __shfl(pk, 16 * (key >> 2) + c, 64);
 #pragma unroll
-                for (int t = 0; t < ES; ++t) {
-                    const f32x4_t w = load4(vr + 16 * t);
+                for (int t = 0; t < ES; ++t)
 #pragma unroll
                     for (int u = 0; u < 4; ++u)
-                        o[t][u] = pk != 0.0f ? fmaf(pk, w[u], o[t][u]) : o[t][u];
-                }
+                        o[t][u] = pk != 0.0f ? fmaf(pk, vr[element(t, u)], o[t][u]) : o[t][u];
             }
         }
     }
@@ -243,7 +265,9 @@ __global__ __launch_bounds__(TA_WAVES * 64) void k_tree_attn_f32(TreeAttnArgs a)
     float *to = tile[wave];
 #pragma unroll
     for (int t = 0; t < ES; ++t)
-        *reinterpret_cast<f32x4_t *>(to + c * OP + 16 * t + 4 * g4) = o[t];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            to[c * OP + element(t, u)] = o[t][u];
     if (g4 == 0)
         ml[wave][c] = make_float2(m_run, l_run);
     __syncthreads();
