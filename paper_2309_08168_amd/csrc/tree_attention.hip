@@ -980,22 +980,24 @@ void launch_join(const TreeAttnArgs &a, hipStream_t s) {
 }
 
 // Rows of a tile and shares of the keys.
-//   float32: tiles of 16 rows, two work-groups per CU (128 rows over 4000 keys, 4
-//   heads of 64: 18.0 us, 21.1 with four).
-//   bfloat16, up to 32 rows of a kv head: the kernel for few, one work-group per
-//   CU, four blocks (one a wave) a share at least (13 rows over 1200 keys, 40
+//   float32: tiles of 16 rows, at most one work-group per CU (us with the join, one
+//   and two per CU: 60 rows of 8 over 300 keys, 8 heads of 128, 14.2 and 25.8; 19
+//   over 1000, 32 heads, 16.0 and 20.6; 4 over 4000, 40 heads, 34.4 and 38.6).
+//   bfloat16, up to 32 rows of a kv head: the kernel for few, at most one work-group
+//   per CU, four blocks (one a wave) a share at least (13 rows over 1200 keys, 40
 //   heads: 10.3 us, 11.3 with two per CU, which halves the keys of a share; one
-//   row over 60000 keys, 8 heads: 43 and 46).
+//   row over 60000 keys, 8 heads: 43 and 46; with a seventh share of 40 heads, 280
+//   work-groups, 9 rows over 2500 take 17.7 in place of 15.7).
 //   More rows: tiles of 64, or of 128 above that (for 72 rows a tile of three waves
 //   took 82.4 us where four, one of which only loads, take 80.3), and one or two
 //   work-groups per CU (mfma_shares).
-// A single share needs no join, which takes a launch: the few-row and float32
-// kernels keep short contexts whole.  us a call, whole and split, among others
-// and alone: 13 rows over 200 keys (40 heads) 8.6 and 24.2, 12.5 and 26.3; over
-// 400 11.1 and 26.9, 12.4 and 26.2; 32 rows over 300 14.2 and 30.0, 12.5 and
-// 28.4; float32, head_dim 64, 5 rows over 300 9.5 and 25.3, 12.7 and 24.9;
-// head_dim 128 over 300 18.8 and 34.5, 12.3 and 27.8.
-constexpr int TA_GROUPS = 512, TA_GROUPS_FEW = 256, TA_CUS = 256, FEW_ROWS = 32;
+// A single share needs no join, whose launch takes a caller 2.4 us: the few-row and
+// float32 kernels keep short contexts whole.  us on the GPU, whole and split: 5 rows
+// over 300 keys (40 heads) 8.9 and 8.6, over 500 11.6 and 8.8; 32 rows over 150 (8
+// heads) 12.1 and 11.2, over 300 14.2 and 11.4; float32, 5 rows over 100 (40 heads)
+// 8.0 and 7.6, over 240 11.2 and 7.8; heads of 64 over 240 7.2 and 6.2, over 500
+// 10.5 and 6.4.
+constexpr int TA_CUS = 256, FEW_ROWS = 32;
 constexpr int whole_blocks(int q_rows) { return q_rows == 16 ? 12 : 6; }  // few rows: blocks of 32 keys
 constexpr int WHOLE_F32 = 6 * 64;                                         // float32: blocks of 64 times head_dim
 
@@ -1037,14 +1039,14 @@ void plan(const sd_kv_layer *kv, int32_t n_heads, int32_t n, int32_t nodes, int3
     const int kb = few ? KB_FEW : KB, step = few ? 4 : 1;
     a->prefix_blocks = (prefix + kb - 1) / kb;
     a->blocks = a->prefix_blocks + (nodes + kb - 1) / kb;
-    const int units = a->q_tiles * a->n_kv_heads, groups = few ? TA_GROUPS_FEW : TA_GROUPS;
+    const int units = a->q_tiles * a->n_kv_heads;
     int want;
     if (few ? a->blocks <= whole_blocks(a->q_rows) : !bf16 && (int64_t)a->blocks * kv->head_dim <= WHOLE_F32)
         want = 1;
     else if (bf16 && !few)
         want = mfma_shares(units, a->blocks);
     else
-        want = std::max(1, std::min((a->blocks + step - 1) / step, (groups + units - 1) / units));
+        want = std::max(1, std::min((a->blocks + step - 1) / step, TA_CUS / units));
     a->per_split = ((a->blocks + want - 1) / want + step - 1) / step * step;
     a->splits = (a->blocks + a->per_split - 1) / a->per_split;
 }
