@@ -378,8 +378,9 @@ size_t sd_tree_attention_workspace(const sd_kv_layer *kv, int32_t n_heads, int32
  * receives the number of nodes on the path (at least 1), the best token of its
  * last node, the path (then -1), and best.  tokens and parents: int32 [n]; an
  * entry of parents outside [0, i) makes node i unreachable.  1 <= n <=
- * SD_TREE_MAX, vocab >= 1.  workspace (16-byte aligned): at least
- * sd_tree_accept_workspace() bytes.  Errors: INVALID_ARG, DEVICE. */
+ * SD_TREE_MAX, 1 <= vocab <= 2^31 - 4097.  workspace (16-byte aligned): at least
+ * sd_tree_accept_workspace() bytes (0 for sizes that are refused).  Errors:
+ * INVALID_ARG, DEVICE. */
 sd_status sd_tree_accept(const float *logits, int64_t ld, int32_t vocab, const int32_t *tokens, const int32_t *parents,
                          int32_t n, int32_t *walk, void *workspace, size_t workspace_bytes, void *hip_stream);
 size_t sd_tree_accept_workspace(int32_t n, int32_t vocab);

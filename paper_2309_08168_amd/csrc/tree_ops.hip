@@ -221,6 +221,15 @@ __device__ __forceinline__ uint64_t best_key(float x, int id) {
     const uint32_t o = (u & 0x80000000u) ? ~u : (u | 0x80000000u);
     return ((uint64_t)o << 32) | (uint32_t)(0x7fffffff - id);
 }
+// Slice `s` of a vocabulary cut into slices of `slice` ids: ids [first, end).
+// (The last slice's first id plus a slice can be past 2^31 - 1.)
+struct Slice {
+    int32_t first, end;
+};
+__host__ __device__ __forceinline__ Slice vocab_slice(int32_t vocab, int32_t slice, int32_t s) {
+    const int32_t first = s * slice, left = vocab - first;
+    return {first, first + (slice < left ? slice : left)};
+}
 __device__ __forceinline__ uint64_t max64(uint64_t a, uint64_t b) { return a > b ? a : b; }
 
 __device__ __forceinline__ uint64_t wave_max64(uint64_t v) {
@@ -250,7 +259,8 @@ constexpr int BEST_LOADS = 4;
 __global__ __launch_bounds__(ACC_THREADS) void k_row_best(AcceptArgs a) {
     __shared__ uint64_t red[ACC_THREADS / 64];
     const int r = blockIdx.y, tid = threadIdx.x;
-    const int i0 = blockIdx.x * a.slice, i1 = min(a.vocab, i0 + a.slice);
+    const Slice ids = vocab_slice(a.vocab, a.slice, blockIdx.x);
+    const int i0 = ids.first, i1 = ids.end;
     const float *x = a.logits + (int64_t)r * a.ld;
     float top = -INFINITY;
     int id = -1;
@@ -352,14 +362,14 @@ __global__ __launch_bounds__(WALK_THREADS) void k_walk(AcceptArgs a) {
 }
 
 // Slices of the vocabulary per row: enough work-groups for eight on every CU,
-// slices of at least 2048 logits (two words a thread).
-int accept_slices(int32_t n, int32_t vocab, int32_t *slice) {
-    int most = (vocab + 2047) / 2048, want = (2048 + n - 1) / n;
-    int slices = most < want ? most : want;
-    if (slices < 1)
-        slices = 1;
-    *slice = ((vocab + slices - 1) / slices + 3) / 4 * 4;
-    return (vocab + *slice - 1) / *slice;
+// slices of at least 2048 logits (two words a thread).  64 bits: the sums pass
+// 2^31 - 1 at the largest vocabularies.
+constexpr int32_t ACC_VOCAB = INT32_MAX - 4096;  // the largest
+int accept_slices(int32_t n, int64_t vocab, int32_t *slice) {
+    const int64_t most = (vocab + 2047) / 2048, want = (2048 + n - 1) / n;
+    const int64_t slices = std::max<int64_t>(1, std::min(most, want));
+    *slice = (int32_t)(((vocab + slices - 1) / slices + 3) / 4 * 4);
+    return (int)((vocab + *slice - 1) / *slice);
 }
 
 // ---------------------------------------------------------------------------
@@ -590,7 +600,7 @@ sd_status sd_rope_append(const sd_rope *rope, const float *qkv, int64_t ld_qkv, 
 }
 
 size_t sd_tree_accept_workspace(int32_t n, int32_t vocab) {
-    if (n < 1 || n > SD_TREE_MAX || vocab < 1)
+    if (n < 1 || n > SD_TREE_MAX || vocab < 1 || vocab > ACC_VOCAB)
         return 0;
     int32_t slice;
     return sizeof(uint64_t) * (size_t)n * accept_slices(n, vocab, &slice);
@@ -602,7 +612,7 @@ sd_status sd_tree_accept(const float *logits, int64_t ld, int32_t vocab, const i
         if (!logits || !tokens || !parents || !walk || (((uintptr_t)logits | (uintptr_t)tokens | (uintptr_t)parents |
                                                          (uintptr_t)walk) & 3))
             return report(SD_ERR_INVALID_ARG, "logits, tokens, parents and walk must be set and aligned");
-        if (n < 1 || n > SD_TREE_MAX || vocab < 1 || vocab > INT32_MAX - 4096 || ld < vocab)
+        if (n < 1 || n > SD_TREE_MAX || vocab < 1 || vocab > ACC_VOCAB || ld < vocab)
             return report(SD_ERR_INVALID_ARG, "a tree has 1 to " + std::to_string(SD_TREE_MAX) +
                                                   " nodes, a row of logits at least one entry and at most ld");
         if (!workspace || !aligned16(workspace) || workspace_bytes < sd_tree_accept_workspace(n, vocab))
@@ -639,6 +649,19 @@ sd_status sd_kv_keep(void *kv, int64_t planes, int64_t plane_stride, int32_t row
         hipLaunchKernelGGL(k_kv_keep, dim3((unsigned)groups), dim3(KEEP_THREADS), 0,
                            reinterpret_cast<hipStream_t>(hip_stream), a);
         return launched("cache move");)
+}
+
+// For the tests: the ids of slice s of a row, as the row maxima take them; returns
+// the number of slices (-1: refused sizes).
+int32_t sdk_accept_slice(int32_t n, int32_t vocab, int32_t s, int32_t *first, int32_t *end) {
+    int32_t slice;
+    if (!sd_tree_accept_workspace(n, vocab))
+        return -1;
+    const int slices = accept_slices(n, vocab, &slice);
+    const Slice ids = vocab_slice(vocab, slice, s);
+    *first = ids.first;
+    *end = ids.end;
+    return slices;
 }
 
 }  // extern "C"

@@ -380,6 +380,19 @@ def test_accept(n, vocab, strided):
     check_accept(logits, tokens, parents, strided)
 
 
+def test_accept_the_largest_vocabulary():
+    """Slices that would end past 2^31 - 1, with larger values right behind the row."""
+    vocab = 2**31 - 4097
+    buf = torch.zeros(vocab + 4096, device="cuda")
+    buf[vocab:] = 2.0
+    root = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for last in (vocab - 1, vocab - 4096, 0):
+        buf[last] = 1.0
+        walk = binding.tree_accept(buf[None, :vocab], root, root - 1)
+        assert walk.tolist() == [1, last, 0, last]
+        buf[last] = 0.0
+
+
 def test_accept_not_a_number_and_infinities():
     nan, inf = float("nan"), float("inf")
     logits = np.array([[nan, 1, 2, nan, 2], [nan] * 5, [-inf] * 5, [inf, nan, inf, 0, 0], [-0.0, 0.0, -1, nan, -0.0],

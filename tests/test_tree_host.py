@@ -186,3 +186,27 @@ def test_null_models_and_caches_are_refused():
     assert lib.sd_kv_cache_keep(None, P, 1) == BAD
     assert lib.sd_model_set_rope(None, None) == BAD
     assert b"model" in lib.sd_last_error()
+
+
+LARGEST = 2**31 - 4097  # of the vocabularies
+
+
+@pytest.mark.parametrize("n", [1, 2, 3, 600, 1024])
+@pytest.mark.parametrize("vocab", [1, 2047, 2049, 32000, 2146435074, 2147475456, 2147475457, LARGEST])
+def test_slices_of_a_row_cover_the_vocabulary(n, vocab):
+    """Each id is in one slice, also where a slice would end past 2^31 - 1."""
+    lib, first, end = binding.load(), ctypes.c_int32(), ctypes.c_int32()
+    slices = lib.sdk_accept_slice(n, vocab, 0, ctypes.byref(first), ctypes.byref(end))
+    assert 1 <= slices <= 2048 and lib.sd_tree_accept_workspace(n, vocab) == 8 * n * slices
+    at = 0
+    for s in range(slices):
+        lib.sdk_accept_slice(n, vocab, s, ctypes.byref(first), ctypes.byref(end))
+        assert first.value == at and at < end.value <= vocab
+        at = end.value
+    assert at == vocab
+
+
+def test_the_walk_needs_no_workspace_for_a_vocabulary_that_it_refuses():
+    for vocab in (0, -1, LARGEST + 1, 2**31 - 1):
+        assert binding.load().sd_tree_accept_workspace(1, vocab) == 0
+        assert binding.load().sd_tree_accept(P, 1 << 40, vocab, P, P, 1, P, P, 1 << 20, None) == BAD
