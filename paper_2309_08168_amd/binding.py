@@ -469,6 +469,7 @@ def rope(base: float = 10000.0, rotary_dim: int = 128, layout: str = "half", sca
          gain: float = 0.0) -> sd_rope:
     """A rotary form (sd_rope): layout "half" or "interleaved", scaling "none",
     "linear", "ntk" or "yarn"; gain 0 is the form's own."""
+    _int32(rotary_dim, original_context)
     return sd_rope(base, factor, gain, beta_fast, beta_slow, rotary_dim, ROPE_LAYOUTS[layout], ROPE_SCALINGS[scaling],
                    original_context)
 
@@ -529,6 +530,7 @@ def _layer(k, v):
         _refuse("k and v are [n_kv_heads, capacity, head_dim], float32 or bfloat16, of one type and one set of strides, "
                 "rows contiguous")
     heads, cap, d = shape
+    _int32(heads, cap, d)
     return sd_kv_layer(k.data_ptr(), v.data_ptr(), stride[0], stride[1], heads, cap, d,
                        SD_BF16 if dtype is _bf16 else SD_F32), heads, d
 
@@ -582,10 +584,10 @@ def rope_append(form: sd_rope, qkv, k, v, slot: int, n_heads: int, positions=Non
     as in kv_layer, rows stored at slot ..; positions int32 [n] or None: pos0 ..
     Returns the rotated queries, float32 [n, n_heads, head_dim]."""
     layer, kvh, d = _layer(k, v)
-    _int32(slot, pos0)
     if qkv.ndim != 2:
         _refuse("qkv is [n, (n_heads + 2 n_kv_heads) head_dim]")
     n = qkv.shape[0]
+    _int32(slot, pos0, n, n_heads)
     ld = _rows2(qkv, n, (n_heads + 2 * kvh) * d, "qkv")
     if positions is None:
         at, dev = None, _device(qkv, k, v)
@@ -611,11 +613,11 @@ def tree_attention(q, k, v, prefix: int, mask=None, scale: float = 0.0, out=None
     0 .. r), scale 0: 1 / sqrt(head_dim).  Returns out, like q; workspace: a tensor of
     at least tree_attention_workspace() bytes (else one is allocated)."""
     layer, _, d = _layer(k, v)
-    _int32(prefix)
     shape = q.shape
     if len(shape) != 3:
         _refuse("q is [n, n_heads, head_dim]")
     n, h, _ = shape
+    _int32(prefix, n, h)
     ld = _rows3(q, n, h, d, "q")
     if mask is None:
         bits, dev = None, _device(q, k, v)
@@ -645,6 +647,7 @@ def tree_attention(q, k, v, prefix: int, mask=None, scale: float = 0.0, out=None
 
 def tree_attention_workspace(k, v, n_heads: int, n: int, prefix: int) -> int:
     """Bytes of workspace tree_attention needs for these sizes."""
+    _int32(n_heads, n, prefix)
     return int(load().sd_tree_attention_workspace(kv_layer(k, v), n_heads, n, prefix))
 
 
@@ -659,6 +662,7 @@ def tree_accept(logits, tokens, parents, walk=None, workspace=None):
     if len(shape) != 2:
         _refuse("logits is [n, vocab]")
     n, vocab = shape
+    _int32(n, vocab)
     ld = _rows2(logits, n, vocab, "logits")
     tok, par = _words(tokens, n, "tokens"), _words(parents, n, "parents")
     dev = _device(logits, tokens, parents)
@@ -684,6 +688,7 @@ def tree_accept(logits, tokens, parents, walk=None, workspace=None):
 
 def tree_accept_workspace(n: int, vocab: int) -> int:
     """Bytes of workspace tree_accept needs for these sizes."""
+    _int32(n, vocab)
     return int(load().sd_tree_accept_workspace(n, vocab))
 
 
@@ -697,11 +702,11 @@ def kv_keep(kv, base: int, walk):
         _refuse("kv is a contiguous [..., capacity, head_dim]")
     n = (walk.numel() - 2) >> 1
     at = _words(walk, 2 + 2 * n, "walk")
+    cap, row = shape[-2], shape[-1] * kv.element_size()
+    _int32(base, cap, row, n)
     dev = _device(kv, walk)
     if dev != _current():
         return _elsewhere(dev, kv_keep, kv, base, walk)
-    _int32(base)
-    cap, row = shape[-2], shape[-1] * kv.element_size()
     planes = kv.numel() // (cap * shape[-1]) if kv.numel() else 0
     status = _lib.sd_kv_keep(kv.data_ptr(), planes, cap * row, row, cap, base, at, n, _raw_stream(dev))
     if status:

@@ -210,3 +210,34 @@ def test_the_walk_needs_no_workspace_for_a_vocabulary_that_it_refuses():
     for vocab in (0, -1, LARGEST + 1, 2**31 - 1):
         assert binding.load().sd_tree_accept_workspace(1, vocab) == 0
         assert binding.load().sd_tree_accept(P, 1 << 40, vocab, P, P, 1, P, P, 1 << 20, None) == BAD
+
+
+def test_sizes_past_32_bits_are_refused_and_not_cut():
+    """(a meta tensor has a shape and no memory)"""
+    torch = pytest.importorskip("torch")
+    far = 2**32
+
+    def meta(*shape, dtype=torch.float32):
+        return torch.empty(shape, dtype=dtype, device="meta")
+
+    k, long, many = meta(2, 64, 64), meta(2, far + 64, 64), meta(far + 2, 64, 64)
+    i32, form = torch.int32, binding.rope(rotary_dim=64)
+    for bad in (lambda: binding.kv_layer(long, long), lambda: binding.kv_layer(many, many),
+                lambda: binding.tree_attention_workspace(long, long, 4, 4, 10),
+                lambda: binding.tree_attention_workspace(k, k, far + 4, 4, 10),
+                lambda: binding.tree_attention_workspace(k, k, 4, far + 4, 10),
+                lambda: binding.tree_attention_workspace(k, k, 4, 4, far + 10),
+                lambda: binding.tree_attention(meta(far + 3, 4, 64), k, k, 0),
+                lambda: binding.tree_attention(meta(3, far + 4, 64), k, k, 0),
+                lambda: binding.rope_append(form, meta(far + 3, 8 * 64), k, k, 0, 4),
+                lambda: binding.rope_append(form, meta(3, (far + 8) * 64), k, k, 0, far + 4),
+                lambda: binding.tree_accept(meta(3, far + 5), meta(3, dtype=i32), meta(3, dtype=i32)),
+                lambda: binding.tree_accept(meta(far + 3, 5), meta(far + 3, dtype=i32), meta(far + 3, dtype=i32)),
+                lambda: binding.tree_accept_workspace(far + 3, 5), lambda: binding.tree_accept_workspace(3, far + 5),
+                lambda: binding.kv_keep(long, 0, meta(8, dtype=i32)),
+                lambda: binding.kv_keep(meta(2, 16, far + 16), 0, meta(8, dtype=i32)),
+                lambda: binding.kv_keep(k, 0, meta(2 * far + 8, dtype=i32)),
+                lambda: binding.rope(rotary_dim=far + 64), lambda: binding.rope(original_context=far + 4096)):
+        with pytest.raises(binding.SDError, match="32-bit") as e:
+            bad()
+        assert e.value.status == BAD
