@@ -322,7 +322,8 @@ typedef struct {
  *           beta_slow) clamped to [0, 1], f_i (g + (1 - g) / s); cosines and
  *           sines times 0.1 ln s + 1.
  * A gain other than 0 replaces the factor on cosines and sines (1 without
- * YARN). */
+ * YARN).  base is at least 1e-9; the base that NTK takes, and a gain in float32,
+ * are finite. */
 typedef enum { SD_ROPE_HALF = 0, SD_ROPE_INTERLEAVED = 1 } sd_rope_layout;
 typedef enum { SD_ROPE_UNSCALED = 0, SD_ROPE_LINEAR = 1, SD_ROPE_NTK = 2, SD_ROPE_YARN = 3 } sd_rope_scaling;
 typedef struct {

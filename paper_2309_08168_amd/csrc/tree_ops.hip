@@ -61,12 +61,13 @@ struct RopeArgs {
     int32_t slot;
 };
 
+double scaled_base(const sd_rope &r) {
+    return r.scaling == SD_ROPE_NTK ? r.base * std::pow(r.factor, (double)r.rotary_dim / (r.rotary_dim - 2)) : r.base;
+}
+
 // The rotary part of the arguments, for a checked form.
 void rope_form(const sd_rope &r, RopeArgs *out) {
-    double base = r.base;
-    if (r.scaling == SD_ROPE_NTK)
-        base *= std::pow(r.factor, (double)r.rotary_dim / (r.rotary_dim - 2));
-    out->step = -2.0 * std::log2(base) / r.rotary_dim;
+    out->step = -2.0 * std::log2(scaled_base(r)) / r.rotary_dim;
     out->yarn = r.scaling == SD_ROPE_YARN;
     out->inv_factor = r.scaling == SD_ROPE_LINEAR || out->yarn ? 1.0 / r.factor : 1.0;
     out->turns = r.original_context / 6.28318530717958647693;
@@ -552,13 +553,14 @@ sd_status check_rope(const sd_rope *r, int32_t head_dim) {
     if ((r->layout != SD_ROPE_HALF && r->layout != SD_ROPE_INTERLEAVED) || r->scaling < SD_ROPE_UNSCALED ||
         r->scaling > SD_ROPE_YARN)
         return report(SD_ERR_INVALID_ARG, "unknown rotary layout or scaling");
-    if (!(r->base > 0.0) || !std::isfinite(r->base) || !std::isfinite(r->gain))
-        return report(SD_ERR_INVALID_ARG, "base must be positive, base and gain finite");
+    // (positions reach 2^31: with a frequency of at most 1e9 an angle's quarter turns fit 64 bits)
+    if (!(r->base >= 1e-9) || !std::isfinite(r->base) || !std::isfinite((float)r->gain))
+        return report(SD_ERR_INVALID_ARG, "base must be at least 1e-9, base and gain finite (gain in float32)");
     const bool scaled = r->scaling != SD_ROPE_UNSCALED;
     if (scaled && (!(r->factor >= 1.0) || !std::isfinite(r->factor)))
         return report(SD_ERR_INVALID_ARG, "the factor of a scaled rotary embedding must be >= 1 and finite");
-    if (r->scaling == SD_ROPE_NTK && r->rotary_dim < 4)
-        return report(SD_ERR_INVALID_ARG, "NTK scaling needs rotary_dim >= 4");
+    if (r->scaling == SD_ROPE_NTK && (r->rotary_dim < 4 || !std::isfinite(scaled_base(*r))))
+        return report(SD_ERR_INVALID_ARG, "NTK scaling needs rotary_dim >= 4 and a finite scaled base");
     if (r->scaling == SD_ROPE_YARN && (!(r->beta_slow >= 0.0) || !(r->beta_fast > r->beta_slow) ||
                                        !std::isfinite(r->beta_fast) || r->original_context < 1))
         return report(SD_ERR_INVALID_ARG, "YARN needs beta_fast > beta_slow >= 0 and original_context >= 1");
@@ -566,10 +568,7 @@ sd_status check_rope(const sd_rope *r, int32_t head_dim) {
 }
 
 double rope_frequency(const sd_rope &r, int32_t i) {
-    double base = r.base;
-    if (r.scaling == SD_ROPE_NTK)
-        base *= std::pow(r.factor, (double)r.rotary_dim / (r.rotary_dim - 2));
-    const double f = std::pow(base, -2.0 * (double)i / (double)r.rotary_dim);
+    const double f = std::pow(scaled_base(r), -2.0 * (double)i / (double)r.rotary_dim);
     if (r.scaling == SD_ROPE_LINEAR)
         return f / r.factor;
     if (r.scaling == SD_ROPE_YARN) {

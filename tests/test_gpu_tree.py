@@ -109,6 +109,13 @@ def test_rope_far_and_negative_positions():
     check_rope(4, 2, 2, 128, "f32", dict(rotary_dim=128), [2**31 - 1, 2**30, -1, -70000])
 
 
+@pytest.mark.parametrize("form", [
+    dict(scaling="ntk", factor=1e150, rotary_dim=4), dict(gain=3e37), dict(base=1e308, rotary_dim=32),
+    dict(scaling="linear", factor=1e308), dict(scaling="yarn", factor=1e308, gain=1.0)], ids=str)
+def test_rope_forms_at_the_limits(form):
+    check_rope(3, 2, 1, 64, "f32", {"rotary_dim": 64, **form}, [0, 1, 2**31 - 1])
+
+
 # ----------------------------------------------------------------------------
 # tree_attention
 

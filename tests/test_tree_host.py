@@ -86,6 +86,21 @@ def test_rope_forms_refused(form):
     assert rope_call(form=binding.rope(**form)) == BAD
 
 
+@pytest.mark.parametrize("form", [
+    dict(scaling="ntk", factor=1e300, base=1e10), dict(scaling="ntk", factor=1e160, rotary_dim=4), dict(gain=1e39),
+    dict(gain=-1e39), dict(base=9e-10), dict(base=5e-324)], ids=str)
+def test_rope_forms_whose_numbers_overflow_are_refused(form):
+    """(slot 61 is refused too, but only further on)"""
+    assert rope_call(form=binding.rope(**form), slot=61) == BAD
+
+
+@pytest.mark.parametrize("form", [
+    dict(scaling="ntk", factor=1e150, rotary_dim=4), dict(gain=3e38), dict(base=1e-9), dict(base=1e308),
+    dict(scaling="linear", factor=1e308), dict(scaling="yarn", factor=1e308)], ids=str)
+def test_rope_forms_at_the_limits_are_taken(form):
+    assert rope_call(form=binding.rope(**form), slot=61) == FULL
+
+
 def test_position_major_layers_are_taken():
     """[capacity][n_kv_heads][head_dim]: refused only further on."""
     assert rope_call(kv=layer(head_stride=128, row_stride=256), slot=61) == FULL
