@@ -298,7 +298,9 @@ __global__ __launch_bounds__(TA_WAVES * 64, 2) void k_tree_attn_f32(TreeAttnArgs
 // GHz); 61 rows over 3001 keys, 32 heads (64) 21 + 4 us.
 
 // A maximum that grows by no more than this (in log2) does not rescale the sums:
-// weights then reach 2^8 and not 1, which float32 sums do not mind.
+// weights then reach 2^8 and not 1, which float32 sums do not mind.  A row decides
+// by its own scores, so that its bits do not follow from what other rows of its
+// wave see; the wave passes over the rescale where no row asks for it.
 constexpr float SLACK = 8.0f;
 
 __device__ __forceinline__ f32x16_t mfma32(u32x4_t a, u32x4_t b, f32x16_t c) {
@@ -522,9 +524,10 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_tree_attn_mfma(TreeAttnArgs
                 const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
                 mx = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
             }
-            if (__any(mx > m_run + SLACK)) {
+            const bool grows = mx > m_run + SLACK;
+            if (__any(grows)) {
                 // (a row that has seen no key yet keeps zeros)
-                const float m_new = fmaxf(m_run, mx);
+                const float m_new = grows ? mx : m_run;
                 const float sc = m_run == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run - m_new);
                 l_run *= sc;
 #pragma unroll
@@ -831,8 +834,9 @@ __global__ __launch_bounds__(256, QT == 1 || D < 128 ? 2 : 1) void k_tree_attn_f
                 mx = fmaxf(mx, p[u]);
             mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
             mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-            if (__any(mx > m_run[i] + SLACK)) {
-                const float m_new = fmaxf(m_run[i], mx);
+            const bool grows = mx > m_run[i] + SLACK;
+            if (__any(grows)) {
+                const float m_new = grows ? mx : m_run[i];
                 const float sc = m_run[i] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run[i] - m_new);
                 l_run[i] *= sc;
 #pragma unroll

@@ -287,6 +287,47 @@ def test_attention_ignores_what_is_hidden(dtype, bad, heads, n, prefix):
     assert not torch.isfinite(got[one, :, 7]).any() and torch.isfinite(got[one, :, :7]).all()
 
 
+# rows of a kv head: up to 16, 17 to 32, 33 to 64, more
+ROWS = [(12, 1), (12, 2), (20, 2), (40, 4)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16"])
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
+@pytest.mark.parametrize("n,group", ROWS)
+def test_rows_keep_their_bits_whatever_they_do_not_see(dtype, d, n, group):
+    """A node's key and value, and its rows' queries, changed: the rows that do
+    not see it keep every bit, next to rows of their tile that do.  (64 kv heads,
+    so that the nodes' block is not the first that a wave takes.)"""
+    prefix, kvh = 1000, 64
+    see = tree(n)
+    node = max(range(1, n), key=lambda j: min(see[:, j].sum(), n - see[:, j].sum()))
+    sees = torch.tensor(see[:, node], device="cuda")
+    assert 0 < int(sees.sum()) < n
+    g = torch.Generator(device="cuda").manual_seed(n + d)
+    k, v = (torch.randn(kvh, prefix + n, d, device="cuda", generator=g).to(TYPES[dtype]) for _ in range(2))
+    q = torch.randn(n, kvh * group, d, device="cuda", generator=g)
+    mask = torch.tensor(T.pack(see).astype(np.int64), device="cuda")
+    before = binding.tree_attention(q, k, v, prefix, mask=mask)
+    k0, v0, q0 = k[:, prefix + node].clone(), v[:, prefix + node].clone(), q[sees].clone()
+
+    def same():
+        return torch.equal(binding.tree_attention(q, k, v, prefix, mask=mask)[~sees], before[~sees])
+
+    k[:, prefix + node] *= 60  # scores of some hundred, far above the others
+    assert same()
+    k[:, prefix + node] = k0
+    q[sees] *= 60
+    assert same()
+    q[sees] = q0
+    for bad in (float("nan"), float("inf"), float("-inf")):
+        v[:, prefix + node, ::5] = bad
+        assert same()
+        k[:, prefix + node, ::7] = bad
+        assert same()
+        k[:, prefix + node], v[:, prefix + node] = k0, v0
+    assert torch.equal(binding.tree_attention(q, k, v, prefix, mask=mask), before)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("order", ["positions", "padded"])
 def test_attention_strides(dtype, order):
