@@ -359,9 +359,9 @@ sd_status sd_rope_append(const sd_rope *rope, const float *qkv, int64_t ld_qkv, 
  * or the nodes 0 .. r when mask is NULL.  Scores are scaled by scale (0: 1 /
  * sqrt(head_dim)); sums are float32.  out [n][n_heads head_dim] (float32, rows
  * ld_out apart, not overlapping q).  A row that sees nothing gives zeros; what
- * a row does not see never touches its result, whatever it holds; what it sees
- * is finite, or its result may be NaN.  workspace
- * (16-byte aligned) holds at least sd_tree_attention_workspace() bytes for these
+ * a row does not see changes no bit of its result, whatever it holds, and neither
+ * do the other rows' queries; what it sees is finite, or its result may be NaN.
+ * workspace (16-byte aligned) holds at least sd_tree_attention_workspace() bytes for these
  * sizes and belongs to the call until it has run.  1 <= n <= SD_TREE_MAX, 0 <=
  * prefix, prefix + n <= capacity.  The same inputs give the same bits.  Errors:
  * INVALID_ARG, CAPACITY, DEVICE. */

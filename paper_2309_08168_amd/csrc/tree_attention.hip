@@ -235,15 +235,10 @@ __global__ __launch_bounds__(TA_WAVES * 64, 2) void k_tree_attn_f32(TreeAttnArgs
                 for (int t = 0; t < ES; ++t)
                     odd |= !finite(vx[v][t / W][t % W]);
         }
-        if (!__any(odd)) {
-#pragma unroll
-            for (int v = 0; v < 4; ++v)
-#pragma unroll
-                for (int t = 0; t < ES; ++t)
-                    o[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(vx[v][t / W][t % W], p[v], o[t], 0, 0, 0);
-        } else {
-            // an infinity or NaN among the nodes' values: a row that does not
-            // see it must not add 0 times it.
+        if (__any(odd)) {
+            // An infinity or NaN among the nodes' values: a row that does not
+            // see it must not add 0 times it.  They are taken out of the
+            // operands, and added here, from memory, where they belong.
             for (int key = 0; key < 16; ++key) {
                 const float *vr = V + (int64_t)(k.first + min(16 * wave + key, k.len - 1)) * a.row_stride;
                 float pk = p[0];
@@ -254,10 +249,23 @@ __global__ __launch_bounds__(TA_WAVES * 64, 2) void k_tree_attn_f32(TreeAttnArgs
 #pragma unroll
                 for (int t = 0; t < ES; ++t)
 #pragma unroll
-                    for (int u = 0; u < 4; ++u)
-                        o[t][u] = pk != 0.0f ? fmaf(pk, vr[element(t, u)], o[t][u]) : o[t][u];
+                    for (int u = 0; u < 4; ++u) {
+                        const float x = vr[element(t, u)];
+                        if (pk != 0.0f && !finite(x))
+                            o[t][u] = fmaf(pk, x, o[t][u]);
+                    }
             }
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+#pragma unroll
+                for (int t = 0; t < ES; ++t)
+                    vx[v][t / W][t % W] = finite(vx[v][t / W][t % W]) ? vx[v][t / W][t % W] : 0.0f;
         }
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+#pragma unroll
+            for (int t = 0; t < ES; ++t)
+                o[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(vx[v][t / W][t % W], p[v], o[t], 0, 0, 0);
     }
     l_run += __shfl_xor(l_run, 16, 64);
     l_run += __shfl_xor(l_run, 32, 64);

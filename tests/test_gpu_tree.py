@@ -291,7 +291,7 @@ def test_attention_ignores_what_is_hidden(dtype, bad, heads, n, prefix):
 ROWS = [(12, 1), (12, 2), (20, 2), (40, 4)]
 
 
-@pytest.mark.parametrize("dtype", ["bf16"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("d", [16, 32, 64, 128])
 @pytest.mark.parametrize("n,group", ROWS)
 def test_rows_keep_their_bits_whatever_they_do_not_see(dtype, d, n, group):
