@@ -329,6 +329,69 @@ def test_rows_keep_their_bits_whatever_they_do_not_see(dtype, d, n, group):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
+@pytest.mark.parametrize("n,group", ROWS)
+@pytest.mark.parametrize("prefix", [0, 70])
+def test_attention_any_mask_in_every_tile(dtype, d, n, group, prefix):
+    """Bits before and behind the diagonal, and rows without any, which see the
+    prefix or nothing."""
+    see = np.random.default_rng(n + d).random((n, n)) < 0.3
+    see[2] = see[n - 1] = False
+    got = check_attention(n, 2 * group, 2, d, dtype, prefix, see)
+    if prefix == 0:
+        assert (got[2] == 0).all() and (got[n - 1] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
+@pytest.mark.parametrize("n,group", ROWS)
+@pytest.mark.parametrize("prefix", [0, 1100])
+def test_attention_with_hidden_nan_in_every_tile(dtype, d, n, group, prefix):
+    """A node that no row sees, and the cache behind the tree, hold NaN and
+    infinities; then a value that is seen by some rows is infinite: those rows
+    receive it, and only there."""
+    see = tree(n)
+    see[:, 3] = False
+
+    def spoil(k, v):
+        k[:, prefix + 3] = v[:, prefix + 3, ::2] = float("nan")
+        v[:, prefix + 3, 1::2] = float("-inf")
+        k[:, prefix + n:] = v[:, prefix + n:] = float("inf")
+
+    clean = check_attention(n, 2 * group, 2, d, dtype, prefix, see, spoil=spoil)
+    seen = torch.tensor(see[:, 5], device="cuda")
+    assert 0 < int(seen.sum()) < n
+
+    def infinite(k, v):
+        v[:, prefix + 5, 3] = v[:, prefix + 5, d - 2] = float("inf")
+
+    rng = np.random.default_rng(31 * n + prefix)  # (the inputs of check_attention)
+    k, v = layers(rng, 2, prefix + n + 3, d, dtype)
+    q = torch.tensor(rng.standard_normal((n, 2 * group, d)), dtype=torch.float32, device="cuda")
+    spoil(k, v)
+    infinite(k, v)
+    got = binding.tree_attention(q, k, v, prefix, mask=torch.tensor(T.pack(see).astype(np.int64), device="cuda"))
+    there = torch.zeros_like(got, dtype=torch.bool)
+    there[seen, :, 3] = there[seen, :, d - 2] = True
+    assert (got[there] == float("inf")).all() and torch.equal(got[~there], clean[~there])
+
+
+@pytest.mark.parametrize("dtype,n,kvh,group,d", [
+    ("f32", 512, 1, 1, 128), ("f32", 1000, 2, 1, 32), ("bf16", 500, 1, 1, 128), ("bf16", 500, 1, 1, 16), ("bf16", 1024, 1, 2, 64)])
+def test_rows_that_see_nothing_in_several_shares(dtype, n, kvh, group, d):
+    """No prefix, and nodes enough that their keys are split: rows that see
+    nothing in one share, and in none."""
+    k = torch.empty(kvh, n + 3, d, dtype=TYPES[dtype], device="cuda")
+    assert binding.tree_attention_workspace(k, k, kvh * group, n, 0) > 0
+    see = tree(n, back=2)
+    see[7] = see[n - 1] = see[n // 2] = False
+    see[n - 2] = False
+    see[n - 2, n - 2] = True  # only the last share has a key of it
+    got = check_attention(n, kvh * group, kvh, d, dtype, 0, see)
+    assert (got[[7, n // 2, n - 1]] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("order", ["positions", "padded"])
 def test_attention_strides(dtype, order):
     check_attention(21, 6, 3, 64, dtype, 150, tree(21), order=order, strided=True)
