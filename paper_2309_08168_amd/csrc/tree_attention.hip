@@ -992,9 +992,7 @@ void launch_join(const TreeAttnArgs &a, hipStream_t s) {
 }
 
 // Rows of a tile and shares of the keys.
-//   float32: tiles of 16 rows, at most one work-group per CU (us with the join, one
-//   and two per CU: 60 rows of 8 over 300 keys, 8 heads of 128, 14.2 and 25.8; 19
-//   over 1000, 32 heads, 16.0 and 20.6; 4 over 4000, 40 heads, 34.4 and 38.6).
+//   float32: tiles of 16 rows, shares by their cost (f32_shares).
 //   bfloat16, up to 32 rows of a kv head: the kernel for few, at most one work-group
 //   per CU, four blocks (one a wave) a share at least (13 rows over 1200 keys, 40
 //   heads: 10.3 us, 11.3 with two per CU, which halves the keys of a share; one
@@ -1008,10 +1006,10 @@ void launch_join(const TreeAttnArgs &a, hipStream_t s) {
 // over 300 keys (40 heads) 8.9 and 8.6, over 500 11.6 and 8.8; 32 rows over 150 (8
 // heads) 12.1 and 11.2, over 300 14.2 and 11.4; float32, 5 rows over 100 (40 heads)
 // 8.0 and 7.6, over 240 11.2 and 7.8; heads of 64 over 240 7.2 and 6.2, over 500
-// 10.5 and 6.4.
+// 10.5 and 6.4; 13 rows (8 heads) of 16 over 700 9.4 and 7.9, over 1400 15.6 and 7.9.
 constexpr int TA_CUS = 256, FEW_ROWS = 32;
 constexpr int whole_blocks(int q_rows) { return q_rows == 16 ? 12 : 6; }  // few rows: blocks of 32 keys
-constexpr int WHOLE_F32 = 6 * 64;                                         // float32: blocks of 64 times head_dim
+constexpr int WHOLE_F32 = 6 * 64;  // float32: blocks of 64 times head_dim, which counts as 32 at least
 
 // Shares of the tiles of more rows.  Two work-groups per CU hide a part of each
 // other's softmax, about a seventh of a long share; every work-group costs its
@@ -1026,6 +1024,31 @@ int mfma_shares(int units, int blocks) {
         const int shares = std::max(1, std::min(blocks, groups / units));
         const int per = (blocks + shares - 1) / shares, w = (units * shares + TA_CUS - 1) / TA_CUS;
         const double cost = w * (per * (w == 1 ? 7.0 / 6.0 : 1.0) + 2.0) + (shares > 1 ? 1.7 : 0.0);
+        if (cost < least) {
+            least = cost;
+            best = shares;
+        }
+    }
+    return best;
+}
+
+// Shares of float32 tiles, in us: a block takes 0.45 + 0.0115 D; another
+// work-group on the busiest CU costs more than the first did, since every tile reads
+// the whole share by itself; a join costs its start and the partial results.  us
+// with the join, by shares: 160 tiles over 4000 keys (heads of 128) one 109-117,
+// two 126, three 106, six 102; 136 113, 121, 93, 97; 280 over 4000 233, 205, 188,
+// 179; 160 over 1000 31.4, 40.7, 34.7, 37.9; 240 over 4000 137, 154, 176, 151; 40
+// over 4000, six 32.3, 13 37.4; heads of 16, 160 over 4000, one 50.7, three 28.0.
+int f32_shares(int units, int blocks, int D) {
+    const double block = 0.45 + 0.0115 * D;
+    int best = 1;
+    double least = INFINITY;
+    for (int c : {1, TA_CUS / units, 2 * TA_CUS / units, (2 * TA_CUS + units - 1) / units}) {
+        const int want = std::max(1, std::min(blocks, c)), per = (blocks + want - 1) / want;
+        const int shares = (blocks + per - 1) / per;
+        const int64_t groups = (int64_t)units * shares, w = (groups + TA_CUS - 1) / TA_CUS;
+        const double cost = block * per * (1.0 + 1.2 * (double)(w - 1)) +
+                            (shares > 1 ? 1.0 + 6.0 * (double)groups * D / (TA_CUS * 128) : 0.0);
         if (cost < least) {
             least = cost;
             best = shares;
@@ -1053,9 +1076,12 @@ void plan(const sd_kv_layer *kv, int32_t n_heads, int32_t n, int32_t nodes, int3
     a->blocks = a->prefix_blocks + (nodes + kb - 1) / kb;
     const int units = a->q_tiles * a->n_kv_heads;
     int want;
-    if (few ? a->blocks <= whole_blocks(a->q_rows) : !bf16 && (int64_t)a->blocks * kv->head_dim <= WHOLE_F32)
+    if (few ? a->blocks <= whole_blocks(a->q_rows)
+            : !bf16 && (int64_t)a->blocks * std::max(32, kv->head_dim) <= WHOLE_F32)
         want = 1;
-    else if (bf16 && !few)
+    else if (!bf16)
+        want = f32_shares(units, a->blocks, kv->head_dim);
+    else if (!few)
         want = mfma_shares(units, a->blocks);
     else
         want = std::max(1, std::min((a->blocks + step - 1) / step, TA_CUS / units));

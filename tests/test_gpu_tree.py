@@ -173,6 +173,12 @@ def test_attention_causal(dtype, n, prefix):
     assert torch.equal(chain, same)
 
 
+@pytest.mark.parametrize("d,n,kvh,prefix", [(128, 80, 32, 1500), (16, 130, 20, 2500), (64, 260, 10, 2000), (32, 30, 140, 1300)])
+def test_float32_tiles_for_more_than_half_the_cus(d, n, kvh, prefix):
+    """160 to 280 tiles of 16 rows over a long context."""
+    check_attention(n, kvh, kvh, d, "f32", prefix, tree(n))
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n", [1, 40, 1024])
 def test_attention_long(dtype, n):

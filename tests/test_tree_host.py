@@ -256,3 +256,27 @@ def test_sizes_past_32_bits_are_refused_and_not_cut():
         with pytest.raises(binding.SDError, match="32-bit") as e:
             bad()
         assert e.value.status == BAD
+
+
+def f32_shares(rows, kvh, d, prefix):
+    """Shares of the keys that a float32 layer's attention takes, by its workspace:
+    an output, a maximum and a sum per share, row and head."""
+    cap = prefix + rows
+    kv = layer(head_stride=cap * d, row_stride=d, n_kv_heads=kvh, capacity=cap, head_dim=d, dtype=binding.SD_F32)
+    nbytes = binding.load().sd_tree_attention_workspace(ctypes.byref(kv), kvh, rows, prefix)
+    assert nbytes % (4 * rows * kvh * (d + 2)) == 0
+    return nbytes // (4 * rows * kvh * (d + 2)) or 1
+
+
+@pytest.mark.parametrize("rows,kvh,d,prefix,least,most", [
+    # more tiles than half the CUs, long contexts: split, so that no CU idles over the whole of it
+    (61, 34, 128, 4000, 3, 8), (64, 40, 128, 4000, 3, 8), (80, 32, 128, 4000, 3, 8), (112, 40, 128, 4000, 2, 8),
+    (80, 32, 64, 4000, 3, 8), (80, 32, 32, 4000, 3, 12), (80, 32, 16, 4000, 3, 12), (80, 32, 16, 1400, 3, 12),
+    # small heads: a long context is not short because its rows are
+    (13, 2, 16, 1400, 6, 24), (13, 8, 16, 1400, 6, 24), (13, 8, 32, 1400, 6, 24),
+    # tiles for every CU, or short contexts: whole
+    (96, 40, 128, 4000, 1, 1), (64, 40, 128, 1000, 1, 1), (60, 40, 128, 300, 1, 1), (5, 4, 64, 30, 1, 1), (5, 40, 128, 100, 1, 1),
+    # few tiles: one work-group per CU
+    (4, 40, 128, 4000, 5, 6), (19, 32, 128, 1000, 4, 5)])
+def test_float32_shares(rows, kvh, d, prefix, least, most):
+    assert least <= f32_shares(rows, kvh, d, prefix) <= most
