@@ -469,7 +469,8 @@ def rope(base: float = 10000.0, rotary_dim: int = 128, layout: str = "half", sca
          gain: float = 0.0) -> sd_rope:
     """A rotary form (sd_rope): layout "half" or "interleaved", scaling "none",
     "linear", "ntk" or "yarn"; gain 0 is the form's own."""
-    _int32(rotary_dim, original_context)
+    if not (0 <= rotary_dim <= _INT32_MAX and 0 <= original_context <= _INT32_MAX):
+        _int32(rotary_dim, original_context)
     return sd_rope(base, factor, gain, beta_fast, beta_slow, rotary_dim, ROPE_LAYOUTS[layout], ROPE_SCALINGS[scaling],
                    original_context)
 
@@ -530,7 +531,8 @@ def _layer(k, v):
         _refuse("k and v are [n_kv_heads, capacity, head_dim], float32 or bfloat16, of one type and one set of strides, "
                 "rows contiguous")
     heads, cap, d = shape
-    _int32(heads, cap, d)
+    if heads > _INT32_MAX or cap > _INT32_MAX or d > _INT32_MAX:
+        _int32(heads, cap, d)
     return sd_kv_layer(k.data_ptr(), v.data_ptr(), stride[0], stride[1], heads, cap, d,
                        SD_BF16 if dtype is _bf16 else SD_F32), heads, d
 
@@ -564,10 +566,13 @@ def _words(t, n: int, what: str) -> int:
     return t.data_ptr()
 
 
+_INT32_MAX = 0x7fffffff
+
+
 def _int32(*values: int):
     """Refuses what ctypes would cut to 32 bits."""
     for value in values:
-        if not -0x80000000 <= value <= 0x7fffffff:
+        if not -0x80000000 <= value <= _INT32_MAX:
             _refuse(f"{value} is outside the 32-bit integers")
 
 
@@ -662,7 +667,8 @@ def tree_accept(logits, tokens, parents, walk=None, workspace=None):
     if len(shape) != 2:
         _refuse("logits is [n, vocab]")
     n, vocab = shape
-    _int32(n, vocab)
+    if n > _INT32_MAX or vocab > _INT32_MAX:
+        _int32(n, vocab)
     ld = _rows2(logits, n, vocab, "logits")
     tok, par = _words(tokens, n, "tokens"), _words(parents, n, "parents")
     dev = _device(logits, tokens, parents)
