@@ -86,6 +86,33 @@ def test_tree_forward(name, n, prefix):
     U.check_logits(cfg, got, om.score(seq)["logits"][-3:], f"{name}: after a path of {len(path)}")
 
 
+@pytest.mark.parametrize("name", ["tiny", "mini", "wide"])
+def test_the_largest_tree(name):
+    """1024 nodes, some 20 deep; one more is refused."""
+    from paper_2309_08168_amd import binding as B
+
+    cfg, model, om = built(name)
+    n, prefix = B.SD_TREE_MAX, 5
+    rng = np.random.default_rng(1)
+    prompt = S.prompt(cfg, prefix, seed=3)
+    tokens = rng.integers(0, cfg.vocab, n).astype(np.int32)
+    parents = T.random_parents(n, rng, 100)
+    c = model.cache(prefix + n + 1)
+    model.forward(prompt, c)
+    lg = model.forward_tree(tokens, parents, c, logits=nan_logits(cfg, n)).cpu().numpy()
+    nodes = [0, 1, 500, 1000, n - 1]
+    U.check_logits(cfg, lg[nodes], oracle_nodes(om, prompt, tokens, parents, nodes), f"{name}: nodes {nodes}")
+    with pytest.raises(B.SDError) as e:
+        model.forward_tree([0] * (n + 1), [-1] + [0] * n, c)
+    assert e.value.status == B.SD_ERR_INVALID_ARG
+    path = path_of(parents, n - 1)
+    c.keep(path)
+    more = rng.integers(0, cfg.vocab, 2).astype(np.int32)
+    got = model.forward(more, c, logits=nan_logits(cfg, 2)).cpu().numpy()
+    seq = np.concatenate([prompt, tokens[path], more]).astype(np.int32)
+    U.check_logits(cfg, got, om.score(seq)["logits"][-2:], f"{name}: after a path of {len(path)}")
+
+
 @pytest.mark.parametrize("name", ["tiny", "mini"])
 @pytest.mark.parametrize("n", [6, 40])
 def test_tree_forward_with_a_skip_mask(name, n):
