@@ -320,7 +320,9 @@ typedef struct {
  *   YARN    by parts: with t_i = original_context f_i / (2 pi) turns in the
  *           original context and g = (t_i - beta_slow) / (beta_fast -
  *           beta_slow) clamped to [0, 1], f_i (g + (1 - g) / s); cosines and
- *           sines times 0.1 ln s + 1.
+ *           sines times 0.1 ln s + 1.  (g is linear in the turns, as the method
+ *           is defined.  Where it is made linear in i, between two rounded
+ *           bounds, the middle pairs turn by other angles: not offered.)
  * A gain other than 0 replaces the factor on cosines and sines (1 without
  * YARN).  base is at least 1e-9; the base that NTK takes, and a gain in float32,
  * are finite. */

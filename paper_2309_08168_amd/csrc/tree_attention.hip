@@ -140,10 +140,11 @@ __device__ __forceinline__ void merge_waves(const TreeAttnArgs &a, const float *
 // of four tiles.  V is asked for before the scores and the next block's K after
 // them.  The waves keep states of their own and merge at the end.
 //
-// Bound by the read of the cache, 4 rows over 4000 keys, 40 heads of 128: 34.2 us,
-// 4.8 TB/s (43 with V by single elements and no load ahead); by the chain of loads,
-// products and softmax of a block where there are few, 5 rows over 30 keys, 4
-// heads of 64: 4.9 us.
+// Bound by the read of the cache, 4 rows over 4000 keys, 40 heads of 128: 32.3 us
+// with the join, 5.1 TB/s (43 with V by single elements and no load ahead); by the
+// chain of loads, products and softmax of a block where there are few, 5 rows over
+// 30 keys, 4 heads of 64: 4.5 us; for more rows by every tile's own read of the
+// context and that chain, 64 rows over 4000 keys, 40 heads: 105 us.
 constexpr int TA_WAVES = 4;
 
 template <int D>
@@ -301,9 +302,9 @@ __global__ __launch_bounds__(TA_WAVES * 64, 2) void k_tree_attn_f32(TreeAttnArgs
 // V read over all banks; the loads permute the chunks of a line on the way in.
 //
 // Heads of 128, with their join: 64 rows of 8 over 16000 keys, 8 kv heads (tiles
-// of 128) 91 + 8 us, 1.1 PFLOP/s issued; 9 rows of 8 over 60000 keys, 8 kv heads
-// 76 + 6 us, 3.2 TB/s (the read alone takes 50, and power holds the clock at 1.7
-// GHz); 61 rows over 3001 keys, 32 heads (64) 21 + 4 us.
+// of 128) 90 + 8 us, 1.1 PFLOP/s issued; 9 rows of 8 over 60000 keys, 8 kv heads
+// 79 + 6 us (74 to 85 over runs), 3.1 TB/s (the read alone takes 50, and power holds
+// the clock at 1.7 GHz); 61 rows over 3001 keys, 32 heads (64) 21 + 4 us.
 
 // A maximum that grows by no more than this (in log2) does not rescale the sums:
 // weights then reach 2^8 and not 1, which float32 sums do not mind.  A row decides
@@ -1004,9 +1005,9 @@ void launch_join(const TreeAttnArgs &a, hipStream_t s) {
 // A single share needs no join, whose launch takes a caller 2.4 us: the few-row and
 // float32 kernels keep short contexts whole.  us on the GPU, whole and split: 5 rows
 // over 300 keys (40 heads) 8.9 and 8.6, over 500 11.6 and 8.8; 32 rows over 150 (8
-// heads) 12.1 and 11.2, over 300 14.2 and 11.4; float32, 5 rows over 100 (40 heads)
-// 8.0 and 7.6, over 240 11.2 and 7.8; heads of 64 over 240 7.2 and 6.2, over 500
-// 10.5 and 6.4; 13 rows (8 heads) of 16 over 700 9.4 and 7.9, over 1400 15.6 and 7.9.
+// heads) 12.1 and 11.2, over 300 14.2 and 11.4; float32, 13 rows, 40 heads of 128 over
+// 100 8.9 and 8.8, over 300 13.0 and 9.1; 4 of 64 over 300 8.5 and 7.0, over 1000
+// 18.2 and 7.2; 8 of 16 over 700 9.4 and 7.9, over 1400 15.6 and 7.9.
 constexpr int TA_CUS = 256, FEW_ROWS = 32;
 constexpr int whole_blocks(int q_rows) { return q_rows == 16 ? 12 : 6; }  // few rows: blocks of 32 keys
 constexpr int WHOLE_F32 = 6 * 64;  // float32: blocks of 64 times head_dim, which counts as 32 at least
