@@ -359,7 +359,7 @@ sd_status sd_rope_append(const sd_rope *rope, const float *qkv, int64_t ld_qkv, 
  * position and the nodes j whose bit j is set in row r of mask (uint64 [n][(n +
  * 63) / 64], as sd_tree_layout writes it; any bits, bits past n are ignored),
  * or the nodes 0 .. r when mask is NULL.  Scores are scaled by scale (0: 1 /
- * sqrt(head_dim)); sums are float32.  out [n][n_heads head_dim] (float32, rows
+ * sqrt(head_dim); scale log2(e) is finite); sums are float32.  out [n][n_heads head_dim] (float32, rows
  * ld_out apart, not overlapping q).  A row that sees nothing gives zeros; what
  * a row does not see changes no bit of its result, whatever it holds, and neither
  * do the other rows' queries; what it sees is finite, or its result may be NaN.

@@ -1150,8 +1150,10 @@ sd_status tree_attention(const sd_kv_layer *kv, const float *q, int64_t ld_q, in
         return report(SD_ERR_INVALID_ARG, "q and out must be set and 16-byte aligned, mask 8-byte aligned");
     if (ld_q % 4 || ld_out % 4 || ld_q < (int64_t)n_heads * D || ld_out < (int64_t)n_heads * D)
         return report(SD_ERR_INVALID_ARG, "ld_q and ld_out must hold a row and be multiples of 4");
-    if (!std::isfinite(scale))
-        return report(SD_ERR_INVALID_ARG, "scale must be finite");
+    // (the scores are taken in units of log2)
+    const float in_log2 = (scale == 0.0f ? 1.0f / std::sqrt((float)D) : scale) * 1.4426950408889634f;
+    if (!std::isfinite(in_log2))
+        return report(SD_ERR_INVALID_ARG, "scale, and scale log2(e), must be finite");
     TreeAttnArgs a{};
     plan(kv, n_heads, n, nodes, prefix, &a);
     const size_t need = workspace_of(a, D);
@@ -1171,7 +1173,7 @@ sd_status tree_attention(const sd_kv_layer *kv, const float *q, int64_t ld_q, in
         a.part_o = static_cast<float *>(workspace);
         a.part_ml = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + o_bytes(a, D));
     }
-    a.scale = (scale == 0.0f ? 1.0f / std::sqrt((float)D) : scale) * 1.4426950408889634f;
+    a.scale = in_log2;
     if (kv->dtype != SD_BF16)
         launch_f32(a, D, s);
     else if (D == 16)

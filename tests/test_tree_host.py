@@ -280,3 +280,15 @@ def f32_shares(rows, kvh, d, prefix):
     (4, 40, 128, 4000, 5, 6), (19, 32, 128, 1000, 4, 5)])
 def test_float32_shares(rows, kvh, d, prefix, least, most):
     assert least <= f32_shares(rows, kvh, d, prefix) <= most
+
+
+@pytest.mark.parametrize("scale", [3e38, -3e38, 2.4e38])
+def test_attention_refuses_a_scale_that_overflows_in_log2(scale):
+    assert attn_call(scale=scale) == BAD
+
+
+def test_attention_takes_the_largest_scale():
+    """(without its workspace: refused only further on, and by another message)"""
+    kv = layer(capacity=60000, head_stride=60000 * 128)
+    assert attn_call(kv=kv, prefix=50000, scale=2.3e38, ws=None, nbytes=0) == BAD
+    assert b"workspace" in binding.load().sd_last_error()
