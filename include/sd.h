@@ -435,6 +435,92 @@ sd_status sd_verify_tree(sd_model *model, const int32_t *tokens, const int32_t *
  * INVALID_ARG, UNIMPLEMENTED, OOM, DEVICE. */
 sd_status sd_model_set_rope(sd_model *model, const sd_rope *rope);
 
+/* Batches over a paged cache.  A server decodes several sequences at once, and
+ * their keys and values lie in pages of one cache: position p of sequence s is
+ * row p % page_size of page table[s][p / page_size].  The rows of a call (new
+ * tokens) are packed: those of sequence s are starts[s] .. starts[s + 1] - 1 and
+ * stand at the last positions of its lengths[s], row i of m at position
+ * lengths[s] - m + i.  One row a sequence decodes, a chain of drafts is verified
+ * (Algorithm 2) by a few, and a prompt comes whole or in chunks.
+ *
+ * The operators take DEVICE pointers on the current device, enqueue on
+ * hip_stream (NULL: the null stream) without waiting, allocate nothing and may
+ * be captured into a graph; what lies in device memory (lengths, starts, the
+ * table) may change between replays.  The same inputs give the same bits.
+ *
+ * The element (page b, head g, row o of it, e) of K and of V is at b *
+ * page_stride + g * head_stride + o * row_stride + e: strides in elements,
+ * multiples of 16 bytes, in any order as long as no two rows overlap; k and v
+ * 16-byte aligned; page_size a power of two in [16, 65536], head_dim one in [16,
+ * 128], dtype an sd_dtype. */
+typedef struct {
+    void *k, *v;
+    int64_t page_stride, head_stride, row_stride;
+    int32_t n_kv_heads, n_pages, page_size, head_dim, dtype;
+} sd_kv_pages;
+
+/* n_seqs sequences (1 to 65536).  table int32 [n_seqs], rows of table_pages
+ * entries, ld_table apart (table_pages * page_size at most 2^30); lengths int32
+ * [n_seqs]; starts int32 [n_seqs + 1], ascending, or NULL: sequence s has the rows
+ * s * max_rows .. (s + 1) * max_rows - 1.  A sequence has at most max_rows rows
+ * (those past them are passed over, as are rows outside every sequence: what
+ * the call would write for them is left as it was), and positions below
+ * max_length (at most table_pages * page_size, which 0 stands for; positions
+ * from there on are neither stored nor seen).  Both only bound what the call
+ * prepares for: a tight bound is a faster call.  An entry of the table outside [0, n_pages) holds no
+ * positions: nothing is stored there, and nothing of it is seen. */
+typedef struct {
+    const int32_t *table, *lengths, *starts;
+    int64_t ld_table;
+    int32_t n_seqs, table_pages, max_rows, max_length;
+} sd_batch;
+
+/* Normalises the heads of a QKV product (optional), rotates queries and keys, and
+ * stores keys and values: sd_rope_append for a batch.  Row r of qkv (x_dtype, an
+ * sd_dtype, rows ld_qkv elements apart: n_heads query heads, then the pages' kv
+ * heads of K, then of V).  q_norm and k_norm (dtype of the pages, [head_dim],
+ * both or neither): each head x of Q and of K becomes x_e w_e / sqrt(mean(x^2) +
+ * eps) before it is rotated.  The rotary position is positions[r] (int32 [n]), or
+ * the row's position in the cache when positions is NULL.  Rotated queries to
+ * q_out [n][n_heads head_dim] (x_dtype, rows ld_q apart, not overlapping qkv; of
+ * rows that no sequence has nothing is written), K and V to the row's
+ * position (rounded to nearest even; a negative one is not stored; rows of a
+ * call that name one row of a page leave a mix there).  Rows 16-byte aligned; 1
+ * <= n <= 2^20, n_heads at most 4096, eps >= 0 and finite.  Errors: INVALID_ARG,
+ * DEVICE. */
+sd_status sd_paged_append(const sd_rope *rope, const void *qkv, int64_t ld_qkv, int32_t x_dtype, int32_t n,
+                          int32_t n_heads, const int32_t *positions, const void *q_norm, const void *k_norm, float eps,
+                          void *q_out, int64_t ld_q, const sd_kv_pages *kv, const sd_batch *batch, void *hip_stream);
+
+/* Attention of a batch's rows over the pages: the row at position p sees the
+ * positions 0 .. p of its sequence (its own and those of the rows before it
+ * are in the pages already).  q and out [n][n_heads head_dim] (x_dtype, rows
+ * ld_q and ld_out apart, not overlapping); scores are scaled by scale (0: 1 /
+ * sqrt(head_dim); scale log2(e) is finite); scores and sums are float32 (with
+ * bfloat16 queries the softmax weights may be rounded to bfloat16 for their
+ * products).  A row that sees nothing gives zeros; what a row does not see
+ * changes no bit of its result, whatever it holds, and neither do the other
+ * rows' queries; what it sees is finite, or its result may be NaN.  workspace
+ * (16-byte aligned) holds at least sd_paged_attention_workspace() bytes for
+ * these sizes and belongs to the call until it has run.  Errors: INVALID_ARG, DEVICE. */
+sd_status sd_paged_attention(const sd_kv_pages *kv, const sd_batch *batch, const void *q, int64_t ld_q, int32_t x_dtype,
+                             int32_t n_heads, int32_t n, float scale, void *out, int64_t ld_out, void *workspace,
+                             size_t workspace_bytes, void *hip_stream);
+/* Bytes of workspace for these sizes (0 where none is needed, or for sizes
+ * that sd_paged_attention refuses); batch's pointers are not read. */
+size_t sd_paged_attention_workspace(const sd_kv_pages *kv, const sd_batch *batch, int32_t x_dtype, int32_t n_heads,
+                                    int32_t n);
+
+/* Causal attention of whole packed prompts: sequence s has the rows starts[s] ..
+ * starts[s + 1] - 1 (int32 [n_seqs + 1], ascending, within [0, n]; NULL: one
+ * sequence of n rows, n_seqs 1) of q, and the same positions of the layer hold
+ * its keys and values (capacity >= n; a packed [rows][kv heads][head_dim] tensor
+ * is a layer with row_stride n_kv_heads head_dim).  Row i of a sequence sees its
+ * rows 0 .. i.  The rest as in sd_paged_attention.  Errors: INVALID_ARG, CAPACITY, DEVICE. */
+sd_status sd_prompt_attention(const sd_kv_layer *kv, const int32_t *starts, int32_t n_seqs, const void *q, int64_t ld_q,
+                              int32_t x_dtype, int32_t n_heads, int32_t n, float scale, void *out, int64_t ld_out,
+                              void *hip_stream);
+
 /* Skip-set search (Sec. 3.3, Eq. 1): z* = argmin f(z) over sublayer masks
  * z in {0, 1}^L, by Bayesian optimisation for a fixed number of steps.
  * Host code; every evaluation of f is one call of the objective.

@@ -28,7 +28,7 @@ EXPORTS = (
     "sd_model_time_kernel", "sd_model_kernel_time", "sd_measure_read_bandwidth", "sd_model_quantize_draft",
     "sd_model_draft_fp8", "sd_tree_layout", "sd_rope_append", "sd_tree_attention", "sd_tree_attention_workspace",
     "sd_tree_accept", "sd_tree_accept_workspace", "sd_kv_keep", "sd_forward_tree", "sd_kv_cache_keep", "sd_verify_tree",
-    "sd_model_set_rope",
+    "sd_model_set_rope", "sd_paged_append", "sd_paged_attention", "sd_paged_attention_workspace", "sd_prompt_attention",
     "sd_last_error", "sd_version",
 )
 
@@ -87,6 +87,19 @@ class sd_kv_layer(ctypes.Structure):
 class sd_rope(ctypes.Structure):
     _fields_ = [(n, ctypes.c_double) for n in ("base", "factor", "gain", "beta_fast", "beta_slow")] + [
         (n, ctypes.c_int32) for n in ("rotary_dim", "layout", "scaling", "original_context")]
+
+
+class sd_kv_pages(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("page_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64), ("n_kv_heads", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32)]
+
+
+class sd_batch(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("starts", ctypes.c_void_p),
+                ("ld_table", ctypes.c_int64), ("n_seqs", ctypes.c_int32), ("table_pages", ctypes.c_int32),
+                ("max_rows", ctypes.c_int32), ("max_length", ctypes.c_int32)]
 
 
 SD_SEARCH_MEASURED, SD_SEARCH_MODELED = 0, 1
@@ -172,6 +185,13 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "sd_kv_cache_keep": ([vp, vp, i32], ctypes.c_int),
         "sd_verify_tree": ([vp, vp, vp, i32, vp, vp, p(i32), p(i32)], ctypes.c_int),
         "sd_model_set_rope": ([vp, p(sd_rope)], ctypes.c_int),
+        "sd_paged_append": ([p(sd_rope), vp, i64, i32, i32, i32, vp, vp, vp, ctypes.c_float, vp, i64, p(sd_kv_pages),
+                             p(sd_batch), vp], ctypes.c_int),
+        "sd_paged_attention": ([p(sd_kv_pages), p(sd_batch), vp, i64, i32, i32, i32, ctypes.c_float, vp, i64, vp,
+                                ctypes.c_size_t, vp], ctypes.c_int),
+        "sd_paged_attention_workspace": ([p(sd_kv_pages), p(sd_batch), i32, i32, i32], ctypes.c_size_t),
+        "sd_prompt_attention": ([p(sd_kv_layer), vp, i32, vp, i64, i32, i32, i32, ctypes.c_float, vp, i64, vp],
+                                ctypes.c_int),
         "sd_last_error": ([], ctypes.c_char_p),
         "sd_version": ([], ctypes.c_char_p),
     }
@@ -718,6 +738,195 @@ def kv_keep(kv, base: int, walk):
     if status:
         check(status)
     return kv
+
+
+# ----------------------------------------------------------------------------
+# Batches over a paged cache: operators on torch tensors, as above.
+
+
+def _pages(k, v):
+    """(sd_kv_pages, n_kv_heads, head_dim) of two tensors."""
+    if _torch is None:
+        _use_torch()
+    dtype, shape, stride = k.dtype, k.shape, k.stride()
+    if (dtype is not _bf16 and dtype is not _f32) or len(shape) != 4 or stride[3] != 1 or v.dtype is not dtype or \
+            v.shape != shape or v.stride() != stride:
+        _refuse("k and v are [n_pages, n_kv_heads, page_size, head_dim], float32 or bfloat16, of one type and one set of "
+                "strides, rows contiguous")
+    pages, heads, size, d = shape
+    if pages > _INT32_MAX or heads > _INT32_MAX or size > _INT32_MAX or d > _INT32_MAX:
+        _int32(pages, heads, size, d)
+    return sd_kv_pages(k.data_ptr(), v.data_ptr(), stride[0], stride[1], stride[2], heads, pages, size, d,
+                       SD_BF16 if dtype is _bf16 else SD_F32), heads, d
+
+
+def kv_pages(k, v) -> sd_kv_pages:
+    """sd_kv_pages over tensors [n_pages, n_kv_heads, page_size, head_dim] (float32
+    or bfloat16, elements of a row adjacent, the same strides, which may follow another
+    order)."""
+    return _pages(k, v)[0]
+
+
+def batch(table, lengths, starts=None, max_rows: int = 1, max_length: int = 0) -> sd_batch:
+    """A batch of sequences (sd_batch) over int32 tensors: table [n_seqs, pages], the
+    page of each page_size positions; lengths [n_seqs], positions with the new rows;
+    starts [n_seqs + 1], the packed rows of each sequence, or None: max_rows rows a
+    sequence.  max_rows and max_length (0: all that the table holds) bound them.  The
+    tensors live on with the batch and may change between calls."""
+    if _torch is None:
+        _use_torch()
+    shape, stride = table.shape, table.stride()
+    if table.dtype is not _i32 or len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
+        _refuse("table is int32 [n_seqs, pages], its rows contiguous")
+    seqs, pages = shape
+    if seqs >= _INT32_MAX or pages > _INT32_MAX or not (0 <= max_rows <= _INT32_MAX and 0 <= max_length <= _INT32_MAX):
+        _int32(seqs + 1, pages, max_rows, max_length)
+    at = _words(lengths, seqs, "lengths")
+    if starts is None:
+        rows, dev = None, _device(table, lengths)
+    else:
+        rows, dev = _words(starts, seqs + 1, "starts"), _device(table, lengths, starts)
+    b = sd_batch(table.data_ptr(), at, rows, stride[0] if seqs > 1 else pages, seqs, pages, max_rows, max_length)
+    b.tensors, b.device = (table, lengths, starts), dev
+    return b
+
+
+def _x_type(t, what: str) -> int:
+    """The sd_dtype of activations."""
+    dtype = t.dtype
+    if dtype is not _f32 and dtype is not _bf16:
+        _refuse(f"{what} is float32 or bfloat16")
+    return SD_BF16 if dtype is _bf16 else SD_F32
+
+
+def _heads(t, n: int, h: int, d: int, dtype, what: str) -> int:
+    """Row stride of a tensor [n, h, d] of a type whose rows are contiguous."""
+    stride = t.stride()
+    if t.dtype is not dtype or t.shape != (n, h, d) or stride[2] != 1 or (stride[1] != d and h > 1):
+        _refuse(f"{what} is {dtype} [{n}, {h}, {d}], its rows contiguous")
+    return stride[0] if n > 1 else h * d
+
+
+def _on(dev: int, b):
+    if b.device != dev:
+        _refuse("the batch is on another device")
+
+
+def paged_append(form: sd_rope, qkv, k, v, batch: sd_batch, n_heads: int, positions=None, q_norm=None, k_norm=None,
+                 eps: float = 1e-6, q_out=None):
+    """sd_paged_append: qkv float32 or bfloat16 [n, (n_heads + 2 n_kv_heads)
+    head_dim], k and v as in kv_pages; positions int32 [n] or None: the rows'
+    positions in the cache; q_norm and k_norm [head_dim] of the type of k, or None.
+    Returns the rotated queries, [n, n_heads, head_dim] like qkv (rows outside every
+    sequence are not written: q_out holds them as it did)."""
+    pages, kvh, d = _pages(k, v)
+    x_type, shape, stride = _x_type(qkv, "qkv"), qkv.shape, qkv.stride()
+    width = (n_heads + 2 * kvh) * d
+    if len(shape) != 2 or shape[1] != width or stride[1] != 1:
+        _refuse(f"qkv is [n, (n_heads + 2 n_kv_heads) head_dim] = [n, {width}], its rows contiguous")
+    n = shape[0]
+    if not 0 <= n_heads <= _INT32_MAX or n > _INT32_MAX:
+        _int32(n, n_heads)
+    dev = _device(qkv, k, v)
+    _on(dev, batch)
+    at = wq = wk = None
+    if positions is not None:
+        at = _words(positions, n, "positions")
+        _device(qkv, positions)
+    if q_norm is not None or k_norm is not None:
+        for w in (q_norm, k_norm):
+            if w is None or w.dtype is not k.dtype or w.shape != (d,) or not w.is_contiguous():
+                _refuse(f"q_norm and k_norm are contiguous [{d}] of the type of k, both or neither")
+        _device(qkv, q_norm, k_norm)
+        wq, wk = q_norm.data_ptr(), k_norm.data_ptr()
+    if dev != _current():
+        return _elsewhere(dev, paged_append, form, qkv, k, v, batch, n_heads, positions, q_norm, k_norm, eps, q_out)
+    if q_out is None:
+        q_out, ldq = qkv.new_empty(n, n_heads, d), n_heads * d
+    else:
+        ldq = _heads(q_out, n, n_heads, d, qkv.dtype, "q_out")
+        _device(qkv, q_out)
+    status = _lib.sd_paged_append(form, qkv.data_ptr(), stride[0] if n > 1 else width, x_type, n, n_heads, at, wq, wk, eps,
+                                  q_out.data_ptr(), ldq, pages, batch, _raw_stream(dev))
+    if status:
+        check(status)
+    return q_out
+
+
+def paged_attention(q, k, v, batch: sd_batch, scale: float = 0.0, out=None, workspace=None):
+    """sd_paged_attention: q float32 or bfloat16 [n, n_heads, head_dim], k and v as in
+    kv_pages, scale 0: 1 / sqrt(head_dim).  Returns out, like q (rows outside every
+    sequence are not written); workspace: a tensor of at least
+    paged_attention_workspace() bytes (else one is allocated)."""
+    pages, _, d = _pages(k, v)
+    x_type, shape = _x_type(q, "q"), q.shape
+    if len(shape) != 3:
+        _refuse("q is [n, n_heads, head_dim]")
+    n, h, _ = shape
+    if n > _INT32_MAX or h > _INT32_MAX:
+        _int32(n, h)
+    ld = _heads(q, n, h, d, q.dtype, "q")
+    dev = _device(q, k, v)
+    _on(dev, batch)
+    if dev != _current():
+        return _elsewhere(dev, paged_attention, q, k, v, batch, scale, out, workspace)
+    if out is None:
+        out, ldo = q.new_empty(n, h, d), h * d
+    else:
+        ldo = _heads(out, n, h, d, q.dtype, "out")
+        _device(q, out)
+    if workspace is None:
+        nbytes = _lib.sd_paged_attention_workspace(pages, batch, x_type, h, n)
+        ws = q.new_empty((nbytes + 3) >> 2, dtype=_f32) if nbytes else None
+        at = ws.data_ptr() if nbytes else None
+    else:
+        at, nbytes = _space(workspace, q)
+    status = _lib.sd_paged_attention(pages, batch, q.data_ptr(), ld, x_type, h, n, scale, out.data_ptr(), ldo, at, nbytes,
+                                     _raw_stream(dev))
+    if status:
+        check(status)
+    return out
+
+
+def paged_attention_workspace(k, v, batch: sd_batch, n_heads: int, n: int, bf16: bool = False) -> int:
+    """Bytes of workspace paged_attention needs for these sizes (bf16: for bfloat16
+    queries)."""
+    _int32(n_heads, n)
+    return int(load().sd_paged_attention_workspace(kv_pages(k, v), batch, SD_BF16 if bf16 else SD_F32, n_heads, n))
+
+
+def prompt_attention(q, k, v, starts=None, scale: float = 0.0, out=None):
+    """sd_prompt_attention: q float32 or bfloat16 [n, n_heads, head_dim], k and v as in
+    kv_layer with the keys and values of row r at position r; starts int32 [n_seqs + 1]
+    or None: one sequence; scale 0: 1 / sqrt(head_dim).  Returns out, like q
+    (rows outside every sequence are not written)."""
+    layer, _, d = _layer(k, v)
+    x_type, shape = _x_type(q, "q"), q.shape
+    if len(shape) != 3:
+        _refuse("q is [n, n_heads, head_dim]")
+    n, h, _ = shape
+    if n > _INT32_MAX or h > _INT32_MAX:
+        _int32(n, h)
+    ld = _heads(q, n, h, d, q.dtype, "q")
+    if starts is None:
+        at, seqs, dev = None, 1, _device(q, k, v)
+    else:
+        seqs = starts.numel() - 1
+        at, dev = _words(starts, seqs + 1, "starts"), _device(q, k, v, starts)
+        if seqs > _INT32_MAX:
+            _int32(seqs)
+    if dev != _current():
+        return _elsewhere(dev, prompt_attention, q, k, v, starts, scale, out)
+    if out is None:
+        out, ldo = q.new_empty(n, h, d), h * d
+    else:
+        ldo = _heads(out, n, h, d, q.dtype, "out")
+        _device(q, out)
+    status = _lib.sd_prompt_attention(layer, at, seqs, q.data_ptr(), ld, x_type, h, n, scale, out.data_ptr(), ldo,
+                                      _raw_stream(dev))
+    if status:
+        check(status)
+    return out
 
 
 def _search_call(call, n_dims: int, objective: int, cost, params: dict) -> dict:

@@ -13,7 +13,8 @@ CSRC = os.path.join(PKG, "csrc")
 OUT = os.path.join(PKG, "libsd.so")
 BUILD = os.path.join(ROOT, "_build")
 SOURCES = ["kernels_linear.hip", "kernels_attn.hip", "kernels_sample.hip", "kernels_prefill.hip", "model.hip",
-           "skip_search.cpp", "probe.hip", "tree_ops.hip", "tree_attention.hip"]
+           "skip_search.cpp", "probe.hip", "tree_ops.hip", "tree_attention.hip",
+           "paged_append.hip", "batch_attention.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
