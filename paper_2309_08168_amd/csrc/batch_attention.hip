@@ -13,9 +13,8 @@
 #include <cmath>
 #include <string>
 
+#include "attn_mfma.h"
 #include "host_api.h"
-#include "rope.h"
-#include "sd_internal.h"
 
 using namespace sdk;
 
@@ -75,8 +74,6 @@ __device__ __forceinline__ Tile tile_of(const BatchAttnArgs &a, int32_t t) {
     return w;
 }
 
-__device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
-
 // The NW waves' states of ROWS rows from row0 on (o [wave][row][D + 4], waves
 // `pitch` floats apart; (maximum, sum) [wave][row]) merged in wave order: the
 // result of a single share, or its part of several.
@@ -128,23 +125,10 @@ __device__ __forceinline__ void merge_waves(const BatchAttnArgs &a, const Tile &
 // own and merge at the end.  A wave's 16 keys lie in one page.
 constexpr int KB = 64, NW = 4;
 
-template <int W, typename T>
-__device__ __forceinline__ void load_some(const T *p, float (&x)[W]) {
-    if constexpr (W == 4) {
-        const f32x4_t y = load4(p);
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-            x[u] = y[u];
-    } else {
-#pragma unroll
-        for (int u = 0; u < W; ++u)
-            x[u] = load1(p + u);
-    }
-}
-
-template <typename TX, typename TK, int D>
+template <typename TX, int D>
 __global__ __launch_bounds__(NW * 64, 2) void k_batch_attn_f32(BatchAttnArgs a) {
-    constexpr int ES = D / 16, OP = D + 4, W = ES < 4 ? ES : 4;  // W: adjacent elements of V
+    constexpr int ES = D / 16, OP = D + 4, W = ES < 4 ? ES : 4;  // W: elements of a load of V
+    typedef float vec_t __attribute__((ext_vector_type(W)));
     __shared__ __attribute__((aligned(16))) float tile[NW][16 * OP];
     __shared__ float2 ml[NW][16];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, c = lane & 15,
@@ -159,8 +143,8 @@ __global__ __launch_bounds__(NW * 64, 2) void k_batch_attn_f32(BatchAttnArgs a) 
     const int b0 = split * a.per_split, b1 = min(b0 + a.per_split, (klen + KB - 1) / KB);
     if (a.splits > 1 && b0 >= b1)
         return;
-    const TK *K = static_cast<const TK *>(a.k) + (int64_t)g * a.head_stride;
-    const TK *V = static_cast<const TK *>(a.v) + (int64_t)g * a.head_stride;
+    const float *K = static_cast<const float *>(a.k) + (int64_t)g * a.head_stride;
+    const float *V = static_cast<const float *>(a.v) + (int64_t)g * a.head_stride;
     const int rr = min(w.row0 + c, rows - 1), node = rr / a.G, head = g * a.G + rr - node * a.G;
     const int see = seen_from(w.rows.past + node, a.max_length);
 
@@ -196,7 +180,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_batch_attn_f32(BatchAttnArgs a) 
     // keys past the last read that one; their scores are masked
     f32x4_t kx[ES];
     auto load_k = [&](int b, int page) {
-        const TK *kp = K + place(b, page) + min(c, klen - 1 - KB * b - 16 * wave) * a.row_stride + 4 * g4;
+        const float *kp = K + place(b, page) + min(c, klen - 1 - KB * b - 16 * wave) * a.row_stride + 4 * g4;
 #pragma unroll
         for (int j = 0; j < ES; ++j)
             kx[j] = load4(kp + 16 * j);
@@ -209,15 +193,15 @@ __global__ __launch_bounds__(NW * 64, 2) void k_batch_attn_f32(BatchAttnArgs a) 
         const int first = KB * b + 16 * wave;
         const bool some = page >= 0;  // uniform over the wave
         f32x4_t s = {0.0f, 0.0f, 0.0f, 0.0f};
-        float vx[4][ES / W][W];
-        const TK *vb = V + place(b, page);
+        vec_t vx[4][ES / W];
+        const float *vb = V + place(b, page);
         if (some) {
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
-                const TK *vp = vb + min(4 * g4 + v, klen - 1 - first) * a.row_stride + W * c;
+                const float *vp = vb + min(4 * g4 + v, klen - 1 - first) * a.row_stride + W * c;
 #pragma unroll
                 for (int t = 0; t < ES / W; ++t)
-                    load_some<W>(vp + 16 * W * t, vx[v][t]);
+                    vx[v][t] = *reinterpret_cast<const vec_t *>(vp + 16 * W * t);
             }
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -268,7 +252,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_batch_attn_f32(BatchAttnArgs a) 
             // not add 0 times it.  They are taken out of the operands, and
             // added here, from memory, where they belong.
             for (int key = 0; key < 16; ++key) {
-                const TK *vr = vb + min(key, klen - 1 - first) * a.row_stride;
+                const float *vr = vb + min(key, klen - 1 - first) * a.row_stride;
                 float pk = p[0];
 #pragma unroll
                 for (int v = 1; v < 4; ++v)
@@ -278,7 +262,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_batch_attn_f32(BatchAttnArgs a) 
                 for (int t = 0; t < ES; ++t)
 #pragma unroll
                     for (int u = 0; u < 4; ++u) {
-                        const float x = load1(vr + element(t, u));
+                        const float x = vr[element(t, u)];
                         if (pk != 0.0f && !finite(x))
                             o[t][u] = fmaf(pk, x, o[t][u]);
                     }
@@ -308,6 +292,400 @@ __global__ __launch_bounds__(NW * 64, 2) void k_batch_attn_f32(BatchAttnArgs a) 
         ml[wave][c] = make_float2(m_run, l_run);
     __syncthreads();
     merge_waves<TX, D, NW, 16>(a, w, &tile[0][0], 16 * OP, &ml[0][0], g, split);
+}
+
+// ---------------------------------------------------------------------------
+// bfloat16 caches: matrix cores.  bfloat16 queries and softmax weights are one
+// bfloat16 term each (the scores are scaled in float32); float32 ones (q times scale
+// log2(e)) are held as three terms that add up to them exactly, so that only the
+// float32 sums round.
+//
+// NQ x NK waves take 32 NQ rows of a kv head; the K and V rows of a block come
+// straight into LDS one block ahead, and all waves read them there.  NK = 2 waves
+// share a block's keys where there are few rows.  32 keys at a time: scores S^T =
+// K q as 32x32x16 products leave lane (col, half) the keys 8 (v / 4) + 4 half +
+// v % 4, v = 0..15, of row col; values v = 8 j .. 8 j + 7 are the slots of the
+// j-th 16-key value product, so the weights stay in their lanes and V^T is read
+// to match, transposed on its way out of LDS.
+//
+// LDS lines are 256 bytes, 16 chunks of 16 bytes: 128 / D rows.  Chunk p of line s
+// lies at p ^ swz(s), which spreads the 16 rows of a K read and the four rows of a
+// V read over all banks; the loads permute the chunks of a line on the way in.
+// The 16 rows of a group lie in one page, so a load of a group's rows (heads of 32 and
+// more) has one base.
+
+// Where the four 16-key groups of a block start: elements from a head's first, and
+// whether there are keys (a bit each).
+struct Groups {
+    int64_t off[4];
+    uint32_t ok;
+};
+// Their entries of the table, asked for a block ahead of what needs them.
+struct Entries {
+    int32_t page[4];
+};
+__device__ __forceinline__ Entries entries_of(const BatchAttnArgs &a, const Tile &w, int first, int klen) {
+    Entries e;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int f = first + 16 * j;
+        e.page[j] = a.table && f < klen ? a.table[(int64_t)w.seq * a.ld_table + (f >> a.page_shift)] : -1;
+    }
+    return e;
+}
+__device__ __forceinline__ Groups groups_of(const BatchAttnArgs &a, const Tile &w, const Entries &e, int first, int klen) {
+    Groups k;
+    k.ok = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int f = first + 16 * j;
+        if (a.table) {
+            // (without a page: any rows, which are masked, and taken for finite)
+            const int page = __builtin_amdgcn_readfirstlane(e.page[j]);
+            const bool there = (uint32_t)page < (uint32_t)a.n_pages;
+            k.off[j] = (there ? page * a.page_stride : 0) + (int64_t)(f & ((1 << a.page_shift) - 1)) * a.row_stride;
+            k.ok |= there ? 1u << j : 0u;
+        } else {
+            k.off[j] = (int64_t)(w.rows.first + f) * a.row_stride;
+            k.ok |= f < klen ? 1u << j : 0u;
+        }
+    }
+    return k;
+}
+// The keys of a block that are seen by one who sees `count` of them, as bits.
+__device__ __forceinline__ uint64_t seen_bits(int count, uint32_t ok) {
+    uint64_t groups = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        groups |= (ok >> j) & 1 ? 0xffffull << (16 * j) : 0;
+    return (count >= 64 ? ~0ull : count <= 0 ? 0 : (1ull << count) - 1) & groups;
+}
+
+template <typename TX, int D, int NQ, int NK>
+__global__ __launch_bounds__(64 * NQ * NK, 2) void k_batch_attn_mfma(BatchAttnArgs a) {
+    constexpr bool EXACT = sizeof(TX) == 4;
+    constexpr int T = EXACT ? X_TERMS : 1, WAVES = NQ * NK, ES = D / 16, ET = D < 32 ? 1 : D / 32;
+    using L = Lines<D>;
+    __shared__ __attribute__((aligned(1024))) uint16_t kv[2][2][KB * D];  // [block % 2][K, V]
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 31,
+              half = lane >> 5;
+    const int wq = wave % NQ, wk = wave / NQ;
+    const int g = blockIdx.x % a.n_kv_heads, rest = blockIdx.x / a.n_kv_heads;
+    const int split = rest / a.slots;
+    // (from the last tile, which has the most keys, to the first)
+    const Tile w = tile_of(a, a.slots - 1 - rest % a.slots);
+    const int rows = w.rows.m * a.G;
+    if (w.row0 >= rows)
+        return;  // uniform
+    auto sees = [&](int rr) { return seen_from(w.rows.past + rr / a.G, a.max_length); };
+    const int klen = __builtin_amdgcn_readfirstlane(sees(min(w.row0 + 32 * NQ, rows) - 1));
+    const int kall = __builtin_amdgcn_readfirstlane(sees(w.row0));
+    const int b0 = split * a.per_split, b1 = min(b0 + a.per_split, (klen + KB - 1) / KB);
+    if (a.splits > 1 && b0 >= b1)
+        return;
+    const int r0 = w.row0 + wq * 32;
+    const bool live = r0 < rows;  // uniform over the wave: a wave without rows loads and waits with the others
+    const int row = min(r0 + col, rows - 1), node = row / a.G, head = g * a.G + row - node * a.G;
+    const int see = seen_from(w.rows.past + node, a.max_length);
+    const uint16_t *K = static_cast<const uint16_t *>(a.k) + (int64_t)g * a.head_stride;
+    const uint16_t *V = static_cast<const uint16_t *>(a.v) + (int64_t)g * a.head_stride;
+
+    // A wave takes every WAVES-th KB of K's and of V's rows.  Whole groups: lane
+    // offsets that do not change, from the group's first row.
+    constexpr int NU = (L::C + WAVES - 1) / WAVES, ROWS = 4 * L::RPL;  // loads of a wave; rows of a load
+    const bool near = D > 16 && near_rows(a.row_stride);
+    uint32_t off[NU];
+#pragma unroll
+    for (int i = 0; i < NU; ++i) {
+        const int u = wave + WAVES * i, s = 4 * u + (lane >> 4), p = (lane & 15) ^ L::swz(s);
+        off[i] = (uint32_t)(2 * ((int64_t)((s * L::RPL + p / L::C) & 15) * a.row_stride + 8 * (p % L::C)));
+    }
+    auto load_block = [&](const Groups &k, int first, int buf) {
+        if (first + KB <= klen && near) {
+#pragma unroll
+            for (int i = 0; i < NU; ++i) {
+                const int u = wave + WAVES * i;
+                if (L::C % WAVES == 0 || u < L::C) {  // uniform over the wave
+                    const int j = ROWS * u / 16;
+                    const int64_t at = j == 0 ? k.off[0] : j == 1 ? k.off[1] : j == 2 ? k.off[2] : k.off[3];
+                    load_to_lds16(K + at, off[i], &kv[buf][0][u * 512]);
+                    load_to_lds16(V + at, off[i], &kv[buf][1][u * 512]);
+                }
+            }
+        } else {
+#pragma unroll 1
+            for (int u = wave; u < L::C; u += WAVES) {
+                const int s = 4 * u + (lane >> 4), p = (lane & 15) ^ L::swz(s);
+                const int r = min(s * L::RPL + p / L::C, klen - 1 - first), j = r >> 4;  // rows past the last: that one
+                const int64_t at = (j == 0 ? k.off[0] : j == 1 ? k.off[1] : j == 2 ? k.off[2] : k.off[3]) +
+                                   (r & 15) * a.row_stride + 8 * (p % L::C);
+                load_to_lds16(K + at, &kv[buf][0][u * 512]);
+                load_to_lds16(V + at, &kv[buf][1][u * 512]);
+            }
+        }
+    };
+    Entries entries = entries_of(a, w, KB * b0, klen);
+    // The queries are asked for before the first block: loads return in order.
+    const TX *qs = static_cast<const TX *>(a.q) + (int64_t)(w.rows.first + node) * a.ld_q + (int64_t)head * D + 8 * half;
+    u32x4_t qf[ES][T];
+    f32x4_t qx[EXACT ? ES : 1][2];
+#pragma unroll
+    for (int s = 0; s < ES; ++s) {
+        if constexpr (EXACT) {
+            qx[s][0] = load4(qs + 16 * s);
+            qx[s][1] = load4(qs + 16 * s + 4);
+        } else {
+            qf[s][0] = *reinterpret_cast<const u32x4_t *>(qs + 16 * s);
+        }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    Groups k = groups_of(a, w, entries, KB * b0, klen);
+    if (b0 < b1)
+        load_block(k, KB * b0, 0);
+    entries = entries_of(a, w, KB * (b0 + 1), klen);
+    // Rows past the last are zeros, which draw less power than copies of it.
+    const bool mine = r0 + col < rows;
+#pragma unroll
+    for (int s = 0; s < ES; ++s) {
+        if constexpr (EXACT) {
+            const float scale = mine ? a.scale : 0.0f;
+            query_terms(qx[s][0] * scale, qx[s][1] * scale, qf[s]);
+        } else {
+            // (a negative scale as one of q, so that the largest score stays the largest)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                qf[s][0][j] = mine ? qf[s][0][j] ^ (a.scale < 0.0f ? 0x80008000u : 0u) : 0u;
+        }
+    }
+    // (a scale that float32 products would take for zero would make NaN of a masked score)
+    const float factor = EXACT ? 1.0f : fmaxf(fabsf(a.scale), 1.17549435e-38f);
+    // V^T reads: ds_read_b64_tr_b16 hands lane l of each 16-lane group element
+    // l % 4 of the 8 bytes that lanes l / 4 + 4 k (k = 0..3) point at, so lane l
+    // points at row 4 half + l / 4 % 4, columns 16 (l / 16 % 2) + 4 (l % 4) ...
+    // (head_dim 16: columns past it repeat the first, in output rows that
+    // nothing reads)
+    const int v_lane = 2 * (KB * D + L::at(4 * half + ((lane >> 2) & 3), (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) % L::C) +
+                            4 * (lane & 1));
+    const char *lds = reinterpret_cast<const char *>(kv);
+    float m_run = -INFINITY, l_run = 0.0f;
+    f32x16_t o[ET];
+#pragma unroll
+    for (int et = 0; et < ET; ++et)
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+            o[et][v] = 0.0f;
+
+    int buf = 0;
+    for (int b = b0; b < b1; ++b, buf ^= 1) {
+        const int first = KB * b;
+        const Groups now = k;
+        // this wave's loads of the block have landed, then everyone's; every
+        // read of the other buffer has returned
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (b + 1 < b1) {
+            k = groups_of(a, w, entries, first + KB, klen);
+            load_block(k, first + KB, buf ^ 1);
+            entries = entries_of(a, w, first + 2 * KB, klen);
+        }
+        const bool full = first + KB <= kall && now.ok == 15;  // every row sees every key
+        bool odd = false;
+        if (!full) {
+            // A row must not add 0 times an infinity or NaN of a value that it
+            // does not see: they are taken out here, and put where they belong
+            // beside the products.
+            uint16_t *vs = kv[buf][1];
+            for (int c = threadIdx.x; c < KB * D / 8; c += 64 * WAVES) {
+                u32x4_t x = reinterpret_cast<const u32x4_t *>(vs)[c];
+                bool hit = false;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t y = without_odd(x[j]);
+                    hit |= y != x[j];
+                    x[j] = y;
+                }
+                if (hit)
+                    reinterpret_cast<u32x4_t *>(vs)[c] = x;
+                odd |= hit;
+            }
+            odd = __syncthreads_or(odd);
+        }
+        const uint64_t visible = full ? ~0ull : seen_bits(see - first, now.ok);
+#pragma unroll 1
+        for (int h = wk; h < 2; h += NK) {
+            const uint32_t bits = h ? (uint32_t)(visible >> 32) : (uint32_t)visible;
+            if (!live || (!full && !__any(bits != 0)))
+                continue;  // uniform over the wave: no row of it sees these keys
+            f32x16_t s;
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+                s[v] = 0.0f;
+            // byte addresses in LDS: rows 32 h + col, chunk 2 e + half at xk ^ 32 e.
+            // (Hidden from the compiler, which would keep every address of the
+            // loop in a register and spill.)
+            int xk = 2 * (buf * 2 * KB * D + 32 * h * D + L::at(col, half)), xv = 2 * (buf * 2 * KB * D + 32 * h * D) + v_lane;
+            asm volatile("" : "+v"(xk), "+v"(xv));
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int e = 0; e < ES; ++e) {
+                const u32x4_t kf = *reinterpret_cast<const u32x4_t *>(lds + (xk ^ (32 * e)));
+#pragma unroll
+                for (int i = 0; i < T; ++i)
+                    s = mfma32(kf, qf[e][i], s);
+            }
+            __builtin_amdgcn_s_setprio(0);
+            if (!full) {
+                uint32_t own = bits >> (4 * half);
+                asm volatile("" : "+v"(own));  // (a branch, and not selects in every block)
+#pragma unroll
+                for (int v = 0; v < 16; ++v)
+                    s[v] = (own >> (8 * (v >> 2) + (v & 3))) & 1 ? s[v] : -INFINITY;
+            }
+            float mx = s[0];
+#pragma unroll
+            for (int v = 1; v < 16; ++v)
+                mx = fmaxf(mx, s[v]);
+            {
+                const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+                mx = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+            }
+            if constexpr (!EXACT)
+                mx *= factor;
+            const bool grows = mx > m_run + SLACK;
+            if (__any(grows)) {
+                // (a row that has seen no key yet keeps zeros)
+                const float m_new = grows ? mx : m_run;
+                const float sc = m_run == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run - m_new);
+                l_run *= sc;
+#pragma unroll
+                for (int et = 0; et < ET; ++et)
+                    o[et] *= sc;
+                m_run = m_new;
+            }
+            const float m_use = m_run == -INFINITY ? 0.0f : m_run;
+            // (the running sum is rounded once for the 16 weights)
+            float p[16], sum = 0.0f;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                p[v] = __builtin_amdgcn_exp2f(EXACT ? s[v] - m_use : fmaf(s[v], factor, -m_use));
+                sum += p[v];
+            }
+            l_run += sum;
+            if (odd) {
+                // what was taken out, from memory: lane (col, half) holds
+                // elements 32 et + 8 (v / 4) + 4 half + v % 4 of row col
+#pragma unroll 1
+                for (int key = 0; key < 32; ++key) {
+                    float pk = 0.0f;
+                    const int own = 4 * (key >> 3) + (key & 3);
+#pragma unroll
+                    for (int v = 0; v < 16; ++v)
+                        pk = v == own ? p[v] : pk;
+                    pk = __shfl(pk, col + 32 * ((key >> 2) & 1), 64);
+                    const int r = min(32 * h + key, klen - 1 - first), j = r >> 4;
+                    const uint16_t *vr = V + (j == 0 ? now.off[0] : j == 1 ? now.off[1] : j == 2 ? now.off[2] : now.off[3]) +
+                                         (r & 15) * a.row_stride;
+#pragma unroll
+                    for (int et = 0; et < ET; ++et)
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) {
+                            const int e = 32 * et + 8 * (v >> 2) + 4 * half + (v & 3);
+                            const float x = e < D ? load1(vr + e) : 0.0f;
+                            if (pk != 0.0f && !finite(x))
+                                o[et][v] = fmaf(pk, x, o[et][v]);
+                        }
+                }
+            }
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                u32x4_t pf[T];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    if constexpr (EXACT) {
+                        uint32_t t[T];
+                        terms2(p[8 * j + 2 * u], p[8 * j + 2 * u + 1], t);
+#pragma unroll
+                        for (int i = 0; i < T; ++i)
+                            pf[i][u] = t[i];
+                    } else {
+                        pf[0][u] = cvt_pk(p[8 * j + 2 * u], p[8 * j + 2 * u + 1]);
+                    }
+                }
+                // A operand V^T: column 32 et + col of keys 16 j + 8 I + 4 half +
+                // 0..3, the row's chunks of et and I one exclusive or away
+#pragma unroll
+                for (int et = 0; et < ET; ++et) {
+                    u32x4_t vf;
+#pragma unroll
+                    for (int I = 0; I < 2; ++I) {
+                        const char *src = lds + (xv ^ (64 * et) ^ (I ? (D == 16 ? 16 : 32) : 0)) + 2 * (16 * j + 8 * I) * D;
+                        const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)src);
+                        const u32x2_t y = __builtin_bit_cast(u32x2_t, x);
+                        vf[2 * I] = y[0];
+                        vf[2 * I + 1] = y[1];
+                    }
+#pragma unroll
+                    for (int i = 0; i < T; ++i)
+                        o[et] = mfma32(vf, pf[i], o[et]);
+                }
+            }
+            __builtin_amdgcn_s_setprio(0);
+        }
+    }
+    {
+        const auto lr = __builtin_amdgcn_permlane32_swap(__float_as_uint(l_run), __float_as_uint(l_run), false, false);
+        l_run = __uint_as_float(lr[0]) + __uint_as_float(lr[1]);
+    }
+    if constexpr (NK == 2) {
+        // the second half of the keys joins the first: its states through LDS,
+        // 16 ET + 2 words a lane
+        static_assert(sizeof(kv) >= NQ * 64 * (16 * ET + 2) * 4 || D < 128, "LDS for the states");
+        __shared__ float st[D == 128 ? 1 : NQ * 64 * (16 * ET + 2)];
+        float *to = D == 128 ? reinterpret_cast<float *>(kv) : st;
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (wk == 1) {
+#pragma unroll
+            for (int et = 0; et < ET; ++et)
+#pragma unroll
+                for (int v = 0; v < 16; ++v)
+                    to[((16 * et + v) * NQ + wq) * 64 + lane] = o[et][v];
+            to[(16 * ET * NQ + wq) * 64 + lane] = m_run;
+            to[((16 * ET + 1) * NQ + wq) * 64 + lane] = l_run;
+        }
+        __syncthreads();
+        if (wk == 1)
+            return;
+        const float m2 = to[(16 * ET * NQ + wq) * 64 + lane], l2 = to[((16 * ET + 1) * NQ + wq) * 64 + lane];
+        const float m = fmaxf(m_run, m2), mu = m == -INFINITY ? 0.0f : m;
+        const float w1 = __builtin_amdgcn_exp2f(m_run - mu), w2 = __builtin_amdgcn_exp2f(m2 - mu);
+        m_run = m;
+        l_run = l_run * w1 + l2 * w2;
+#pragma unroll
+        for (int et = 0; et < ET; ++et)
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+                o[et][v] = o[et][v] * w1 + to[((16 * et + v) * NQ + wq) * 64 + lane] * w2;
+    }
+    if (!mine)
+        return;
+    const int64_t at = (int64_t)(w.rows.first + node), slot = ((int64_t)split * a.n + at) * a.n_heads + head;
+    TX *out = static_cast<TX *>(a.out) + at * a.ld_out + (int64_t)head * D;
+    const float inv = a.splits > 1 ? 1.0f : l_run == 0.0f ? 0.0f : 1.0f / l_run;
+#pragma unroll
+    for (int et = 0; et < ET; ++et)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int e = 32 * et + 8 * q + 4 * half;
+            const f32x4_t y = f32x4_t{o[et][4 * q], o[et][4 * q + 1], o[et][4 * q + 2], o[et][4 * q + 3]} * inv;
+            if (e < D) {
+                if (a.splits == 1)
+                    store4(out + e, y);
+                else
+                    store4(a.part_o + slot * D + e, y);
+            }
+        }
+    if (a.splits > 1 && half == 0)
+        a.part_ml[slot] = make_float2(m_run, l_run);
 }
 
 // The shares of a (row, head) joined: a work-group each.  D / 4 lanes hold a row, the
@@ -365,10 +743,10 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_batch_join(BatchAttnArgs a) {
 
 // Tiles, and shares of the keys, from the sizes alone (what lies in device memory
 // is not known here).
-void plan(BatchAttnArgs *a) {
-    a->tile = 16;
-    a->block = KB;
+void plan(BatchAttnArgs *a, bool bf16) {
     const int64_t most = (int64_t)a->max_rows * a->G;
+    a->tile = !bf16 ? 16 : most <= 64 ? 64 : 128;
+    a->block = KB;
     a->one_tile = most <= a->tile;
     a->slots = (int32_t)(a->one_tile ? a->n_seqs : (int64_t)a->n * a->G / a->tile + a->n_seqs);
     const int blocks = (a->max_length + a->block - 1) / a->block;
@@ -383,17 +761,37 @@ size_t workspace_of(const BatchAttnArgs &a, int D) {
     return a.splits == 1 ? 0 : o_bytes(a, D) + sizeof(float2) * (size_t)a.splits * a.n * a.n_heads;
 }
 
-template <typename TX, typename TK>
+template <typename TX>
 void launch_f32(const BatchAttnArgs &a, int D, hipStream_t s) {
     const dim3 grid((unsigned)(a.slots * a.n_kv_heads), (unsigned)a.splits), block(NW * 64);
     if (D == 16)
-        hipLaunchKernelGGL((k_batch_attn_f32<TX, TK, 16>), grid, block, 0, s, a);
+        hipLaunchKernelGGL((k_batch_attn_f32<TX, 16>), grid, block, 0, s, a);
     else if (D == 32)
-        hipLaunchKernelGGL((k_batch_attn_f32<TX, TK, 32>), grid, block, 0, s, a);
+        hipLaunchKernelGGL((k_batch_attn_f32<TX, 32>), grid, block, 0, s, a);
     else if (D == 64)
-        hipLaunchKernelGGL((k_batch_attn_f32<TX, TK, 64>), grid, block, 0, s, a);
+        hipLaunchKernelGGL((k_batch_attn_f32<TX, 64>), grid, block, 0, s, a);
     else
-        hipLaunchKernelGGL((k_batch_attn_f32<TX, TK, 128>), grid, block, 0, s, a);
+        hipLaunchKernelGGL((k_batch_attn_f32<TX, 128>), grid, block, 0, s, a);
+}
+
+template <typename TX, int D>
+void launch_mfma(const BatchAttnArgs &a, hipStream_t s) {
+    const dim3 grid((unsigned)(a.slots * a.n_kv_heads * a.splits));
+    if (a.tile == 64)
+        hipLaunchKernelGGL((k_batch_attn_mfma<TX, D, 2, 2>), grid, dim3(256), 0, s, a);
+    else
+        hipLaunchKernelGGL((k_batch_attn_mfma<TX, D, 4, 1>), grid, dim3(256), 0, s, a);
+}
+template <typename TX>
+void launch_bf16(const BatchAttnArgs &a, int D, hipStream_t s) {
+    if (D == 16)
+        launch_mfma<TX, 16>(a, s);
+    else if (D == 32)
+        launch_mfma<TX, 32>(a, s);
+    else if (D == 64)
+        launch_mfma<TX, 64>(a, s);
+    else
+        launch_mfma<TX, 128>(a, s);
 }
 
 template <typename TX>
@@ -436,13 +834,13 @@ sd_status check_call(const void *q, int64_t ld_q, int32_t x_dtype, int32_t n_hea
 sd_status launch(const BatchAttnArgs &a, int32_t x_dtype, int32_t dtype, int D, hipStream_t s) {
     if (x_dtype == SD_BF16) {
         if (dtype == SD_BF16)
-            launch_f32<uint16_t, uint16_t>(a, D, s);
+            launch_bf16<uint16_t>(a, D, s);
         else
-            launch_f32<uint16_t, float>(a, D, s);
+            launch_f32<uint16_t>(a, D, s);
     } else if (dtype == SD_BF16) {
-        launch_f32<float, uint16_t>(a, D, s);
+        launch_bf16<float>(a, D, s);
     } else {
-        launch_f32<float, float>(a, D, s);
+        launch_f32<float>(a, D, s);
     }
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && a.splits > 1) {
@@ -491,7 +889,7 @@ sd_status paged_attention(const sd_kv_pages *kv, const sd_batch *batch, const vo
     if (st != SD_OK || (st = check_call(q, ld_q, x_dtype, n_heads, n, a.n_seqs, a.n_kv_heads, kv->head_dim, out, ld_out,
                                         &scale)) != SD_OK)
         return st;
-    plan(&a);
+    plan(&a, kv->dtype == SD_BF16);
     const size_t need = workspace_of(a, kv->head_dim);
     if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need))
         return report(SD_ERR_INVALID_ARG, "these sizes need " + std::to_string(need) +
@@ -537,7 +935,7 @@ sd_status prompt_attention(const sd_kv_layer *kv, const int32_t *starts, int32_t
     a.n_heads = n_heads;
     a.n_kv_heads = kv->n_kv_heads;
     a.G = n_heads / kv->n_kv_heads;
-    plan(&a);
+    plan(&a, kv->dtype == SD_BF16);
     return launch(a, x_dtype, kv->dtype, kv->head_dim, s);
 }
 
@@ -551,7 +949,7 @@ size_t sd_paged_attention_workspace(const sd_kv_pages *kv, const sd_batch *batch
     if (paged_sizes(kv, batch, n_heads, n, false, &a) != SD_OK ||
         check_call(nullptr, 0, x_dtype, n_heads, n, a.n_seqs, a.n_kv_heads, kv->head_dim, nullptr, 0, nullptr) != SD_OK)
         return 0;
-    plan(&a);
+    plan(&a, kv->dtype == SD_BF16);
     return workspace_of(a, kv->head_dim);
 }
 
