@@ -20,6 +20,8 @@ using namespace sdk;
 
 namespace {
 
+constexpr int KB = 64, KB_FEW = 32, NW = 4;  // keys of a block; waves
+
 struct BatchAttnArgs {
     const void *q;
     int64_t ld_q;
@@ -36,6 +38,9 @@ struct BatchAttnArgs {
     float scale;      // of the scores, times log2(e)
     int32_t n, n_seqs, max_rows, max_length, n_pages, page_shift;
     int32_t n_heads, n_kv_heads, G;
+    int32_t paged;                     // whether over pages
+    int32_t chunks, least, span;       // of the streams: chunks (0: no streams), spans of one at least, keys of a span
+    int32_t *spans;                    // [n_seqs + 2]: spans before each sequence, and of a chunk
     int32_t tile, slots, one_tile;     // rows of a tile; tiles at most; whether a sequence has at most one
     int32_t splits, per_split, block;  // shares of the keys; blocks of a share; keys of a block
 };
@@ -74,12 +79,13 @@ __device__ __forceinline__ Tile tile_of(const BatchAttnArgs &a, int32_t t) {
     return w;
 }
 
-// The NW waves' states of ROWS rows from row0 on (o [wave][row][D + 4], waves
-// `pitch` floats apart; (maximum, sum) [wave][row]) merged in wave order: the
-// result of a single share, or its part of several.
-template <typename TX, int D, int NW, int ROWS>
+// The waves' states of ROWS rows from row0 on (o [wave][row][D + 4], waves `pitch`
+// floats apart; (maximum, sum) [wave][row]) merged in wave order: the result, or with
+// part >= 0 that part's state, its rows adjacent there from `part` on, or by
+// packed row and head with a.chunks 0.
+template <typename TX, int D, int ROWS>
 __device__ __forceinline__ void merge_waves(const BatchAttnArgs &a, const Tile &w, const float *o, int pitch,
-                                            const float2 *ml, int g, int split) {
+                                            const float2 *ml, int g, int part) {
 #pragma unroll
     for (int i = threadIdx.x; i < ROWS * D / 4; i += NW * 64) {
         const int rc = i / (D / 4), e = 4 * (i % (D / 4)), rr = w.row0 + rc;
@@ -100,16 +106,87 @@ __device__ __forceinline__ void merge_waves(const BatchAttnArgs &a, const Tile &
         }
         const int node = rr / a.G, head = g * a.G + rr - node * a.G;
         const int64_t row = w.rows.first + node;
-        if (a.splits == 1) {
+        if (part < 0) {
             store4(static_cast<TX *>(a.out) + row * a.ld_out + (int64_t)head * D + e,
                    L == 0.0f ? f32x4_t{0.0f, 0.0f, 0.0f, 0.0f} : O / L);
         } else {
-            const int64_t slot = ((int64_t)split * a.n + row) * a.n_heads + head;
+            const int64_t slot = a.chunks ? (int64_t)part * a.tile + rc : ((int64_t)part * a.n + row) * a.n_heads + head;
             store4(a.part_o + slot * D + e, O);
             if (e == 0)
                 a.part_ml[slot] = make_float2(m, L);
         }
     }
+}
+
+// ---------------------------------------------------------------------------
+// Streams.  Where every sequence is one tile, the keys of a kv head are one stream:
+// the spans (of `span` keys) of all its sequences one after the other, cut into
+// chunks of as many spans each, a work-group a chunk.  So every work-group
+// has the same work, whatever the lengths are: 64 sequences of 500 to 8000 keys
+// took 224 us with a work-group a sequence, 190 of 4250 each.  A chunk that holds a sequence
+// whole normalises its result; of others a chunk has at most two, one that began
+// before it (part 0) and one that goes on after it (part 1).
+constexpr int MAX_STREAM = 1024;  // sequences: every work-group adds up their spans
+
+struct Stream {
+    int32_t pre[MAX_STREAM + 1], wave[NW], first;
+};
+// Spans of a sequence: one at least where it has rows, which get zeros.
+__device__ __forceinline__ int32_t spans_of(const BatchAttnArgs &a, const SeqRows &r) {
+    return r.m == 0 ? 0 : max(1, (seen_from(r.past + r.m - 1, a.max_length) + a.span - 1) / a.span);
+}
+// The spans [at, end) of chunk c and the sequence that `at` is in; false: none.
+__device__ __forceinline__ bool chunk_of(const BatchAttnArgs &a, Stream &st, int32_t c, int32_t *at, int32_t *end,
+                                         int32_t *seq) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, per = (a.n_seqs + NW * 64 - 1) / (NW * 64);
+    int32_t own[MAX_STREAM / (NW * 64)], sum = 0;
+#pragma unroll
+    for (int j = 0; j < MAX_STREAM / (NW * 64); ++j) {
+        const int s = tid * per + j;
+        own[j] = j < per && s < a.n_seqs ? spans_of(a, rows_of(a, s)) : 0;
+        sum += own[j];
+    }
+    int32_t upto = sum;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int32_t y = __shfl_up(upto, d, 64);
+        upto += lane >= d ? y : 0;
+    }
+    if (lane == 63)
+        st.wave[wave] = upto;
+    __syncthreads();
+    int32_t before = upto - sum, total = 0;
+#pragma unroll
+    for (int v = 0; v < NW; ++v) {
+        before += v < wave ? st.wave[v] : 0;
+        total += st.wave[v];
+    }
+    const int32_t len = max((total + a.chunks - 1) / a.chunks, a.least);
+    *at = c * len;
+    *end = min(*at + len, total);
+#pragma unroll
+    for (int j = 0; j < MAX_STREAM / (NW * 64); ++j) {
+        const int s = tid * per + j;
+        if (j < per && s < a.n_seqs) {
+            st.pre[s] = before;
+            if (before <= *at && *at < before + own[j])
+                st.first = s;
+            before += own[j];
+            if (s == a.n_seqs - 1)
+                st.pre[a.n_seqs] = before;
+        }
+    }
+    __syncthreads();
+    *seq = st.first;
+    return *at < *end;
+}
+// What the join reads, by one work-group.
+__device__ __forceinline__ void keep_spans(const BatchAttnArgs &a, const Stream &st) {
+    const int32_t total = st.pre[a.n_seqs], len = max((total + a.chunks - 1) / a.chunks, a.least);
+    for (int s = threadIdx.x; s <= a.n_seqs; s += NW * 64)
+        a.spans[s] = st.pre[s];
+    if (threadIdx.x == 0)
+        a.spans[a.n_seqs + 1] = len;
 }
 
 // ---------------------------------------------------------------------------
@@ -123,7 +200,6 @@ __device__ __forceinline__ void merge_waves(const BatchAttnArgs &a, const Tile &
 // elements of row 4 g + v are a lane's operands of four tiles.  V is asked for before
 // the scores and the next block's K after them.  The waves keep states of their
 // own and merge at the end.  A wave's 16 keys lie in one page.
-constexpr int KB = 64, NW = 4;
 
 template <typename TX, int D>
 __global__ __launch_bounds__(NW * 64, 2) void k_batch_attn_f32(BatchAttnArgs a) {
@@ -291,7 +367,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_batch_attn_f32(BatchAttnArgs a) 
     if (g4 == 0)
         ml[wave][c] = make_float2(m_run, l_run);
     __syncthreads();
-    merge_waves<TX, D, NW, 16>(a, w, &tile[0][0], 16 * OP, &ml[0][0], g, split);
+    merge_waves<TX, D, 16>(a, w, &tile[0][0], 16 * OP, &ml[0][0], g, a.splits > 1 ? split : -1);
 }
 
 // ---------------------------------------------------------------------------
@@ -326,30 +402,43 @@ struct Entries {
 };
 __device__ __forceinline__ Entries entries_of(const BatchAttnArgs &a, const Tile &w, int first, int klen) {
     Entries e;
+    if (!a.table)
+        return e;
+    const int32_t *row = a.table + (int64_t)w.seq * a.ld_table;
+    e.page[0] = first < klen ? row[first >> a.page_shift] : -1;
+    if (a.page_shift < 6) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int f = first + 16 * j;
-        e.page[j] = a.table && f < klen ? a.table[(int64_t)w.seq * a.ld_table + (f >> a.page_shift)] : -1;
+        for (int j = 1; j < 4; ++j)
+            e.page[j] = first + 16 * j < klen ? row[(first + 16 * j) >> a.page_shift] : -1;
     }
     return e;
 }
 __device__ __forceinline__ Groups groups_of(const BatchAttnArgs &a, const Tile &w, const Entries &e, int first, int klen) {
     Groups k;
-    k.ok = 0;
+    k.ok = 15;  // (keys past the last are masked by their number)
+    if (a.table && a.page_shift < 6) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int f = first + 16 * j;
-        if (a.table) {
+        for (int j = 0; j < 4; ++j) {
             // (without a page: any rows, which are masked, and taken for finite)
             const int page = __builtin_amdgcn_readfirstlane(e.page[j]);
             const bool there = (uint32_t)page < (uint32_t)a.n_pages;
-            k.off[j] = (there ? page * a.page_stride : 0) + (int64_t)(f & ((1 << a.page_shift) - 1)) * a.row_stride;
-            k.ok |= there ? 1u << j : 0u;
-        } else {
-            k.off[j] = (int64_t)(w.rows.first + f) * a.row_stride;
-            k.ok |= f < klen ? 1u << j : 0u;
+            k.off[j] = (there ? page * a.page_stride : 0) +
+                       (int64_t)((first + 16 * j) & ((1 << a.page_shift) - 1)) * a.row_stride;
+            k.ok &= there || first + 16 * j >= klen ? 15u : ~(1u << j);
         }
+        return k;
     }
+    if (a.table) {
+        const int page = __builtin_amdgcn_readfirstlane(e.page[0]);
+        const bool there = (uint32_t)page < (uint32_t)a.n_pages;
+        k.off[0] = (there ? page * a.page_stride : 0) + (int64_t)(first & ((1 << a.page_shift) - 1)) * a.row_stride;
+        k.ok = there ? 15 : 0;
+    } else {
+        k.off[0] = (int64_t)(w.rows.first + first) * a.row_stride;
+    }
+#pragma unroll
+    for (int j = 1; j < 4; ++j)
+        k.off[j] = k.off[0] + 16 * j * a.row_stride;
     return k;
 }
 // The keys of a block that are seen by one who sees `count` of them, as bits.
@@ -390,15 +479,16 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_batch_attn_mfma(BatchAttnAr
     const uint16_t *K = static_cast<const uint16_t *>(a.k) + (int64_t)g * a.head_stride;
     const uint16_t *V = static_cast<const uint16_t *>(a.v) + (int64_t)g * a.head_stride;
 
-    // A wave takes every WAVES-th KB of K's and of V's rows.  Whole groups: lane
-    // offsets that do not change, from the group's first row.
+    // A wave takes every WAVES-th KB of K's and of V's rows.  Whole blocks: lane
+    // offsets that do not change, from the block's first row where its rows follow
+    // one another (packed, or pages of a block and more), else from a group's.
     constexpr int NU = (L::C + WAVES - 1) / WAVES, ROWS = 4 * L::RPL;  // loads of a wave; rows of a load
-    const bool near = D > 16 && near_rows(a.row_stride);
+    const bool one = !a.table || a.page_shift >= 6, near = (one || D > 16) && near_rows(a.row_stride);
     uint32_t off[NU];
 #pragma unroll
     for (int i = 0; i < NU; ++i) {
         const int u = wave + WAVES * i, s = 4 * u + (lane >> 4), p = (lane & 15) ^ L::swz(s);
-        off[i] = (uint32_t)(2 * ((int64_t)((s * L::RPL + p / L::C) & 15) * a.row_stride + 8 * (p % L::C)));
+        off[i] = (uint32_t)(2 * ((int64_t)((s * L::RPL + p / L::C) & (one ? 63 : 15)) * a.row_stride + 8 * (p % L::C)));
     }
     auto load_block = [&](const Groups &k, int first, int buf) {
         if (first + KB <= klen && near) {
@@ -406,7 +496,7 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_batch_attn_mfma(BatchAttnAr
             for (int i = 0; i < NU; ++i) {
                 const int u = wave + WAVES * i;
                 if (L::C % WAVES == 0 || u < L::C) {  // uniform over the wave
-                    const int j = ROWS * u / 16;
+                    const int j = one ? 0 : ROWS * u / 16;
                     const int64_t at = j == 0 ? k.off[0] : j == 1 ? k.off[1] : j == 2 ? k.off[2] : k.off[3];
                     load_to_lds16(K + at, off[i], &kv[buf][0][u * 512]);
                     load_to_lds16(V + at, off[i], &kv[buf][1][u * 512]);
@@ -508,6 +598,81 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_batch_attn_mfma(BatchAttnAr
                 odd |= hit;
             }
             odd = __syncthreads_or(odd);
+        }
+        if constexpr (!EXACT && NK == 1) {
+            // A whole block's 64 keys at once: the reads of K run ahead of their
+            // products, those of V under the softmax.
+            if (full) {
+                if (!live)
+                    continue;
+                int xk = 2 * (buf * 2 * KB * D + L::at(col, half)), xv = 2 * buf * 2 * KB * D + v_lane;
+                asm volatile("" : "+v"(xk), "+v"(xv));
+                f32x16_t s[2];
+                u32x4_t kf[ES][2];
+#pragma unroll
+                for (int e = 0; e < ES; ++e)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        kf[e][h] = *reinterpret_cast<const u32x4_t *>(lds + (xk ^ (32 * e)) + 2 * 32 * h * D);
+                __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+                for (int e = 0; e < ES; ++e)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        s[h] = mfma32(kf[e][h], qf[e][0], e == 0 ? f32x16_t{} : s[h]);
+                __builtin_amdgcn_s_setprio(0);
+                // V^T: keys 16 j + 8 I + 4 half + 0 .. 3 of tile et
+                u32x4_t vf[4][ET];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int et = 0; et < ET; ++et)
+#pragma unroll
+                        for (int I = 0; I < 2; ++I) {
+                            const char *src = lds + (xv ^ (64 * et) ^ (I ? (D == 16 ? 16 : 32) : 0)) + 2 * (16 * j + 8 * I) * D;
+                            const u32x2_t y =
+                                __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)src));
+                            vf[j][et][2 * I] = y[0];
+                            vf[j][et][2 * I + 1] = y[1];
+                        }
+                float mx = s[0][0];
+#pragma unroll
+                for (int v = 1; v < 32; ++v)
+                    mx = fmaxf(mx, s[v >> 4][v & 15]);
+                {
+                    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+                    mx = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])) * factor;
+                }
+                const bool grows = mx > m_run + SLACK;
+                if (__any(grows)) {
+                    const float m_new = grows ? mx : m_run;
+                    const float sc = m_run == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run - m_new);
+                    l_run *= sc;
+#pragma unroll
+                    for (int et = 0; et < ET; ++et)
+                        o[et] *= sc;
+                    m_run = m_new;
+                }
+                const float m_use = m_run == -INFINITY ? 0.0f : m_run;
+                float sum[4] = {};
+                u32x4_t pf[4];
+#pragma unroll
+                for (int v = 0; v < 32; v += 2) {
+                    const float p0 = __builtin_amdgcn_exp2f(fmaf(s[v >> 4][v & 15], factor, -m_use));
+                    const float p1 = __builtin_amdgcn_exp2f(fmaf(s[v >> 4][(v & 15) + 1], factor, -m_use));
+                    sum[v >> 3] += p0 + p1;
+                    pf[v >> 3][(v >> 1) & 3] = cvt_pk(p0, p1);
+                }
+                l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int et = 0; et < ET; ++et)
+                        o[et] = mfma32(vf[j][et], pf[j], o[et]);
+                __builtin_amdgcn_s_setprio(0);
+                continue;
+            }
         }
         const uint64_t visible = full ? ~0ull : seen_bits(see - first, now.ok);
 #pragma unroll 1
@@ -688,6 +853,354 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_batch_attn_mfma(BatchAttnAr
         a.part_ml[slot] = make_float2(m_run, l_run);
 }
 
+// ---------------------------------------------------------------------------
+// The same for up to 32 rows of a kv head (one token of up to 32 query heads, or a
+// few), where the read of the cache counts and not the products: four waves, each
+// with 32-key blocks of its own and no barrier until the end.  K goes straight
+// into registers as the A operand of 16x16x32 score products, V straight into the
+// wave's LDS, both one block ahead.  Lane (col, grp) receives the keys 16 t + 4 grp +
+// v of row col, which are the slots u = 4 t + v that the value products take from it.
+// LDS lines are permuted for the reads here: eight rows, two adjacent chunks each.
+// A lane holds the table's entry for half a block of the wave, 32 blocks at a time.
+// A work-group takes a sequence whole, or the chunk of a stream.
+template <typename TX, int D, int QT>
+__global__ __launch_bounds__(256, QT == 1 || D < 128 ? 2 : 1) void k_batch_attn_few(BatchAttnArgs a) {
+    constexpr bool EXACT = sizeof(TX) == 4;
+    constexpr int T = EXACT ? X_TERMS : 1, ES = D < 32 ? 1 : D / 32, ET = D / 16, ROWS = 16 * QT, OP = D + 4;
+    using L = FewLines<D>;
+    constexpr int VB = KB_FEW * D;  // elements of a V block
+    constexpr int WORDS = VB > ROWS * OP ? VB : ROWS * OP;
+    __shared__ __attribute__((aligned(1024))) uint32_t tile[NW][WORDS];  // two V blocks, or the outputs
+    __shared__ float2 ml[NW][ROWS];
+    __shared__ Stream stream;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 15,
+              grp = lane >> 4;
+    const int g = blockIdx.x % a.n_kv_heads, chunk = blockIdx.x / a.n_kv_heads;
+    int32_t seq = chunk, at = 0, end = 1;
+    if (a.chunks) {
+        const bool some = chunk_of(a, stream, chunk, &at, &end, &seq);
+        if (blockIdx.x == 0)
+            keep_spans(a, stream);
+        if (!some)
+            return;  // uniform
+    }
+    for (;;) {
+    seq = __builtin_amdgcn_readfirstlane(seq);
+    const int32_t from = a.chunks ? __builtin_amdgcn_readfirstlane(at - stream.pre[seq]) : 0;
+    const int32_t all = a.chunks ? __builtin_amdgcn_readfirstlane(stream.pre[seq + 1] - stream.pre[seq]) : 1 << 30;
+    const int32_t to = a.chunks ? min(all, from + end - at) : all;
+    constexpr int BLOCKS = NW;  // of a span
+    const int b0 = BLOCKS * from + wave;
+    // the entries of this wave's blocks b .., of groups past the table none
+    const int32_t *table = a.table + (int64_t)seq * a.ld_table;
+    auto entries_from = [&](int b) {
+        const int64_t first = KB_FEW * ((int64_t)b + NW * (lane >> 1)) + 16 * (lane & 1);
+        return first < a.max_length ? table[first >> a.page_shift] : -1;
+    };
+    int entries = entries_from(b0);
+    Tile w;
+    w.seq = seq;
+    w.row0 = 0;
+    w.rows = rows_of(a, seq);
+    const int rows = w.rows.m * a.G;
+    if (rows == 0)
+        return;  // uniform (no sequence of a stream's)
+    const int klen = __builtin_amdgcn_readfirstlane(seen_from(w.rows.past + w.rows.m - 1, a.max_length));
+    const int kall = __builtin_amdgcn_readfirstlane(seen_from(w.rows.past, a.max_length));
+    const int64_t last = (int64_t)BLOCKS * to;
+    const int b1 = (int)min(last, (int64_t)(klen + KB_FEW - 1) / KB_FEW);
+    const uint16_t *K = static_cast<const uint16_t *>(a.k) + (int64_t)g * a.head_stride;
+    const uint16_t *V = static_cast<const uint16_t *>(a.v) + (int64_t)g * a.head_stride;
+    uint16_t *vt = reinterpret_cast<uint16_t *>(tile[wave]);
+
+    // Where the halves of a block start (elements), and whether they have a page.
+    struct Halves {
+        int64_t off[2];
+        int ok;
+    };
+    auto halves_of = [&](int b, int slot) {  // slot: among the entries
+        Halves h;
+        h.ok = 0;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            // (without a page: any rows, which are masked, and taken for finite)
+            const int page = __builtin_amdgcn_readlane(entries, 2 * slot + t);
+            const bool there = (uint32_t)page < (uint32_t)a.n_pages;
+            h.off[t] = (there ? page * a.page_stride : 0) +
+                       (int64_t)((KB_FEW * b + 16 * t) & ((1 << a.page_shift) - 1)) * a.row_stride;
+            h.ok |= there ? 1 << t : 0;
+        }
+        return h;
+    };
+    // Whole blocks: lane offsets that do not change, from a half's first row.
+    // (Of V's loads u, only the lane's place in odd and even ones differs.)
+    const bool near = D > 16 && near_rows(a.row_stride);
+    const uint32_t koff = (uint32_t)(2 * ((int64_t)col * a.row_stride + (8 * grp) % D));
+    uint32_t voff[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const int s = 4 * u + (lane >> 4), p = (lane & 15) ^ L::swz(s);
+        voff[u] = (uint32_t)(2 * ((int64_t)((lane >> 4) * L::RPL + p / L::C) * a.row_stride + 8 * (p % L::C)));
+    }
+    u32x4_t kf[2][ES];
+    auto load_k = [&](const Halves &h, int first) {
+        const bool whole = first + KB_FEW <= klen && near;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            // keys past the last: that one, masked; head_dim 16: the upper slots are zeros of q
+            const int r = min(16 * t + col, klen - 1 - first);
+            const char *kp = whole ? reinterpret_cast<const char *>(K + h.off[t]) + koff
+                                   : reinterpret_cast<const char *>(K + (r < 16 ? h.off[0] : h.off[1]) +
+                                                                    (r & 15) * a.row_stride + (8 * grp) % D);
+#pragma unroll
+            for (int s = 0; s < ES; ++s)
+                kf[t][s] = *reinterpret_cast<const u32x4_t *>(kp + 64 * s);
+        }
+    };
+    auto load_v = [&](const Halves &h, int first, int buf) {
+        constexpr int LOAD_ROWS = 4 * L::RPL;
+        if (first + KB_FEW <= klen && near) {
+#pragma unroll
+            for (int u = 0; u < VB / 512; ++u)
+                load_to_lds16(V + h.off[LOAD_ROWS * u / 16] + (int64_t)(LOAD_ROWS * u % 16) * a.row_stride, voff[u & 1],
+                              vt + buf * VB + u * 512);
+        } else {
+#pragma unroll 1
+            for (int u = 0; u < VB / 512; ++u) {
+                const int s = 4 * u + (lane >> 4), p = (lane & 15) ^ L::swz(s);
+                const int r = min(s * L::RPL + p / L::C, klen - 1 - first);
+                load_to_lds16(V + (r < 16 ? h.off[0] : h.off[1]) + (r & 15) * a.row_stride + 8 * (p % L::C),
+                              vt + buf * VB + u * 512);
+            }
+        }
+    };
+    Halves k{};
+    int b = b0, slot = 0;
+    if (b < b1) {
+        k = halves_of(b, 0);
+        load_k(k, KB_FEW * b);
+        load_v(k, KB_FEW * b, 0);
+    }
+    int see[QT];
+    u32x4_t qf[QT][ES][T];
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+        const int row = min(16 * i + col, rows - 1), node = row / a.G;
+        see[i] = seen_from(w.rows.past + node, a.max_length);
+        const TX *qs = static_cast<const TX *>(a.q) + (int64_t)(w.rows.first + node) * a.ld_q +
+                       (int64_t)(g * a.G + row - node * a.G) * D + (8 * grp) % D;
+        const bool none = (D < 32 && grp >= 2) || 16 * i + col >= rows;  // head_dim 16: the upper half of the reduction
+#pragma unroll
+        for (int s = 0; s < ES; ++s) {
+            if constexpr (EXACT) {
+                const float scale = a.scale;
+                f32x4_t x0 = load4(qs + 32 * s) * scale, x1 = load4(qs + 32 * s + 4) * scale;
+                if (none)
+                    x0 = x1 = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+                query_terms(x0, x1, qf[i][s]);
+            } else {
+                // (a negative scale as one of q, so that the largest score stays the largest)
+                const u32x4_t x = *reinterpret_cast<const u32x4_t *>(qs + 32 * s);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    qf[i][s][0][j] = none ? 0u : x[j] ^ (a.scale < 0.0f ? 0x80008000u : 0u);
+            }
+        }
+    }
+    // (a scale that float32 products would take for zero would make NaN of a masked score)
+    const float factor = EXACT ? 1.0f : fmaxf(fabsf(a.scale), 1.17549435e-38f);
+    float m_run[QT], l_run[QT];
+    f32x4_t o[QT][ET];
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+        m_run[i] = -INFINITY;
+        l_run[i] = 0.0f;
+#pragma unroll
+        for (int et = 0; et < ET; ++et)
+            o[i][et] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    const int v_lane = 2 * L::at(4 * grp + (col >> 2), (col & 3) >> 1) + 8 * (col & 1);
+    const char *vb = reinterpret_cast<const char *>(vt);
+
+    int buf = 0;
+    for (; b < b1; b += NW, buf ^= 1) {
+        const int first = KB_FEW * b;
+        const Halves now = k;
+        f32x4_t s[QT][2];
+#pragma unroll
+        for (int i = 0; i < QT; ++i)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                s[i][t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int e = 0; e < ES; ++e)
+#pragma unroll
+                    for (int u = 0; u < T; ++u)
+                        s[i][t] = mfma16(kf[t][e], qf[i][e][u], s[i][t]);
+            }
+        // this block's V has landed (it was asked for before this block's K, or
+        // just after), then the next block's loads
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (b + NW < b1) {
+            if (++slot == 32) {
+                slot = 0;
+                entries = entries_from(b + NW);
+            }
+            k = halves_of(b + NW, slot);
+            load_v(k, first + NW * KB_FEW, buf ^ 1);
+            load_k(k, first + NW * KB_FEW);
+        }
+        const bool full = first + KB_FEW <= kall && now.ok == 3;  // every row sees every key
+        // Infinities and NaN among values that some row does not see: it must not
+        // add 0 times one.  They are taken out here, and put where they belong
+        // beside the products.
+        bool odd = false;
+        if (!full) {
+            u32x4_t *vw = reinterpret_cast<u32x4_t *>(vt + buf * VB);
+            for (int c = lane; c < VB / 8; c += 64) {
+                u32x4_t x = vw[c];
+                bool hit = false;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t y = without_odd(x[j]);
+                    hit |= y != x[j];
+                    x[j] = y;
+                }
+                if (hit)
+                    vw[c] = x;
+                odd |= hit;
+            }
+            odd = __any(odd);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
+        // (a tile's rows at a time: V again from LDS for the second costs less than
+        // the registers of both)
+#pragma unroll
+        for (int i = 0; i < QT; ++i) {
+            float p[8], mx = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                p[u] = s[i][u >> 2][u & 3];
+            if (!full) {
+                const int count = see[i] - first;
+                uint32_t own = count >= 32 ? ~0u : count <= 0 ? 0u : (1u << count) - 1;
+                own = (own & ((now.ok & 1 ? 0xffffu : 0u) | (now.ok & 2 ? 0xffff0000u : 0u))) >> (4 * grp);
+                asm volatile("" : "+v"(own));  // (a branch, and not selects in every block)
+#pragma unroll
+                for (int u = 0; u < 8; ++u)
+                    p[u] = (own >> (16 * (u >> 2) + (u & 3))) & 1 ? p[u] : -INFINITY;
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                mx = fmaxf(mx, p[u]);
+            mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+            if constexpr (!EXACT)
+                mx *= factor;
+            const bool grows = mx > m_run[i] + SLACK;
+            if (__any(grows)) {
+                const float m_new = grows ? mx : m_run[i];
+                const float sc = m_run[i] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run[i] - m_new);
+                l_run[i] *= sc;
+#pragma unroll
+                for (int et = 0; et < ET; ++et)
+                    o[i][et] *= sc;
+                m_run[i] = m_new;
+            }
+            const float m_use = m_run[i] == -INFINITY ? 0.0f : m_run[i];
+            float sum = 0.0f;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                p[u] = __builtin_amdgcn_exp2f(EXACT ? p[u] - m_use : fmaf(p[u], factor, -m_use));
+                sum += p[u];
+            }
+            l_run[i] += sum;
+            if (odd) {
+                // lane (col, grp) holds elements 16 et + 4 grp + u of row col
+#pragma unroll 1
+                for (int key = 0; key < KB_FEW; ++key) {
+                    float pk = 0.0f;
+                    const int own = 4 * (key >> 4) + (key & 3);
+#pragma unroll
+                    for (int u = 0; u < 8; ++u)
+                        pk = u == own ? p[u] : pk;
+                    pk = __shfl(pk, col + 16 * ((key >> 2) & 3), 64);
+                    const int r = min(key, klen - 1 - first);
+                    const uint16_t *vr = V + (r < 16 ? now.off[0] : now.off[1]) + (r & 15) * a.row_stride + 4 * grp;
+#pragma unroll
+                    for (int et = 0; et < ET; ++et) {
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) {
+                            const float x = load1(vr + 16 * et + u);
+                            if (pk != 0.0f && !finite(x))
+                                o[i][et][u] = fmaf(pk, x, o[i][et][u]);
+                        }
+                        __builtin_amdgcn_sched_barrier(0);  // a few loads at a time: registers
+                    }
+                }
+            }
+            u32x4_t pf[T];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (EXACT) {
+                    uint32_t t[T];
+                    terms2(p[2 * j], p[2 * j + 1], t);
+#pragma unroll
+                    for (int u = 0; u < T; ++u)
+                        pf[u][j] = t[u];
+                } else {
+                    pf[0][j] = cvt_pk(p[2 * j], p[2 * j + 1]);
+                }
+            }
+            // A operand V^T: column 16 et + col of keys 16 I + 4 grp + 0..3
+            int xv = v_lane + 2 * buf * VB;
+            asm volatile("" : "+v"(xv));
+#pragma unroll
+            for (int et = 0; et < ET; ++et) {
+                u32x4_t vf;
+#pragma unroll
+                for (int I = 0; I < 2; ++I) {
+                    const char *src = vb + (xv ^ (32 * et)) + 2 * 16 * I * D;
+                    const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)src);
+                    const u32x2_t y = __builtin_bit_cast(u32x2_t, x);
+                    vf[2 * I] = y[0];
+                    vf[2 * I + 1] = y[1];
+                }
+#pragma unroll
+                for (int u = 0; u < T; ++u)
+                    o[i][et] = mfma16(vf, pf[u], o[i][et]);
+            }
+        }
+        // (every read of this block has returned before its buffer is filled again)
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+    // the waves' states, merged in wave order
+    float *mine = reinterpret_cast<float *>(tile[wave]);
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+        l_run[i] += __shfl_xor(l_run[i], 16, 64);
+        l_run[i] += __shfl_xor(l_run[i], 32, 64);
+#pragma unroll
+        for (int et = 0; et < ET; ++et)
+            *reinterpret_cast<f32x4_t *>(mine + (16 * i + col) * OP + 16 * et + 4 * grp) = o[i][et];
+        if (grp == 0)
+            ml[wave][16 * i + col] = make_float2(m_run[i], l_run[i]);
+    }
+    __syncthreads();
+    const bool whole = !a.chunks || (from == 0 && to == all);
+    merge_waves<TX, D, ROWS>(a, w, reinterpret_cast<const float *>(tile), WORDS, &ml[0][0], g,
+                             whole ? -1 : 2 * (g * a.chunks + chunk) + (from == 0));
+    at += to - from;
+    if (!a.chunks || at >= end)
+        return;
+    // the next sequence that has spans
+    do
+        ++seq;
+    while (stream.pre[seq + 1] <= at);
+    __syncthreads();
+    }
+}
+
 // The shares of a (row, head) joined: a work-group each.  D / 4 lanes hold a row, the
 // groups of lanes take the shares in turn and add up in order.
 constexpr int JOIN_THREADS = 256;
@@ -741,24 +1254,108 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_batch_join(BatchAttnArgs a) {
            total == 0.0f ? f32x4_t{0.0f, 0.0f, 0.0f, 0.0f} : O / total);
 }
 
+// The parts of a sequence joined, of a stream's chunks: a work-group a row of a
+// (sequence, kv head).
+template <typename TX, int D, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_batch_join_stream(BatchAttnArgs a, int rows_most) {
+    constexpr int LANES = D / 4, NG = THREADS / LANES;
+    __shared__ f32x4_t red[NG][LANES];
+    const int lane = threadIdx.x & 63, e = threadIdx.x % LANES, gi = threadIdx.x / LANES;
+    const int rr = blockIdx.x % rows_most, unit = blockIdx.x / rows_most, g = unit % a.n_kv_heads,
+              s = unit / a.n_kv_heads;
+    const int32_t at = a.spans[s], end = a.spans[s + 1], len = a.spans[a.n_seqs + 1];
+    const SeqRows rows = rows_of(a, s);
+    if (rr >= rows.m * a.G || at == end)
+        return;  // uniform
+    const int c0 = at / len, parts = (end - 1) / len - c0 + 1;
+    if (parts == 1)
+        return;
+    // the first is part 1 of its chunk, the others are part 0
+    auto slot_of = [&](int j) { return (int64_t)(2 * (g * a.chunks + c0 + j) + (j == 0)) * a.tile + rr; };
+    constexpr int J = 4;
+    f32x4_t x[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+        x[j] = load4(a.part_o + slot_of(min(gi + j * NG, parts - 1)) * D + 4 * e);
+    const float2 first = a.part_ml[slot_of(min(lane, parts - 1))];
+    float m = first.x;
+    for (int j = lane + 64; j < parts; j += 64)
+        m = fmaxf(m, a.part_ml[slot_of(j)].x);
+    m = wave_max_all(m);
+    const float mu = m == -INFINITY ? 0.0f : m;
+    const float w0 = __builtin_amdgcn_exp2f(first.x - mu);  // of part `lane`
+    float sum = lane < parts ? w0 * first.y : 0.0f;
+    for (int j = lane + 64; j < parts; j += 64) {
+        const float2 v = a.part_ml[slot_of(j)];
+        sum = fmaf(__builtin_amdgcn_exp2f(v.x - mu), v.y, sum);
+    }
+    const float total = wave_sum_all(sum);
+    f32x4_t O = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        const int p = gi + j * NG;
+        const float wt = __shfl(w0, p & 63, 64);
+        if (p < parts)
+            O += (p < 64 ? wt : __builtin_amdgcn_exp2f(a.part_ml[slot_of(p)].x - mu)) * x[j];
+    }
+#pragma unroll 4
+    for (int p = gi + J * NG; p < parts; p += NG)
+        O += __builtin_amdgcn_exp2f(a.part_ml[slot_of(p)].x - mu) * load4(a.part_o + slot_of(p) * D + 4 * e);
+    red[gi][e] = O;
+    __syncthreads();
+    if (gi > 0)
+        return;
+#pragma unroll
+    for (int j = 1; j < NG; ++j)
+        O += red[j][e];
+    const int node = rr / a.G, head = g * a.G + rr - node * a.G;
+    store4(static_cast<TX *>(a.out) + (int64_t)(rows.first + node) * a.ld_out + (int64_t)head * D + 4 * e,
+           total == 0.0f ? f32x4_t{0.0f, 0.0f, 0.0f, 0.0f} : O / total);
+}
+
 // Tiles, and shares of the keys, from the sizes alone (what lies in device memory
 // is not known here).
-void plan(BatchAttnArgs *a, bool bf16) {
+static int env(const char *n, int d) { const char *v = getenv(n); return v ? atoi(v) : d; }
+constexpr int FEW_ROWS = 32;
+void plan(BatchAttnArgs *a, bool bf16, int D) {
     const int64_t most = (int64_t)a->max_rows * a->G;
-    a->tile = !bf16 ? 16 : most <= 64 ? 64 : 128;
-    a->block = KB;
+    const bool few = bf16 && a->paged && most <= FEW_ROWS;
+    a->tile = !bf16 ? 16 : few ? (most <= 16 ? 16 : 32) : most <= 64 ? 64 : 128;
+    a->block = few ? KB_FEW : KB;
     a->one_tile = most <= a->tile;
     a->slots = (int32_t)(a->one_tile ? a->n_seqs : (int64_t)a->n * a->G / a->tile + a->n_seqs);
-    const int blocks = (a->max_length + a->block - 1) / a->block;
     const int64_t units = (int64_t)a->slots * a->n_kv_heads;
-    const int want = a->lengths ? (int)std::max<int64_t>(1, std::min<int64_t>(blocks / 2, 512 / units)) : 1;
+    a->splits = 1;
+    a->chunks = 0;
+    const int blocks = (a->max_length + a->block - 1) / a->block;
+    a->per_split = blocks;
+    if (few) {
+        a->span = NW * KB_FEW;
+        const int64_t spans = (int64_t)a->n_seqs * ((a->max_length + a->span - 1) / a->span);
+        if (a->max_length <= env("BA_WHOLE", 512) || a->n_seqs > MAX_STREAM || spans > 1 << 30)
+            return;
+        const int groups = env("BA_GROUPS", a->tile == 32 && D == 128 ? 256 : 512);
+        a->chunks = (int32_t)std::min<int64_t>(spans, std::max(1, groups / a->n_kv_heads));
+        a->least = env("BA_LEAST", 1);
+        return;
+    }
+    if (!a->paged)
+        return;
+    const int want = (int)std::max<int64_t>(1, std::min<int64_t>((blocks + 7) / 8, 512 / units));
     a->per_split = (blocks + want - 1) / want;
     a->splits = (blocks + a->per_split - 1) / a->per_split;
 }
 
-size_t o_bytes(const BatchAttnArgs &a, int D) { return sizeof(float) * (size_t)a.splits * a.n * a.n_heads * D; }
-size_t workspace_of(const BatchAttnArgs &a, int D) {
-    return a.splits == 1 ? 0 : o_bytes(a, D) + sizeof(float2) * (size_t)a.splits * a.n * a.n_heads;
+// What the workspace holds: outputs and states of the parts, and the spans.
+struct Space {
+    size_t o, ml, spans;
+    size_t bytes() const { return o + ml + spans; }
+};
+Space space_of(const BatchAttnArgs &a, int D) {
+    const size_t rows = a.chunks       ? (size_t)2 * a.n_kv_heads * a.chunks * a.tile
+                        : a.splits > 1 ? (size_t)a.splits * a.n * a.n_heads
+                                       : 0;
+    return {rows * D * sizeof(float), rows * sizeof(float2), a.chunks ? sizeof(int32_t) * ((size_t)a.n_seqs + 2) : 0};
 }
 
 template <typename TX>
@@ -776,8 +1373,12 @@ void launch_f32(const BatchAttnArgs &a, int D, hipStream_t s) {
 
 template <typename TX, int D>
 void launch_mfma(const BatchAttnArgs &a, hipStream_t s) {
-    const dim3 grid((unsigned)(a.slots * a.n_kv_heads * a.splits));
-    if (a.tile == 64)
+    const dim3 grid((unsigned)(a.chunks ? a.chunks * a.n_kv_heads : a.slots * a.n_kv_heads * a.splits));
+    if (a.tile == 16)
+        hipLaunchKernelGGL((k_batch_attn_few<TX, D, 1>), grid, dim3(256), 0, s, a);
+    else if (a.tile == 32)
+        hipLaunchKernelGGL((k_batch_attn_few<TX, D, 2>), grid, dim3(256), 0, s, a);
+    else if (a.tile == 64)
         hipLaunchKernelGGL((k_batch_attn_mfma<TX, D, 2, 2>), grid, dim3(256), 0, s, a);
     else
         hipLaunchKernelGGL((k_batch_attn_mfma<TX, D, 4, 1>), grid, dim3(256), 0, s, a);
@@ -794,8 +1395,30 @@ void launch_bf16(const BatchAttnArgs &a, int D, hipStream_t s) {
         launch_mfma<TX, 128>(a, s);
 }
 
+template <typename TX, int D>
+void launch_join_stream(const BatchAttnArgs &a, hipStream_t s) {
+    const int rows = std::min(a.max_rows * a.G, a.tile);
+    const dim3 grid((unsigned)(a.n_seqs * a.n_kv_heads * rows));
+    // (parts of a sequence: one or two of many, or all of one)
+    if (a.chunks <= 4 * a.n_seqs)
+        hipLaunchKernelGGL((k_batch_join_stream<TX, D, 64>), grid, dim3(64), 0, s, a, rows);
+    else
+        hipLaunchKernelGGL((k_batch_join_stream<TX, D, 256>), grid, dim3(256), 0, s, a, rows);
+}
+
 template <typename TX>
 void launch_join(const BatchAttnArgs &a, int D, hipStream_t s) {
+    if (a.chunks) {
+        if (D == 16)
+            launch_join_stream<TX, 16>(a, s);
+        else if (D == 32)
+            launch_join_stream<TX, 32>(a, s);
+        else if (D == 64)
+            launch_join_stream<TX, 64>(a, s);
+        else
+            launch_join_stream<TX, 128>(a, s);
+        return;
+    }
     const dim3 grid((unsigned)(a.n * a.n_heads)), block(JOIN_THREADS);
     if (D == 16)
         hipLaunchKernelGGL((k_batch_join<TX, 16>), grid, block, 0, s, a);
@@ -843,7 +1466,7 @@ sd_status launch(const BatchAttnArgs &a, int32_t x_dtype, int32_t dtype, int D, 
         launch_f32<float>(a, D, s);
     }
     hipError_t e = hipGetLastError();
-    if (e == hipSuccess && a.splits > 1) {
+    if (e == hipSuccess && (a.splits > 1 || a.chunks)) {
         if (x_dtype == SD_BF16)
             launch_join<uint16_t>(a, D, s);
         else
@@ -860,6 +1483,7 @@ sd_status paged_sizes(const sd_kv_pages *kv, const sd_batch *batch, int32_t n_he
     if (st != SD_OK || (st = check_rows(n, n_heads, kv->n_kv_heads)) != SD_OK ||
         (st = check_batch(batch, kv, n, addresses)) != SD_OK)
         return st;
+    a->paged = 1;
     a->k = kv->k;
     a->v = kv->v;
     a->page_stride = kv->page_stride;
@@ -889,8 +1513,9 @@ sd_status paged_attention(const sd_kv_pages *kv, const sd_batch *batch, const vo
     if (st != SD_OK || (st = check_call(q, ld_q, x_dtype, n_heads, n, a.n_seqs, a.n_kv_heads, kv->head_dim, out, ld_out,
                                         &scale)) != SD_OK)
         return st;
-    plan(&a, kv->dtype == SD_BF16);
-    const size_t need = workspace_of(a, kv->head_dim);
+    plan(&a, kv->dtype == SD_BF16, kv->head_dim);
+    const Space space = space_of(a, kv->head_dim);
+    const size_t need = space.bytes();
     if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need))
         return report(SD_ERR_INVALID_ARG, "these sizes need " + std::to_string(need) +
                                               " bytes of 16-byte aligned workspace");
@@ -901,7 +1526,8 @@ sd_status paged_attention(const sd_kv_pages *kv, const sd_batch *batch, const vo
     a.scale = scale;
     if (need) {
         a.part_o = static_cast<float *>(workspace);
-        a.part_ml = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + o_bytes(a, kv->head_dim));
+        a.part_ml = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + space.o);
+        a.spans = reinterpret_cast<int32_t *>(static_cast<char *>(workspace) + space.o + space.ml);
     }
     return launch(a, x_dtype, kv->dtype, kv->head_dim, s);
 }
@@ -935,7 +1561,7 @@ sd_status prompt_attention(const sd_kv_layer *kv, const int32_t *starts, int32_t
     a.n_heads = n_heads;
     a.n_kv_heads = kv->n_kv_heads;
     a.G = n_heads / kv->n_kv_heads;
-    plan(&a, kv->dtype == SD_BF16);
+    plan(&a, kv->dtype == SD_BF16, kv->head_dim);
     return launch(a, x_dtype, kv->dtype, kv->head_dim, s);
 }
 
@@ -949,8 +1575,8 @@ size_t sd_paged_attention_workspace(const sd_kv_pages *kv, const sd_batch *batch
     if (paged_sizes(kv, batch, n_heads, n, false, &a) != SD_OK ||
         check_call(nullptr, 0, x_dtype, n_heads, n, a.n_seqs, a.n_kv_heads, kv->head_dim, nullptr, 0, nullptr) != SD_OK)
         return 0;
-    plan(&a, kv->dtype == SD_BF16);
-    return workspace_of(a, kv->head_dim);
+    plan(&a, kv->dtype == SD_BF16, kv->head_dim);
+    return space_of(a, kv->head_dim).bytes();
 }
 
 sd_status sd_paged_attention(const sd_kv_pages *kv, const sd_batch *batch, const void *q, int64_t ld_q, int32_t x_dtype,
