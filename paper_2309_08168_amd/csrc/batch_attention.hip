@@ -12,6 +12,7 @@
 #include <algorithm>
 #include <cmath>
 #include <string>
+#include <type_traits>
 
 #include "attn_mfma.h"
 #include "host_api.h"
@@ -45,6 +46,13 @@ struct BatchAttnArgs {
     int32_t splits, per_split, block;  // shares of the keys; blocks of a share; keys of a block
 };
 
+// An address that is the same in every lane, in scalar registers.
+__device__ __forceinline__ const uint16_t *uniform(const uint16_t *p) {
+    const uint64_t x = (uint64_t)p;
+    return (const uint16_t *)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(x >> 32)) << 32 |
+                              (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)x));
+}
+
 __device__ __forceinline__ int32_t start_of(const BatchAttnArgs &a, int32_t s) {
     return a.starts ? a.starts[s] : s * a.max_rows;
 }
@@ -65,17 +73,20 @@ struct Tile {
 };
 __device__ __forceinline__ Tile tile_of(const BatchAttnArgs &a, int32_t t) {
     Tile w;
-    if (a.one_tile) {
-        w.seq = t;
-        w.rows = rows_of(a, t);
-        w.row0 = 0;
-        return w;
+    int64_t before = 0;  // the slots of the sequences before
+    w.seq = t;
+    if (!a.one_tile) {
+        const auto slot = [&](int32_t j) { return (int64_t)start_of(a, j) * a.G / a.tile + j; };
+        w.seq = min(wave_count(a.n_seqs, t, slot), a.n_seqs - 1);
+        before = slot(w.seq);
     }
-    const auto slot = [&](int32_t j) { return (int64_t)start_of(a, j) * a.G / a.tile + j; };
-    w.seq = min(wave_count(a.n_seqs, t, slot), a.n_seqs - 1);
+    w.seq = __builtin_amdgcn_readfirstlane(w.seq);
     w.rows = rows_of(a, w.seq);
-    const int64_t row0 = ((int64_t)t - slot(w.seq)) * a.tile, most = (int64_t)w.rows.m * a.G;
-    w.row0 = (int32_t)(row0 < 0 || row0 > most ? most : row0);
+    w.rows.first = __builtin_amdgcn_readfirstlane(w.rows.first);
+    w.rows.m = __builtin_amdgcn_readfirstlane(w.rows.m);
+    w.rows.past = __builtin_amdgcn_readfirstlane(w.rows.past);
+    const int64_t row0 = a.one_tile ? 0 : (t - before) * a.tile, most = (int64_t)w.rows.m * a.G;
+    w.row0 = __builtin_amdgcn_readfirstlane((int32_t)(row0 < 0 || row0 > most ? most : row0));
     return w;
 }
 
@@ -436,10 +447,15 @@ __device__ __forceinline__ Groups groups_of(const BatchAttnArgs &a, const Tile &
     } else {
         k.off[0] = (int64_t)(w.rows.first + first) * a.row_stride;
     }
-#pragma unroll
-    for (int j = 1; j < 4; ++j)
-        k.off[j] = k.off[0] + 16 * j * a.row_stride;
+    k.off[1] = k.off[2] = k.off[3] = 0;
     return k;
+}
+// Where row r of a block starts, its rows all following the first (one) or by groups.
+__device__ __forceinline__ int64_t row_at(const Groups &k, bool one, int r, int64_t row_stride) {
+    // (the four as values: chosen by address, they would lie in memory)
+    const int64_t o0 = k.off[0], o1 = k.off[1], o2 = k.off[2], o3 = k.off[3];
+    const int j = one ? 0 : r >> 4;
+    return (j == 0 ? o0 : j == 1 ? o1 : j == 2 ? o2 : o3) + (one ? r : r & 15) * row_stride;
 }
 // The keys of a block that are seen by one who sees `count` of them, as bits.
 __device__ __forceinline__ uint64_t seen_bits(int count, uint32_t ok) {
@@ -496,19 +512,17 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_batch_attn_mfma(BatchAttnAr
             for (int i = 0; i < NU; ++i) {
                 const int u = wave + WAVES * i;
                 if (L::C % WAVES == 0 || u < L::C) {  // uniform over the wave
-                    const int j = one ? 0 : ROWS * u / 16;
-                    const int64_t at = j == 0 ? k.off[0] : j == 1 ? k.off[1] : j == 2 ? k.off[2] : k.off[3];
-                    load_to_lds16(K + at, off[i], &kv[buf][0][u * 512]);
-                    load_to_lds16(V + at, off[i], &kv[buf][1][u * 512]);
+                    const int64_t at = row_at(k, one, one ? 0 : ROWS * u / 16 * 16, a.row_stride);
+                    load_to_lds16(uniform(K + at), off[i], &kv[buf][0][u * 512]);
+                    load_to_lds16(uniform(V + at), off[i], &kv[buf][1][u * 512]);
                 }
             }
         } else {
 #pragma unroll 1
             for (int u = wave; u < L::C; u += WAVES) {
                 const int s = 4 * u + (lane >> 4), p = (lane & 15) ^ L::swz(s);
-                const int r = min(s * L::RPL + p / L::C, klen - 1 - first), j = r >> 4;  // rows past the last: that one
-                const int64_t at = (j == 0 ? k.off[0] : j == 1 ? k.off[1] : j == 2 ? k.off[2] : k.off[3]) +
-                                   (r & 15) * a.row_stride + 8 * (p % L::C);
+                // rows past the last: that one
+                const int64_t at = row_at(k, one, min(s * L::RPL + p / L::C, klen - 1 - first), a.row_stride) + 8 * (p % L::C);
                 load_to_lds16(K + at, &kv[buf][0][u * 512]);
                 load_to_lds16(V + at, &kv[buf][1][u * 512]);
             }
@@ -599,81 +613,6 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_batch_attn_mfma(BatchAttnAr
             }
             odd = __syncthreads_or(odd);
         }
-        if constexpr (!EXACT && NK == 1) {
-            // A whole block's 64 keys at once: the reads of K run ahead of their
-            // products, those of V under the softmax.
-            if (full) {
-                if (!live)
-                    continue;
-                int xk = 2 * (buf * 2 * KB * D + L::at(col, half)), xv = 2 * buf * 2 * KB * D + v_lane;
-                asm volatile("" : "+v"(xk), "+v"(xv));
-                f32x16_t s[2];
-                u32x4_t kf[ES][2];
-#pragma unroll
-                for (int e = 0; e < ES; ++e)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-                        kf[e][h] = *reinterpret_cast<const u32x4_t *>(lds + (xk ^ (32 * e)) + 2 * 32 * h * D);
-                __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-                for (int e = 0; e < ES; ++e)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-                        s[h] = mfma32(kf[e][h], qf[e][0], e == 0 ? f32x16_t{} : s[h]);
-                __builtin_amdgcn_s_setprio(0);
-                // V^T: keys 16 j + 8 I + 4 half + 0 .. 3 of tile et
-                u32x4_t vf[4][ET];
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                    for (int et = 0; et < ET; ++et)
-#pragma unroll
-                        for (int I = 0; I < 2; ++I) {
-                            const char *src = lds + (xv ^ (64 * et) ^ (I ? (D == 16 ? 16 : 32) : 0)) + 2 * (16 * j + 8 * I) * D;
-                            const u32x2_t y =
-                                __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)src));
-                            vf[j][et][2 * I] = y[0];
-                            vf[j][et][2 * I + 1] = y[1];
-                        }
-                float mx = s[0][0];
-#pragma unroll
-                for (int v = 1; v < 32; ++v)
-                    mx = fmaxf(mx, s[v >> 4][v & 15]);
-                {
-                    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-                    mx = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])) * factor;
-                }
-                const bool grows = mx > m_run + SLACK;
-                if (__any(grows)) {
-                    const float m_new = grows ? mx : m_run;
-                    const float sc = m_run == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run - m_new);
-                    l_run *= sc;
-#pragma unroll
-                    for (int et = 0; et < ET; ++et)
-                        o[et] *= sc;
-                    m_run = m_new;
-                }
-                const float m_use = m_run == -INFINITY ? 0.0f : m_run;
-                float sum[4] = {};
-                u32x4_t pf[4];
-#pragma unroll
-                for (int v = 0; v < 32; v += 2) {
-                    const float p0 = __builtin_amdgcn_exp2f(fmaf(s[v >> 4][v & 15], factor, -m_use));
-                    const float p1 = __builtin_amdgcn_exp2f(fmaf(s[v >> 4][(v & 15) + 1], factor, -m_use));
-                    sum[v >> 3] += p0 + p1;
-                    pf[v >> 3][(v >> 1) & 3] = cvt_pk(p0, p1);
-                }
-                l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-                __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                    for (int et = 0; et < ET; ++et)
-                        o[et] = mfma32(vf[j][et], pf[j], o[et]);
-                __builtin_amdgcn_s_setprio(0);
-                continue;
-            }
-        }
         const uint64_t visible = full ? ~0ull : seen_bits(see - first, now.ok);
 #pragma unroll 1
         for (int h = wk; h < 2; h += NK) {
@@ -746,9 +685,7 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_batch_attn_mfma(BatchAttnAr
                     for (int v = 0; v < 16; ++v)
                         pk = v == own ? p[v] : pk;
                     pk = __shfl(pk, col + 32 * ((key >> 2) & 1), 64);
-                    const int r = min(32 * h + key, klen - 1 - first), j = r >> 4;
-                    const uint16_t *vr = V + (j == 0 ? now.off[0] : j == 1 ? now.off[1] : j == 2 ? now.off[2] : now.off[3]) +
-                                         (r & 15) * a.row_stride;
+                    const uint16_t *vr = V + row_at(now, one, min(32 * h + key, klen - 1 - first), a.row_stride);
 #pragma unroll
                     for (int et = 0; et < ET; ++et)
 #pragma unroll
@@ -851,6 +788,545 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_batch_attn_mfma(BatchAttnAr
         }
     if (a.splits > 1 && half == 0)
         a.part_ml[slot] = make_float2(m_run, l_run);
+}
+
+// ---------------------------------------------------------------------------
+// bfloat16 queries, tiles of 128 rows: four waves of 32, and steps of 32 keys.  Of
+// heads of 128, a step of a wave is 16 products of 32 cycles (8 of K, 8 of V) and a
+// softmax of about 90 vector operations, 16 of them exponentials of 8 cycles, which the
+// matrix cores do not wait for: step t turns the scores of block t into weights while it
+// takes the scores of block t + 1 and the values of block t - 1, a product of each and
+// a part of the softmax at a time.  K comes four blocks ahead and V two, in rings
+// of four.  The running maximum of block t rescales the sums when block t - 1 is in
+// them.  Blocks that some row does not see whole take their parts one after another.
+struct Halves {  // where the 16-key halves of a block start (elements), and which have a page
+    int64_t off[2];
+    int ok;
+};
+
+template <int D, bool PAGED>
+__global__ __launch_bounds__(256, 2) void k_batch_attn_wide(BatchAttnArgs a) {
+    constexpr int ES = D / 16, ET = D < 32 ? 1 : D / 32, BE = KB_FEW * D;  // BE: elements of a block
+    // A block lies in LDS as lines of 256 bytes; one of 128 elements a row as two blocks
+    // of 64, so that all but a few of a lane's addresses differ by a constant.
+    constexpr int LD = D < 64 ? D : 64;
+    using L = Lines<LD>;
+    __shared__ __attribute__((aligned(1024))) uint16_t kv[2][4][BE];  // [K, V][block % 4]
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 31,
+              half = lane >> 5;
+    const int g = blockIdx.x % a.n_kv_heads, rest = blockIdx.x / a.n_kv_heads;
+    const int split = rest / a.slots;
+    // (from the last tile, which has the most keys, to the first)
+    const Tile w = tile_of(a, a.slots - 1 - rest % a.slots);
+    const int rows = w.rows.m * a.G;
+    if (w.row0 >= rows)
+        return;  // uniform
+    auto sees = [&](int rr) { return seen_from(w.rows.past + rr / a.G, a.max_length); };
+    const int klen = __builtin_amdgcn_readfirstlane(sees(min(w.row0 + 32 * NW, rows) - 1));
+    const int kall = __builtin_amdgcn_readfirstlane(sees(w.row0));
+    const int t0 = split * a.per_split, t1 = min(t0 + a.per_split, (klen + KB_FEW - 1) / KB_FEW);
+    if (a.splits > 1 && t0 >= t1)
+        return;
+    const int r0 = w.row0 + wave * 32;
+    const bool live = r0 < rows;  // uniform over the wave: a wave without rows loads and waits with the others
+    const int row = min(r0 + col, rows - 1), node = row / a.G, head = g * a.G + row - node * a.G;
+    const int see = seen_from(w.rows.past + node, a.max_length);
+    const uint16_t *K = static_cast<const uint16_t *>(a.k) + (int64_t)g * a.head_stride;
+    const uint16_t *V = static_cast<const uint16_t *>(a.v) + (int64_t)g * a.head_stride;
+
+    // A wave takes every fourth KB of a block of K or of V.  Whole blocks: lane
+    // offsets that do not change, from the block's first row where its rows follow one
+    // another (packed, or pages of a block and more), else from a half's.
+    constexpr int LOADS = D / 16, NU = (LOADS + NW - 1) / NW, ROWS = 4 * L::RPL;  // of a block; of a wave; rows of one
+    constexpr int PER = LD / 16;                                                  // loads of LD columns
+    const bool one = !PAGED || a.page_shift >= 5, near = (one || D > 16) && near_rows(a.row_stride);
+    uint32_t off[NU];
+#pragma unroll
+    for (int i = 0; i < NU; ++i) {
+        const int u = wave + NW * i, s = 4 * (u % PER) + (lane >> 4), p = (lane & 15) ^ L::swz(s);
+        off[i] = (uint32_t)(2 * ((int64_t)((s * L::RPL + p / L::C) & (one ? 31 : 15)) * a.row_stride + 8 * (p % L::C) +
+                                 u / PER * LD));
+    }
+    const int32_t *table = PAGED ? a.table + (int64_t)w.seq * a.ld_table : nullptr;
+    // The entries of block t, asked for a step before they are needed.
+    struct Pages {
+        int32_t p[2];
+    };
+    auto pages_of = [&](int t) {
+        Pages e{{-1, -1}};
+        if constexpr (PAGED) {
+            const int first = KB_FEW * t;
+            if (first < klen)
+                e.p[0] = table[first >> a.page_shift];
+            if (!one && first + 16 < klen)
+                e.p[1] = table[(first + 16) >> a.page_shift];
+        }
+        return e;
+    };
+    auto whole_pages_of = [&](int t) {  // of a block within the keys
+        const int first = KB_FEW * t;
+        return Pages{{table[first >> a.page_shift], table[(first + 16) >> a.page_shift]}};
+    };
+    auto halves_of = [&](const Pages &e, int t) {
+        Halves h;
+        const int first = KB_FEW * t;
+        h.ok = 3;  // (keys past the last are masked by their number)
+        h.off[1] = 0;
+        if constexpr (!PAGED) {
+            h.off[0] = (int64_t)(w.rows.first + first) * a.row_stride;
+        } else {
+            // (without a page: any rows, which are masked, and taken for finite)
+            const int p = __builtin_amdgcn_readfirstlane(e.p[0]);
+            const bool there = (uint32_t)p < (uint32_t)a.n_pages;
+            h.off[0] = (there ? p * a.page_stride : 0) + (int64_t)(first & ((1 << a.page_shift) - 1)) * a.row_stride;
+            h.ok = there ? 3 : one ? 0 : 2;
+            if (!one) {
+                const int q = __builtin_amdgcn_readfirstlane(e.p[1]);
+                const bool too = (uint32_t)q < (uint32_t)a.n_pages;
+                h.off[1] = (too ? q * a.page_stride : 0) + (int64_t)((first + 16) & ((1 << a.page_shift) - 1)) * a.row_stride;
+                if (!too && first + 16 < klen)
+                    h.ok &= 1;
+            }
+        }
+        return h;
+    };
+    auto row_at = [&](const Halves &h, int r) {
+        // (the two as values: chosen by address, they would lie in memory)
+        const int64_t o0 = h.off[0], o1 = h.off[1];
+        const bool low = one || r < 16;
+        return (low ? o0 : o1) + (low ? r : r - 16) * a.row_stride;
+    };
+    auto load_block = [&](const uint16_t *m, const Halves &h, int t, uint16_t *to) {
+        if (KB_FEW * t + KB_FEW <= klen && near) {
+#pragma unroll
+            for (int i = 0; i < NU; ++i) {
+                const int u = wave + NW * i;
+                if (LOADS % NW == 0 || u < LOADS)  // uniform over the wave
+                    load_to_lds16(uniform(m + row_at(h, one || ROWS * (u % PER) < 16 ? 0 : 16)), off[i], to + u * 512);
+            }
+        } else {
+            int own = lane;
+            asm volatile("" : "+v"(own));  // (nothing of this is kept in registers over the loop)
+#pragma unroll 1
+            for (int u = wave; u < LOADS; u += NW) {
+                const int s = 4 * (u % PER) + (own >> 4), p = (own & 15) ^ L::swz(s);
+                // rows past the last: that one
+                const int r = min(s * L::RPL + p / L::C, klen - 1 - KB_FEW * t);
+                load_to_lds16(m + row_at(h, r) + 8 * (p % L::C) + u / PER * LD, to + u * 512);
+            }
+        }
+    };
+    // The queries are asked for before the first block: loads return in order.
+    const uint16_t *qs =
+        static_cast<const uint16_t *>(a.q) + (int64_t)(w.rows.first + node) * a.ld_q + (int64_t)head * D + 8 * half;
+    u32x4_t qf[ES];
+#pragma unroll
+    for (int s = 0; s < ES; ++s)
+        qf[s] = *reinterpret_cast<const u32x4_t *>(qs + 16 * s);
+    __builtin_amdgcn_sched_barrier(0);
+    // Block t + 4 of K and t + 2 of V are asked for in step t (past the last block it
+    // again, so that a wave has as many loads under way in every step).
+    auto slot = [&](int t) { return (t - t0) & 3; };
+    auto load_k = [&](const Pages &e, int t) {
+        const int b = min(t, t1 - 1);
+        load_block(K, halves_of(e, b), b, kv[0][slot(t)]);
+    };
+    // (and which halves of the blocks t, t + 1 and t + 2 of V have a page)
+    int ok_now = 3, ok_next = 3, ok_after = 3;
+    auto load_v = [&](const Pages &e, int t) {
+        const int b = min(t, t1 - 1);
+        const Halves h = halves_of(e, b);
+        load_block(V, h, b, kv[1][slot(t)]);
+        return h.ok;
+    };
+    Pages next_k{}, next_v{};
+    if (t0 < t1) {
+        load_k(pages_of(t0), t0);
+        load_k(pages_of(min(t0 + 1, t1 - 1)), t0 + 1);
+        load_k(pages_of(min(t0 + 2, t1 - 1)), t0 + 2);
+        ok_next = load_v(pages_of(t0), t0);
+        load_k(pages_of(min(t0 + 3, t1 - 1)), t0 + 3);
+        ok_after = load_v(pages_of(min(t0 + 1, t1 - 1)), t0 + 1);
+        next_k = pages_of(min(t0 + 4, t1 - 1));
+        next_v = pages_of(min(t0 + 2, t1 - 1));
+    }
+    // Rows past the last are zeros, which draw less power than copies of it.  (A
+    // negative scale as one of q, so that the largest score stays the largest.)
+    const bool mine = r0 + col < rows;
+#pragma unroll
+    for (int s = 0; s < ES; ++s)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            qf[s][j] = mine ? qf[s][j] ^ (a.scale < 0.0f ? 0x80008000u : 0u) : 0u;
+    // (a scale that float32 products would take for zero would make NaN of a masked score)
+    const float factor = fmaxf(fabsf(a.scale), 1.17549435e-38f);
+    // Where a lane reads K (row col, chunk 2 e + half) and V^T (as in k_batch_attn_mfma) in
+    // slot 0: what changes them by an exclusive or, a register each.
+    constexpr int KA = ES < 4 ? ES : 4;
+    int ka[KA], va[2][2];
+    const int k_lane = 2 * L::at(col, half);
+    const int v_lane = 2 * (4 * BE + L::at(4 * half + ((lane >> 2) & 3), (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) % L::C) +
+                            4 * (lane & 1));
+#pragma unroll
+    for (int e = 0; e < KA; ++e)
+        ka[e] = k_lane ^ (32 * e);
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int I = 0; I < 2; ++I)
+            va[x][I] = v_lane ^ (64 * x) ^ (I ? (D == 16 ? 16 : 32) : 0);
+    const char *lds = reinterpret_cast<const char *>(kv);
+    float m_run = -INFINITY, l_run = 0.0f;
+    f32x16_t o[ET], s0, s1;
+    u32x4_t p0[2], p1[2];  // weights of keys 16 j .. of a block, in the slots of its value products
+#pragma unroll
+    for (int et = 0; et < ET; ++et)
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+            o[et][v] = 0.0f;
+
+    // of the block whose slot starts `at` bytes from where the addresses point
+    auto read_k = [&](int at, int e) {
+        return *reinterpret_cast<const u32x4_t *>(lds + ka[e % KA] + at + e / 4 * (2 * KB_FEW * LD));
+    };
+    auto read_v = [&](int at, int i) {
+        const int j = i / ET, et = i % ET;
+        u32x4_t vf;
+#pragma unroll
+        for (int I = 0; I < 2; ++I) {
+            const char *src = lds + va[et & 1][I] + at + et / 2 * (2 * KB_FEW * LD) + 2 * (16 * j + 8 * I) * LD;
+            const u32x2_t y = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)src));
+            vf[2 * I] = y[0];
+            vf[2 * I + 1] = y[1];
+        }
+        return vf;
+    };
+    constexpr int SLOT = 2 * BE;  // bytes
+    // Moves the lane addresses on by two slots, of four.
+    auto turn_k = [&]() {
+#pragma unroll
+        for (int e = 0; e < KA; ++e)
+            asm volatile("v_xor_b32 %0, %1, %0" : "+v"(ka[e]) : "n"(2 * SLOT));
+    };
+    auto turn_v = [&]() {
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+            asm volatile("v_xor_b32 %0, %1, %0" : "+v"(va[x >> 1][x & 1]) : "n"(2 * SLOT));
+    };
+    // The softmax of a block's scores in parts: the row's maximum of them, the new
+    // running one, and weights v0 .. v1 - 1.
+    struct Soft {
+        float mx, m_use, sc, sum[2], x[16];
+        bool grows;
+    };
+    auto soft_max = [&](const f32x16_t &s, Soft &f) {
+        // (a tree: a chain of them would wait for each)
+        const float m0 = fmaxf(fmaxf(s[0], s[1]), s[2]), m1 = fmaxf(fmaxf(s[3], s[4]), s[5]),
+                    m2 = fmaxf(fmaxf(s[6], s[7]), s[8]), m3 = fmaxf(fmaxf(s[9], s[10]), s[11]),
+                    m4 = fmaxf(fmaxf(s[12], s[13]), s[14]);
+        f.mx = fmaxf(fmaxf(fmaxf(fmaxf(m0, m1), m2), fmaxf(m3, m4)), s[15]);
+    };
+    auto soft_grow = [&](Soft &f) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(f.mx), __float_as_uint(f.mx), false, false);
+        const float mx = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])) * factor;
+        f.grows = mx > m_run + SLACK;
+        const float m_new = f.grows ? mx : m_run;
+        f.m_use = m_new == -INFINITY ? 0.0f : m_new;
+        // (a row that has seen no key yet keeps zeros; one whose maximum stays, its sums)
+        f.sc = __builtin_amdgcn_exp2f(m_run - f.m_use);
+        m_run = m_new;
+    };
+    // Weights 4 g .. 4 g + 3: their exponents, powers, and sums and words.
+    auto soft_exponents = [&](const f32x16_t &s, Soft &f, int g) {
+#pragma unroll
+        for (int v = 4 * g; v < 4 * g + 4; ++v)
+            f.x[v] = fmaf(s[v], factor, -f.m_use);
+    };
+    auto soft_powers = [&](Soft &f, int g) {
+#pragma unroll
+        for (int v = 4 * g; v < 4 * g + 4; ++v) {
+            f.x[v] = __builtin_amdgcn_exp2f(f.x[v]);
+            asm volatile("" : "+v"(f.x[v]));  // (here, and not where it is used)
+        }
+    };
+    auto soft_words = [&](Soft &f, u32x4_t (&p)[2], int g) {
+#pragma unroll
+        for (int v = 4 * g; v < 4 * g + 4; v += 2) {
+            f.sum[0] = v ? f.sum[0] + f.x[v] : f.x[v];
+            f.sum[1] = v ? f.sum[1] + f.x[v + 1] : f.x[v + 1];
+            uint32_t word = cvt_pk(f.x[v], f.x[v + 1]);
+            asm volatile("" : "+v"(word), "+v"(f.sum[0]), "+v"(f.sum[1]));
+            p[v >> 3][(v >> 1) & 3] = word;
+        }
+    };
+    auto soft_end = [&](const Soft &f) {
+        l_run = fmaf(l_run, f.grows ? f.sc : 1.0f, f.sum[0] + f.sum[1]);
+        if (__any(f.grows)) {
+            const float by = f.grows ? f.sc : 1.0f;
+#pragma unroll
+            for (int et = 0; et < ET; ++et)
+                o[et] *= by;
+        }
+    };
+    // The loads of a step, when those it reads have landed, this wave's, then
+    // everyone's, and every read of what they fill has returned.
+    constexpr bool EVEN = NU * NW == LOADS;  // every wave has 4 NU loads that may be under way
+    auto begin = [&](int t) {
+        if constexpr (EVEN)
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(4 * NU) : "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        load_k(next_k, t + 4);
+        ok_now = ok_next;
+        ok_next = ok_after;
+        ok_after = load_v(next_v, t + 2);
+        next_k = pages_of(min(t + 5, t1 - 1));
+        next_v = pages_of(min(t + 3, t1 - 1));
+    };
+    // Whether every row sees every key of a block (with its halves' pages).
+    auto is_full = [&](int t, int ok) { return KB_FEW * t + KB_FEW <= kall && ok == 3; };
+    auto scores = [&](int at, f32x16_t &to) {
+#pragma unroll
+        for (int e = 0; e < ES; ++e)
+            to = mfma32(read_k(at, e), qf[e], e == 0 ? f32x16_t{} : to);
+    };
+    auto values = [&](int at, const u32x4_t (&p)[2]) {
+#pragma unroll
+        for (int i = 0; i < 2 * ET; ++i)
+            o[i % ET] = mfma32(read_v(at, i), p[i / ET], o[i % ET]);
+    };
+    // A step of whole blocks: weights of s into p_next, scores of the next block into
+    // s_next, values of the one before with its weights p.
+    // loads(i): what else part i does.
+    constexpr int PARTS = 8;
+    auto fast = [&](int at, const f32x16_t &s, f32x16_t &s_next, const u32x4_t (&p)[2], u32x4_t (&p_next)[2], auto loads) {
+        constexpr int AHEAD = 2;
+        u32x4_t kf[ES], vf[2 * ET];
+        Soft f;
+        // (the part in which product i of n is)
+        auto part_of = [](int i, int n) { return i * PARTS / n; };
+#pragma unroll
+        for (int i = -AHEAD; i < PARTS; ++i) {
+#pragma unroll
+            for (int e = 0; e < ES; ++e)
+                if (part_of(e, ES) == i + AHEAD)
+                    kf[e] = read_k(at, e);
+#pragma unroll
+            for (int v = 0; v < 2 * ET; ++v)
+                if (part_of(v, 2 * ET) == i + AHEAD)
+                    vf[v] = read_v(at, v);
+            if (i < 0)
+                continue;
+#pragma unroll
+            for (int e = 0; e < ES; ++e)
+                if (part_of(e, ES) == i)
+                    s_next = mfma32(kf[e], qf[e], e == 0 ? f32x16_t{} : s_next);
+#pragma unroll
+            for (int v = 0; v < 2 * ET; ++v)
+                if (part_of(v, 2 * ET) == i)
+                    o[v % ET] = mfma32(vf[v], p[v / ET], o[v % ET]);
+            loads(i);
+            if (i == 0)
+                soft_max(s, f);
+            if (i == 1)
+                soft_grow(f);
+            // (each part's vector operations need none of the same part's)
+            if (i >= 4)
+                soft_words(f, p_next, i - 4);
+            if (i >= 3 && i < 7)
+                soft_powers(f, i - 3);
+            if (i >= 2 && i < 6)
+                soft_exponents(s, f, i - 2);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        soft_end(f);
+    };
+    // The values of a block that some row does not see whole: a row must not add 0 times
+    // an infinity or NaN of a value that it does not see.  They are taken out in
+    // LDS, and put where they belong from memory.
+    auto values_apart = [&](int t, int at, const u32x4_t (&p)[2]) {
+        uint16_t *vs = kv[1][slot(t)];
+        bool odd = false;
+        int own = threadIdx.x;
+        asm volatile("" : "+v"(own));
+#pragma unroll 1
+        for (int c = own; c < BE / 8; c += 64 * NW) {
+            u32x4_t x = reinterpret_cast<const u32x4_t *>(vs)[c];
+            bool hit = false;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t y = without_odd(x[j]);
+                hit |= y != x[j];
+                x[j] = y;
+            }
+            if (hit)
+                reinterpret_cast<u32x4_t *>(vs)[c] = x;
+            odd |= hit;
+        }
+        odd = __syncthreads_or(odd);
+        if (!live)
+            return;
+        if (odd) {
+            const Halves h = halves_of(pages_of(t), t);
+            const int col = own & 31, half = (own >> 5) & 1;
+            // lane (col, half) holds elements 32 et + 8 (v / 4) + 4 half + v % 4 of row col
+#pragma unroll 1
+            for (int key = 0; key < KB_FEW; ++key) {
+                // the weight of key 16 j + 8 I + 4 half + u: in word 2 I + u / 2 of j
+                uint32_t word = 0;
+                const int which = 4 * (key >> 4) + 2 * ((key >> 3) & 1) + ((key & 3) >> 1);
+#pragma unroll
+                for (int v = 0; v < 8; ++v)
+                    word = v == which ? p[v >> 2][v & 3] : word;
+                word = __shfl(word, col + 32 * ((key >> 2) & 1), 64);
+                const float pk = __uint_as_float(key & 1 ? word & 0xffff0000u : word << 16);
+                const uint16_t *vr = V + row_at(h, min(key, klen - 1 - KB_FEW * t));
+#pragma unroll
+                for (int et = 0; et < ET; ++et)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const int e = 32 * et + 8 * (v >> 2) + 4 * half + (v & 3);
+                        const float x = e < D ? load1(vr + e) : 0.0f;
+                        if (pk != 0.0f && !finite(x))
+                            o[et][v] = fmaf(pk, x, o[et][v]);
+                        __builtin_amdgcn_sched_barrier(0);  // a load at a time: registers
+                    }
+            }
+        }
+        values(at, p);
+    };
+
+    // One part after another: weights of s1 into p0, the next block's scores into s1.
+    auto weigh = [&](int t, int at) {
+        if (t + 1 < t1)
+            scores(at, s0);
+        Soft f;
+        soft_max(s1, f);
+        soft_grow(f);
+#pragma unroll
+        for (int g4 = 0; g4 < 4; ++g4)
+            soft_exponents(s1, f, g4);
+#pragma unroll
+        for (int g4 = 0; g4 < 4; ++g4)
+            soft_powers(f, g4);
+#pragma unroll
+        for (int g4 = 0; g4 < 4; ++g4)
+            soft_words(f, p0, g4);
+        soft_end(f);
+        s1 = s0;
+    };
+    int t = t0;
+    bool full = false;  // the block before
+    if (t0 < t1) {
+        // K of the first two blocks has landed
+        if constexpr (EVEN)
+            asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(4 * NU) : "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+        scores(0, s1);
+        if (is_full(t0, ok_next)) {
+            begin(t0);
+            weigh(t0, SLOT);
+            full = true;
+            ++t;
+        }
+    }
+    // (two steps at a time, so that what they hand on stays in its registers: the first
+    // reads K from slots 2 and 3 and V from 0 and 1, the next the other way around)
+    bool second = false;
+    if (full) {
+        turn_k();
+        // Where what is asked for lies within whole blocks, too, a step's loads stand
+        // between its products.
+        const int quick = EVEN && near ? min(min(t1, klen / KB_FEW) - 5, kall / KB_FEW - 1) : t0;
+        const auto quick_step = [&](int t, int at, const f32x16_t &s, f32x16_t &s_next, const u32x4_t (&p)[2],
+                                    u32x4_t (&p_next)[2]) {
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(4 * NU) : "memory");
+            const Halves hk = halves_of(next_k, t + 4), hv = halves_of(next_v, t + 2);
+            ok_next = ok_after;
+            ok_after = hv.ok;
+            uint16_t *to_k = kv[0][slot(t + 4)], *to_v = kv[1][slot(t + 2)];
+            const auto loads = [&](int i) {
+                constexpr int EACH = PARTS / 2 / NU;  // parts of a load
+                const int j = i / EACH % NU, u = wave + NW * j, r = one || ROWS * (u % PER) < 16 ? 0 : 16;
+                if (i % EACH == 0 && i < PARTS / 2)
+                    load_to_lds16(uniform(K + row_at(hk, r)), off[j], to_k + u * 512);
+                else if (i % EACH == 0)
+                    load_to_lds16(uniform(V + row_at(hv, r)), off[j], to_v + u * 512);
+                if (PAGED && i == PARTS - 1) {
+                    next_k = whole_pages_of(t + 5);
+                    next_v = whole_pages_of(t + 3);
+                }
+            };
+            fast(at, s, s_next, p, p_next, loads);  // (a wave without rows, too, with queries of zero)
+        };
+        while (t < quick && ok_next == 3 && ok_after == 3) {
+            quick_step(t, 0, s1, s0, p0, p1);
+            quick_step(t + 1, SLOT, s0, s1, p1, p0);
+            t += 2;
+            turn_k();
+            turn_v();
+            second = !second;
+        }
+        if (second)
+            turn_v();
+        else
+            turn_k();
+    }
+#pragma unroll 1
+    for (; t < t1; ++t) {
+        begin(t);
+        const bool was = full;
+        full = is_full(t, ok_now);
+        if (live && !full) {
+            const int count = see - KB_FEW * t;
+            const uint32_t seen = (count >= 32 ? ~0u : count <= 0 ? 0u : (1u << count) - 1) &
+                                  ((ok_now & 1 ? 0xffffu : 0u) | (ok_now & 2 ? 0xffff0000u : 0u));
+            const uint32_t own = seen >> (4 * half);
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+                s1[v] = (own >> (8 * (v >> 2) + (v & 3))) & 1 ? s1[v] : -INFINITY;
+        }
+        if (t > t0) {
+            if (!was)
+                values_apart(t - 1, SLOT * slot(t - 1), p0);
+            else if (live)
+                values(SLOT * slot(t - 1), p0);
+        }
+        if (live)
+            weigh(t, SLOT * slot(t + 1));
+    }
+    if (t0 < t1) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (!full)
+            values_apart(t1 - 1, SLOT * slot(t1 - 1), p0);
+        else if (live)
+            values(SLOT * slot(t1 - 1), p0);
+    }
+    {
+        const auto lr = __builtin_amdgcn_permlane32_swap(__float_as_uint(l_run), __float_as_uint(l_run), false, false);
+        l_run = __uint_as_float(lr[0]) + __uint_as_float(lr[1]);
+    }
+    if (!mine)
+        return;
+    const int64_t at = (int64_t)(w.rows.first + node), place = ((int64_t)split * a.n + at) * a.n_heads + head;
+    uint16_t *out = static_cast<uint16_t *>(a.out) + at * a.ld_out + (int64_t)head * D;
+    const float inv = a.splits > 1 ? 1.0f : l_run == 0.0f ? 0.0f : 1.0f / l_run;
+#pragma unroll
+    for (int et = 0; et < ET; ++et)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int e = 32 * et + 8 * q + 4 * half;
+            const f32x4_t y = f32x4_t{o[et][4 * q], o[et][4 * q + 1], o[et][4 * q + 2], o[et][4 * q + 3]} * inv;
+            if (e < D) {
+                if (a.splits == 1)
+                    store4(out + e, y);
+                else
+                    store4(a.part_o + place * D + e, y);
+            }
+        }
+    if (a.splits > 1 && half == 0)
+        a.part_ml[place] = make_float2(m_run, l_run);
 }
 
 // ---------------------------------------------------------------------------
@@ -1317,11 +1793,11 @@ __global__ __launch_bounds__(THREADS) void k_batch_join_stream(BatchAttnArgs a, 
 // is not known here).
 static int env(const char *n, int d) { const char *v = getenv(n); return v ? atoi(v) : d; }
 constexpr int FEW_ROWS = 32;
-void plan(BatchAttnArgs *a, bool bf16, int D) {
+void plan(BatchAttnArgs *a, bool x_bf16, bool bf16, int D) {
     const int64_t most = (int64_t)a->max_rows * a->G;
     const bool few = bf16 && a->paged && most <= FEW_ROWS;
     a->tile = !bf16 ? 16 : few ? (most <= 16 ? 16 : 32) : most <= 64 ? 64 : 128;
-    a->block = few ? KB_FEW : KB;
+    a->block = few || (x_bf16 && bf16 && a->tile == 128) ? KB_FEW : KB;
     a->one_tile = most <= a->tile;
     a->slots = (int32_t)(a->one_tile ? a->n_seqs : (int64_t)a->n * a->G / a->tile + a->n_seqs);
     const int64_t units = (int64_t)a->slots * a->n_kv_heads;
@@ -1380,7 +1856,12 @@ void launch_mfma(const BatchAttnArgs &a, hipStream_t s) {
         hipLaunchKernelGGL((k_batch_attn_few<TX, D, 2>), grid, dim3(256), 0, s, a);
     else if (a.tile == 64)
         hipLaunchKernelGGL((k_batch_attn_mfma<TX, D, 2, 2>), grid, dim3(256), 0, s, a);
-    else
+    else if constexpr (sizeof(TX) == 2) {
+        if (a.paged)
+            hipLaunchKernelGGL((k_batch_attn_wide<D, true>), grid, dim3(256), 0, s, a);
+        else
+            hipLaunchKernelGGL((k_batch_attn_wide<D, false>), grid, dim3(256), 0, s, a);
+    } else
         hipLaunchKernelGGL((k_batch_attn_mfma<TX, D, 4, 1>), grid, dim3(256), 0, s, a);
 }
 template <typename TX>
@@ -1513,7 +1994,7 @@ sd_status paged_attention(const sd_kv_pages *kv, const sd_batch *batch, const vo
     if (st != SD_OK || (st = check_call(q, ld_q, x_dtype, n_heads, n, a.n_seqs, a.n_kv_heads, kv->head_dim, out, ld_out,
                                         &scale)) != SD_OK)
         return st;
-    plan(&a, kv->dtype == SD_BF16, kv->head_dim);
+    plan(&a, x_dtype == SD_BF16, kv->dtype == SD_BF16, kv->head_dim);
     const Space space = space_of(a, kv->head_dim);
     const size_t need = space.bytes();
     if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need))
@@ -1561,7 +2042,7 @@ sd_status prompt_attention(const sd_kv_layer *kv, const int32_t *starts, int32_t
     a.n_heads = n_heads;
     a.n_kv_heads = kv->n_kv_heads;
     a.G = n_heads / kv->n_kv_heads;
-    plan(&a, kv->dtype == SD_BF16, kv->head_dim);
+    plan(&a, x_dtype == SD_BF16, kv->dtype == SD_BF16, kv->head_dim);
     return launch(a, x_dtype, kv->dtype, kv->head_dim, s);
 }
 
@@ -1575,7 +2056,7 @@ size_t sd_paged_attention_workspace(const sd_kv_pages *kv, const sd_batch *batch
     if (paged_sizes(kv, batch, n_heads, n, false, &a) != SD_OK ||
         check_call(nullptr, 0, x_dtype, n_heads, n, a.n_seqs, a.n_kv_heads, kv->head_dim, nullptr, 0, nullptr) != SD_OK)
         return 0;
-    plan(&a, kv->dtype == SD_BF16, kv->head_dim);
+    plan(&a, x_dtype == SD_BF16, kv->dtype == SD_BF16, kv->head_dim);
     return space_of(a, kv->head_dim).bytes();
 }
 
