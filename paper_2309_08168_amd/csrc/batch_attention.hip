@@ -476,24 +476,17 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_batch_attn_mfma(BatchAttnAr
               half = lane >> 5;
     const int wq = wave % NQ, wk = wave / NQ;
     const int g = blockIdx.x % a.n_kv_heads, rest = blockIdx.x / a.n_kv_heads;
-    const int split = rest / a.slots;
-    // (from the last tile, which has the most keys, to the first)
-    const Tile w = tile_of(a, a.slots - 1 - rest % a.slots);
-    const int rows = w.rows.m * a.G;
-    if (w.row0 >= rows)
-        return;  // uniform
-    auto sees = [&](int rr) { return seen_from(w.rows.past + rr / a.G, a.max_length); };
-    const int klen = __builtin_amdgcn_readfirstlane(sees(min(w.row0 + 32 * NQ, rows) - 1));
-    const int kall = __builtin_amdgcn_readfirstlane(sees(w.row0));
-    const int b0 = split * a.per_split, b1 = min(b0 + a.per_split, (klen + KB - 1) / KB);
-    if (a.splits > 1 && b0 >= b1)
-        return;
-    const int r0 = w.row0 + wq * 32;
-    const bool live = r0 < rows;  // uniform over the wave: a wave without rows loads and waits with the others
-    const int row = min(r0 + col, rows - 1), node = row / a.G, head = g * a.G + row - node * a.G;
-    const int see = seen_from(w.rows.past + node, a.max_length);
     const uint16_t *K = static_cast<const uint16_t *>(a.k) + (int64_t)g * a.head_stride;
     const uint16_t *V = static_cast<const uint16_t *>(a.v) + (int64_t)g * a.head_stride;
+    __shared__ Stream stream;
+    int32_t seq = 0, at = 0, end = 1;  // of a stream: the sequence, the spans left
+    if (a.chunks) {
+        const bool some = chunk_of(a, stream, rest, &at, &end, &seq);
+        if (blockIdx.x == 0)
+            keep_spans(a, stream);
+        if (!some)
+            return;  // uniform
+    }
 
     // A wave takes every WAVES-th KB of K's and of V's rows.  Whole blocks: lane
     // offsets that do not change, from the block's first row where its rows follow
@@ -506,15 +499,57 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_batch_attn_mfma(BatchAttnAr
         const int u = wave + WAVES * i, s = 4 * u + (lane >> 4), p = (lane & 15) ^ L::swz(s);
         off[i] = (uint32_t)(2 * ((int64_t)((s * L::RPL + p / L::C) & (one ? 63 : 15)) * a.row_stride + 8 * (p % L::C)));
     }
+    for (;;) {
+    Tile w;
+    int b0, b1, part = 0;  // blocks of keys; the part of the result, or -1: all of it
+    int klen, kall, done = 0;
+    auto sees = [&](int rr) { return seen_from(w.rows.past + rr / a.G, a.max_length); };
+    if (a.chunks) {
+        seq = __builtin_amdgcn_readfirstlane(seq);
+        w.seq = seq;
+        w.row0 = 0;
+        w.rows = rows_of(a, seq);
+    } else {
+        // (from the last tile, which has the most keys, to the first)
+        w = tile_of(a, a.slots - 1 - rest % a.slots);
+    }
+    const int rows = w.rows.m * a.G;
+    if (w.row0 >= rows)
+        return;  // uniform
+    klen = __builtin_amdgcn_readfirstlane(sees(min(w.row0 + 32 * NQ, rows) - 1));
+    kall = __builtin_amdgcn_readfirstlane(sees(w.row0));
+    if (a.chunks) {
+        const int32_t from = at - stream.pre[seq], all = stream.pre[seq + 1] - stream.pre[seq];
+        done = min(all - from, end - at);
+        b0 = __builtin_amdgcn_readfirstlane(from);
+        b1 = __builtin_amdgcn_readfirstlane(from + done);
+        part = from == 0 && done == all ? -1 : 2 * (g * a.chunks + rest) + (from == 0);
+    } else {
+        part = a.splits > 1 ? rest / a.slots : -1;
+        b0 = rest / a.slots * a.per_split;
+        b1 = b0 + a.per_split;
+    }
+    b1 = min(b1, (klen + KB - 1) / KB);
+    if (part >= 0 && !a.chunks && b0 >= b1)
+        return;
+    const int r0 = w.row0 + wq * 32;
+    const bool live = r0 < rows;  // uniform over the wave: a wave without rows loads and waits with the others
+    const int row = min(r0 + col, rows - 1), node = row / a.G, head = g * a.G + row - node * a.G;
+    const int see = seen_from(w.rows.past + node, a.max_length);
     auto load_block = [&](const Groups &k, int first, int buf) {
         if (first + KB <= klen && near) {
+            const uint16_t *k0 = uniform(K + k.off[0]), *v0 = uniform(V + k.off[0]);
 #pragma unroll
             for (int i = 0; i < NU; ++i) {
                 const int u = wave + WAVES * i;
                 if (L::C % WAVES == 0 || u < L::C) {  // uniform over the wave
-                    const int64_t at = row_at(k, one, one ? 0 : ROWS * u / 16 * 16, a.row_stride);
-                    load_to_lds16(uniform(K + at), off[i], &kv[buf][0][u * 512]);
-                    load_to_lds16(uniform(V + at), off[i], &kv[buf][1][u * 512]);
+                    if (!one) {
+                        const int64_t o = row_at(k, false, ROWS * u / 16 * 16, a.row_stride);
+                        k0 = uniform(K + o);
+                        v0 = uniform(V + o);
+                    }
+                    load_to_lds16(k0, off[i], &kv[buf][0][u * 512]);
+                    load_to_lds16(v0, off[i], &kv[buf][1][u * 512]);
                 }
             }
         } else {
@@ -755,8 +790,7 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_batch_attn_mfma(BatchAttnAr
             to[((16 * ET + 1) * NQ + wq) * 64 + lane] = l_run;
         }
         __syncthreads();
-        if (wk == 1)
-            return;
+        if (wk == 0) {
         const float m2 = to[(16 * ET * NQ + wq) * 64 + lane], l2 = to[((16 * ET + 1) * NQ + wq) * 64 + lane];
         const float m = fmaxf(m_run, m2), mu = m == -INFINITY ? 0.0f : m;
         const float w1 = __builtin_amdgcn_exp2f(m_run - mu), w2 = __builtin_amdgcn_exp2f(m2 - mu);
@@ -767,27 +801,38 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_batch_attn_mfma(BatchAttnAr
 #pragma unroll
             for (int v = 0; v < 16; ++v)
                 o[et][v] = o[et][v] * w1 + to[((16 * et + v) * NQ + wq) * 64 + lane] * w2;
-    }
-    if (!mine)
-        return;
-    const int64_t at = (int64_t)(w.rows.first + node), slot = ((int64_t)split * a.n + at) * a.n_heads + head;
-    TX *out = static_cast<TX *>(a.out) + at * a.ld_out + (int64_t)head * D;
-    const float inv = a.splits > 1 ? 1.0f : l_run == 0.0f ? 0.0f : 1.0f / l_run;
-#pragma unroll
-    for (int et = 0; et < ET; ++et)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int e = 32 * et + 8 * q + 4 * half;
-            const f32x4_t y = f32x4_t{o[et][4 * q], o[et][4 * q + 1], o[et][4 * q + 2], o[et][4 * q + 3]} * inv;
-            if (e < D) {
-                if (a.splits == 1)
-                    store4(out + e, y);
-                else
-                    store4(a.part_o + slot * D + e, y);
-            }
         }
-    if (a.splits > 1 && half == 0)
-        a.part_ml[slot] = make_float2(m_run, l_run);
+    }
+    if (mine && wk == 0) {
+        const int64_t packed = w.rows.first + node;
+        const int64_t slot = a.chunks ? (int64_t)part * a.tile + 32 * wq + col : ((int64_t)part * a.n + packed) * a.n_heads + head;
+        TX *out = static_cast<TX *>(a.out) + packed * a.ld_out + (int64_t)head * D;
+        const float inv = part >= 0 ? 1.0f : l_run == 0.0f ? 0.0f : 1.0f / l_run;
+#pragma unroll
+        for (int et = 0; et < ET; ++et)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int e = 32 * et + 8 * q + 4 * half;
+                const f32x4_t y = f32x4_t{o[et][4 * q], o[et][4 * q + 1], o[et][4 * q + 2], o[et][4 * q + 3]} * inv;
+                if (e < D) {
+                    if (part < 0)
+                        store4(out + e, y);
+                    else
+                        store4(a.part_o + slot * D + e, y);
+                }
+            }
+        if (part >= 0 && half == 0)
+            a.part_ml[slot] = make_float2(m_run, l_run);
+    }
+    at += done;
+    if (!a.chunks || at >= end)
+        return;
+    // the next sequence that has spans
+    do
+        ++seq;
+    while (stream.pre[seq + 1] <= at);
+    __syncthreads();
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -1796,17 +1841,21 @@ constexpr int FEW_ROWS = 32;
 void plan(BatchAttnArgs *a, bool x_bf16, bool bf16, int D) {
     const int64_t most = (int64_t)a->max_rows * a->G;
     const bool few = bf16 && a->paged && most <= FEW_ROWS;
-    a->tile = !bf16 ? 16 : few ? (most <= 16 ? 16 : 32) : most <= 64 ? 64 : 128;
-    a->block = few || (x_bf16 && bf16 && a->tile == 128) ? KB_FEW : KB;
+    const auto slots_of = [&](int tile) {
+        return most <= tile ? (int64_t)a->n_seqs : (int64_t)a->n * a->G / tile + a->n_seqs;
+    };
+    a->tile = !bf16 ? 16 : few ? (most <= 16 ? 16 : 32) : most <= 64 || (!a->paged && slots_of(128) * a->n_kv_heads <= env("BA_T64", 450)) ? 64 : 128;
     a->one_tile = most <= a->tile;
-    a->slots = (int32_t)(a->one_tile ? a->n_seqs : (int64_t)a->n * a->G / a->tile + a->n_seqs);
+    a->slots = (int32_t)slots_of(a->tile);
     const int64_t units = (int64_t)a->slots * a->n_kv_heads;
+    const bool stream = bf16 && a->paged && a->one_tile;
+    a->block = few || (x_bf16 && bf16 && a->tile == 128 && !stream) ? KB_FEW : KB;
     a->splits = 1;
     a->chunks = 0;
     const int blocks = (a->max_length + a->block - 1) / a->block;
     a->per_split = blocks;
-    if (few) {
-        a->span = NW * KB_FEW;
+    if (stream) {
+        a->span = few ? NW * KB_FEW : KB;
         const int64_t spans = (int64_t)a->n_seqs * ((a->max_length + a->span - 1) / a->span);
         if (a->max_length <= env("BA_WHOLE", 512) || a->n_seqs > MAX_STREAM || spans > 1 << 30)
             return;
@@ -1856,13 +1905,14 @@ void launch_mfma(const BatchAttnArgs &a, hipStream_t s) {
         hipLaunchKernelGGL((k_batch_attn_few<TX, D, 2>), grid, dim3(256), 0, s, a);
     else if (a.tile == 64)
         hipLaunchKernelGGL((k_batch_attn_mfma<TX, D, 2, 2>), grid, dim3(256), 0, s, a);
+    else if (a.block == KB)
+        hipLaunchKernelGGL((k_batch_attn_mfma<TX, D, 4, 1>), grid, dim3(256), 0, s, a);
     else if constexpr (sizeof(TX) == 2) {
         if (a.paged)
             hipLaunchKernelGGL((k_batch_attn_wide<D, true>), grid, dim3(256), 0, s, a);
         else
             hipLaunchKernelGGL((k_batch_attn_wide<D, false>), grid, dim3(256), 0, s, a);
-    } else
-        hipLaunchKernelGGL((k_batch_attn_mfma<TX, D, 4, 1>), grid, dim3(256), 0, s, a);
+    }
 }
 template <typename TX>
 void launch_bf16(const BatchAttnArgs &a, int D, hipStream_t s) {
