@@ -908,9 +908,9 @@ __global__ __launch_bounds__(256, 2) void k_batch_attn_wide(BatchAttnArgs a) {
         }
         return e;
     };
-    auto whole_pages_of = [&](int t) {  // of a block within the keys
+    auto whole_pages_of = [&](int t) {  // the same without a branch
         const int first = KB_FEW * t;
-        return Pages{{table[first >> a.page_shift], table[(first + 16) >> a.page_shift]}};
+        return Pages{{table[first >> a.page_shift], table[min(first + 16, klen - 1) >> a.page_shift]}};
     };
     auto halves_of = [&](const Pages &e, int t) {
         Halves h;
@@ -1283,11 +1283,14 @@ __global__ __launch_bounds__(256, 2) void k_batch_attn_wide(BatchAttnArgs a) {
         turn_k();
         // Where what is asked for lies within whole blocks, too, a step's loads stand
         // between its products.
-        const int quick = EVEN && near ? min(min(t1, klen / KB_FEW) - 5, kall / KB_FEW - 1) : t0;
+        // (Rows past the last key, of its block: of its pages, or of rows of the call; not
+        // past those.)
+        const bool within = PAGED || w.rows.first + KB_FEW * t1 <= a.n;
+        const int quick = EVEN && near ? min(within ? t1 - 2 : klen / KB_FEW - 5, kall / KB_FEW - 1) : t0;
         const auto quick_step = [&](int t, int at, const f32x16_t &s, f32x16_t &s_next, const u32x4_t (&p)[2],
                                     u32x4_t (&p_next)[2]) {
             asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(4 * NU) : "memory");
-            const Halves hk = halves_of(next_k, t + 4), hv = halves_of(next_v, t + 2);
+            const Halves hk = halves_of(next_k, min(t + 4, t1 - 1)), hv = halves_of(next_v, min(t + 2, t1 - 1));
             ok_next = ok_after;
             ok_after = hv.ok;
             uint16_t *to_k = kv[0][slot(t + 4)], *to_v = kv[1][slot(t + 2)];
@@ -1299,8 +1302,8 @@ __global__ __launch_bounds__(256, 2) void k_batch_attn_wide(BatchAttnArgs a) {
                 else if (i % EACH == 0)
                     load_to_lds16(uniform(V + row_at(hv, r)), off[j], to_v + u * 512);
                 if (PAGED && i == PARTS - 1) {
-                    next_k = whole_pages_of(t + 5);
-                    next_v = whole_pages_of(t + 3);
+                    next_k = whole_pages_of(min(t + 5, t1 - 1));
+                    next_v = whole_pages_of(min(t + 3, t1 - 1));
                 }
             };
             fast(at, s, s_next, p, p_next, loads);  // (a wave without rows, too, with queries of zero)
