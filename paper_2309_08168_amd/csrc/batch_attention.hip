@@ -411,9 +411,10 @@ struct Groups {
 struct Entries {
     int32_t page[4];
 };
+template <bool PAGED>
 __device__ __forceinline__ Entries entries_of(const BatchAttnArgs &a, const Tile &w, int first, int klen) {
     Entries e;
-    if (!a.table)
+    if constexpr (!PAGED)
         return e;
     const int32_t *row = a.table + (int64_t)w.seq * a.ld_table;
     e.page[0] = first < klen ? row[first >> a.page_shift] : -1;
@@ -424,10 +425,11 @@ __device__ __forceinline__ Entries entries_of(const BatchAttnArgs &a, const Tile
     }
     return e;
 }
+template <bool PAGED>
 __device__ __forceinline__ Groups groups_of(const BatchAttnArgs &a, const Tile &w, const Entries &e, int first, int klen) {
     Groups k;
     k.ok = 15;  // (keys past the last are masked by their number)
-    if (a.table && a.page_shift < 6) {
+    if (PAGED && a.page_shift < 6) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             // (without a page: any rows, which are masked, and taken for finite)
@@ -439,7 +441,7 @@ __device__ __forceinline__ Groups groups_of(const BatchAttnArgs &a, const Tile &
         }
         return k;
     }
-    if (a.table) {
+    if constexpr (PAGED) {
         const int page = __builtin_amdgcn_readfirstlane(e.page[0]);
         const bool there = (uint32_t)page < (uint32_t)a.n_pages;
         k.off[0] = (there ? page * a.page_stride : 0) + (int64_t)(first & ((1 << a.page_shift) - 1)) * a.row_stride;
@@ -466,9 +468,13 @@ __device__ __forceinline__ uint64_t seen_bits(int count, uint32_t ok) {
     return (count >= 64 ? ~0ull : count <= 0 ? 0 : (1ull << count) - 1) & groups;
 }
 
-template <typename TX, int D, int NQ, int NK>
+// Where keys come from: packed, pages (tiles, and shares of their keys), or pages as a
+// stream (a tile a sequence).
+enum Source { PACKED, PAGES, STREAM };
+
+template <typename TX, int D, int NQ, int NK, Source FROM>
 __global__ __launch_bounds__(64 * NQ * NK, 2) void k_batch_attn_mfma(BatchAttnArgs a) {
-    constexpr bool EXACT = sizeof(TX) == 4;
+    constexpr bool EXACT = sizeof(TX) == 4, PAGED = FROM != PACKED;
     constexpr int T = EXACT ? X_TERMS : 1, WAVES = NQ * NK, ES = D / 16, ET = D < 32 ? 1 : D / 32;
     using L = Lines<D>;
     __shared__ __attribute__((aligned(1024))) uint16_t kv[2][2][KB * D];  // [block % 2][K, V]
@@ -478,9 +484,9 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_batch_attn_mfma(BatchAttnAr
     const int g = blockIdx.x % a.n_kv_heads, rest = blockIdx.x / a.n_kv_heads;
     const uint16_t *K = static_cast<const uint16_t *>(a.k) + (int64_t)g * a.head_stride;
     const uint16_t *V = static_cast<const uint16_t *>(a.v) + (int64_t)g * a.head_stride;
-    __shared__ Stream stream;
+    __shared__ typename std::conditional<FROM == STREAM, Stream, int>::type stream;
     int32_t seq = 0, at = 0, end = 1;  // of a stream: the sequence, the spans left
-    if (a.chunks) {
+    if constexpr (FROM == STREAM) {
         const bool some = chunk_of(a, stream, rest, &at, &end, &seq);
         if (blockIdx.x == 0)
             keep_spans(a, stream);
@@ -492,7 +498,7 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_batch_attn_mfma(BatchAttnAr
     // offsets that do not change, from the block's first row where its rows follow
     // one another (packed, or pages of a block and more), else from a group's.
     constexpr int NU = (L::C + WAVES - 1) / WAVES, ROWS = 4 * L::RPL;  // loads of a wave; rows of a load
-    const bool one = !a.table || a.page_shift >= 6, near = (one || D > 16) && near_rows(a.row_stride);
+    const bool one = !PAGED || a.page_shift >= 6, near = (one || D > 16) && near_rows(a.row_stride);
     uint32_t off[NU];
 #pragma unroll
     for (int i = 0; i < NU; ++i) {
@@ -504,7 +510,7 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_batch_attn_mfma(BatchAttnAr
     int b0, b1, part = 0;  // blocks of keys; the part of the result, or -1: all of it
     int klen, kall, done = 0;
     auto sees = [&](int rr) { return seen_from(w.rows.past + rr / a.G, a.max_length); };
-    if (a.chunks) {
+    if constexpr (FROM == STREAM) {
         seq = __builtin_amdgcn_readfirstlane(seq);
         w.seq = seq;
         w.row0 = 0;
@@ -518,19 +524,23 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_batch_attn_mfma(BatchAttnAr
         return;  // uniform
     klen = __builtin_amdgcn_readfirstlane(sees(min(w.row0 + 32 * NQ, rows) - 1));
     kall = __builtin_amdgcn_readfirstlane(sees(w.row0));
-    if (a.chunks) {
+    if constexpr (FROM == STREAM) {
         const int32_t from = at - stream.pre[seq], all = stream.pre[seq + 1] - stream.pre[seq];
         done = min(all - from, end - at);
         b0 = __builtin_amdgcn_readfirstlane(from);
         b1 = __builtin_amdgcn_readfirstlane(from + done);
         part = from == 0 && done == all ? -1 : 2 * (g * a.chunks + rest) + (from == 0);
-    } else {
+    } else if constexpr (FROM == PAGES) {
         part = a.splits > 1 ? rest / a.slots : -1;
         b0 = rest / a.slots * a.per_split;
         b1 = b0 + a.per_split;
+    } else {
+        part = -1;
+        b0 = 0;
+        b1 = INT32_MAX;
     }
     b1 = min(b1, (klen + KB - 1) / KB);
-    if (part >= 0 && !a.chunks && b0 >= b1)
+    if (FROM == PAGES && part >= 0 && b0 >= b1)
         return;
     const int r0 = w.row0 + wq * 32;
     const bool live = r0 < rows;  // uniform over the wave: a wave without rows loads and waits with the others
@@ -563,7 +573,7 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_batch_attn_mfma(BatchAttnAr
             }
         }
     };
-    Entries entries = entries_of(a, w, KB * b0, klen);
+    Entries entries = entries_of<PAGED>(a, w, KB * b0, klen);
     // The queries are asked for before the first block: loads return in order.
     const TX *qs = static_cast<const TX *>(a.q) + (int64_t)(w.rows.first + node) * a.ld_q + (int64_t)head * D + 8 * half;
     u32x4_t qf[ES][T];
@@ -578,10 +588,10 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_batch_attn_mfma(BatchAttnAr
         }
     }
     __builtin_amdgcn_sched_barrier(0);
-    Groups k = groups_of(a, w, entries, KB * b0, klen);
+    Groups k = groups_of<PAGED>(a, w, entries, KB * b0, klen);
     if (b0 < b1)
         load_block(k, KB * b0, 0);
-    entries = entries_of(a, w, KB * (b0 + 1), klen);
+    entries = entries_of<PAGED>(a, w, KB * (b0 + 1), klen);
     // Rows past the last are zeros, which draw less power than copies of it.
     const bool mine = r0 + col < rows;
 #pragma unroll
@@ -622,9 +632,9 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_batch_attn_mfma(BatchAttnAr
         // read of the other buffer has returned
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         if (b + 1 < b1) {
-            k = groups_of(a, w, entries, first + KB, klen);
+            k = groups_of<PAGED>(a, w, entries, first + KB, klen);
             load_block(k, first + KB, buf ^ 1);
-            entries = entries_of(a, w, first + 2 * KB, klen);
+            entries = entries_of<PAGED>(a, w, first + 2 * KB, klen);
         }
         const bool full = first + KB <= kall && now.ok == 15;  // every row sees every key
         bool odd = false;
@@ -805,7 +815,7 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_batch_attn_mfma(BatchAttnAr
     }
     if (mine && wk == 0) {
         const int64_t packed = w.rows.first + node;
-        const int64_t slot = a.chunks ? (int64_t)part * a.tile + 32 * wq + col : ((int64_t)part * a.n + packed) * a.n_heads + head;
+        const int64_t slot = FROM == STREAM ? (int64_t)part * a.tile + 32 * wq + col : ((int64_t)part * a.n + packed) * a.n_heads + head;
         TX *out = static_cast<TX *>(a.out) + packed * a.ld_out + (int64_t)head * D;
         const float inv = part >= 0 ? 1.0f : l_run == 0.0f ? 0.0f : 1.0f / l_run;
 #pragma unroll
@@ -824,14 +834,18 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_batch_attn_mfma(BatchAttnAr
         if (part >= 0 && half == 0)
             a.part_ml[slot] = make_float2(m_run, l_run);
     }
-    at += done;
-    if (!a.chunks || at >= end)
+    if constexpr (FROM != STREAM) {
         return;
-    // the next sequence that has spans
-    do
-        ++seq;
-    while (stream.pre[seq + 1] <= at);
-    __syncthreads();
+    } else {
+        at += done;
+        if (at >= end)
+            return;
+        // the next sequence that has spans
+        do
+            ++seq;
+        while (stream.pre[seq + 1] <= at);
+        __syncthreads();
+    }
     }
 }
 
@@ -1387,7 +1401,7 @@ __global__ __launch_bounds__(256, 2) void k_batch_attn_wide(BatchAttnArgs a) {
 // LDS lines are permuted for the reads here: eight rows, two adjacent chunks each.
 // A lane holds the table's entry for half a block of the wave, 32 blocks at a time.
 // A work-group takes a sequence whole, or the chunk of a stream.
-template <typename TX, int D, int QT>
+template <typename TX, int D, int QT, bool STREAMED>
 __global__ __launch_bounds__(256, QT == 1 || D < 128 ? 2 : 1) void k_batch_attn_few(BatchAttnArgs a) {
     constexpr bool EXACT = sizeof(TX) == 4;
     constexpr int T = EXACT ? X_TERMS : 1, ES = D < 32 ? 1 : D / 32, ET = D / 16, ROWS = 16 * QT, OP = D + 4;
@@ -1396,12 +1410,12 @@ __global__ __launch_bounds__(256, QT == 1 || D < 128 ? 2 : 1) void k_batch_attn_
     constexpr int WORDS = VB > ROWS * OP ? VB : ROWS * OP;
     __shared__ __attribute__((aligned(1024))) uint32_t tile[NW][WORDS];  // two V blocks, or the outputs
     __shared__ float2 ml[NW][ROWS];
-    __shared__ Stream stream;
+    __shared__ typename std::conditional<STREAMED, Stream, int>::type stream;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 15,
               grp = lane >> 4;
     const int g = blockIdx.x % a.n_kv_heads, chunk = blockIdx.x / a.n_kv_heads;
     int32_t seq = chunk, at = 0, end = 1;
-    if (a.chunks) {
+    if constexpr (STREAMED) {
         const bool some = chunk_of(a, stream, chunk, &at, &end, &seq);
         if (blockIdx.x == 0)
             keep_spans(a, stream);
@@ -1410,9 +1424,12 @@ __global__ __launch_bounds__(256, QT == 1 || D < 128 ? 2 : 1) void k_batch_attn_
     }
     for (;;) {
     seq = __builtin_amdgcn_readfirstlane(seq);
-    const int32_t from = a.chunks ? __builtin_amdgcn_readfirstlane(at - stream.pre[seq]) : 0;
-    const int32_t all = a.chunks ? __builtin_amdgcn_readfirstlane(stream.pre[seq + 1] - stream.pre[seq]) : 1 << 30;
-    const int32_t to = a.chunks ? min(all, from + end - at) : all;
+    int32_t from = 0, to = 0, all = 0;  // spans
+    if constexpr (STREAMED) {
+        from = __builtin_amdgcn_readfirstlane(at - stream.pre[seq]);
+        all = __builtin_amdgcn_readfirstlane(stream.pre[seq + 1] - stream.pre[seq]);
+        to = min(all, from + end - at);
+    }
     constexpr int BLOCKS = NW;  // of a span
     const int b0 = BLOCKS * from + wave;
     // the entries of this wave's blocks b .., of groups past the table none
@@ -1431,8 +1448,7 @@ __global__ __launch_bounds__(256, QT == 1 || D < 128 ? 2 : 1) void k_batch_attn_
         return;  // uniform (no sequence of a stream's)
     const int klen = __builtin_amdgcn_readfirstlane(seen_from(w.rows.past + w.rows.m - 1, a.max_length));
     const int kall = __builtin_amdgcn_readfirstlane(seen_from(w.rows.past, a.max_length));
-    const int64_t last = (int64_t)BLOCKS * to;
-    const int b1 = (int)min(last, (int64_t)(klen + KB_FEW - 1) / KB_FEW);
+    const int blocks = (klen + KB_FEW - 1) / KB_FEW, b1 = STREAMED ? min(BLOCKS * to, blocks) : blocks;
     const uint16_t *K = static_cast<const uint16_t *>(a.k) + (int64_t)g * a.head_stride;
     const uint16_t *V = static_cast<const uint16_t *>(a.v) + (int64_t)g * a.head_stride;
     uint16_t *vt = reinterpret_cast<uint16_t *>(tile[wave]);
@@ -1711,17 +1727,22 @@ __global__ __launch_bounds__(256, QT == 1 || D < 128 ? 2 : 1) void k_batch_attn_
             ml[wave][16 * i + col] = make_float2(m_run[i], l_run[i]);
     }
     __syncthreads();
-    const bool whole = !a.chunks || (from == 0 && to == all);
-    merge_waves<TX, D, ROWS>(a, w, reinterpret_cast<const float *>(tile), WORDS, &ml[0][0], g,
-                             whole ? -1 : 2 * (g * a.chunks + chunk) + (from == 0));
-    at += to - from;
-    if (!a.chunks || at >= end)
+    int part = -1;
+    if constexpr (STREAMED)
+        part = from == 0 && to == all ? -1 : 2 * (g * a.chunks + chunk) + (from == 0);
+    merge_waves<TX, D, ROWS>(a, w, reinterpret_cast<const float *>(tile), WORDS, &ml[0][0], g, part);
+    if constexpr (!STREAMED) {
         return;
-    // the next sequence that has spans
-    do
-        ++seq;
-    while (stream.pre[seq + 1] <= at);
-    __syncthreads();
+    } else {
+        at += to - from;
+        if (at >= end)
+            return;
+        // the next sequence that has spans
+        do
+            ++seq;
+        while (stream.pre[seq + 1] <= at);
+        __syncthreads();
+    }
     }
 }
 
@@ -1851,23 +1872,22 @@ void plan(BatchAttnArgs *a, bool x_bf16, bool bf16, int D) {
     a->one_tile = most <= a->tile;
     a->slots = (int32_t)slots_of(a->tile);
     const int64_t units = (int64_t)a->slots * a->n_kv_heads;
-    const bool stream = bf16 && a->paged && a->one_tile;
+    a->span = few ? NW * KB_FEW : KB;
+    const int64_t spans = (int64_t)a->n_seqs * ((a->max_length + a->span - 1) / a->span);
+    const bool stream = bf16 && a->paged && a->one_tile && a->max_length > env("BA_WHOLE", 512) && a->n_seqs <= MAX_STREAM &&
+                        spans <= 1 << 30;
     a->block = few || (x_bf16 && bf16 && a->tile == 128 && !stream) ? KB_FEW : KB;
     a->splits = 1;
     a->chunks = 0;
     const int blocks = (a->max_length + a->block - 1) / a->block;
     a->per_split = blocks;
     if (stream) {
-        a->span = few ? NW * KB_FEW : KB;
-        const int64_t spans = (int64_t)a->n_seqs * ((a->max_length + a->span - 1) / a->span);
-        if (a->max_length <= env("BA_WHOLE", 512) || a->n_seqs > MAX_STREAM || spans > 1 << 30)
-            return;
         const int groups = env("BA_GROUPS", a->tile == 32 && D == 128 ? 256 : 512);
         a->chunks = (int32_t)std::min<int64_t>(spans, std::max(1, groups / a->n_kv_heads));
         a->least = env("BA_LEAST", 1);
         return;
     }
-    if (!a->paged)
+    if (!a->paged || few)
         return;
     const int want = (int)std::max<int64_t>(1, std::min<int64_t>((blocks + 7) / 8, 512 / units));
     a->per_split = (blocks + want - 1) / want;
@@ -1901,20 +1921,36 @@ void launch_f32(const BatchAttnArgs &a, int D, hipStream_t s) {
 
 template <typename TX, int D>
 void launch_mfma(const BatchAttnArgs &a, hipStream_t s) {
-    const dim3 grid((unsigned)(a.chunks ? a.chunks * a.n_kv_heads : a.slots * a.n_kv_heads * a.splits));
-    if (a.tile == 16)
-        hipLaunchKernelGGL((k_batch_attn_few<TX, D, 1>), grid, dim3(256), 0, s, a);
-    else if (a.tile == 32)
-        hipLaunchKernelGGL((k_batch_attn_few<TX, D, 2>), grid, dim3(256), 0, s, a);
-    else if (a.tile == 64)
-        hipLaunchKernelGGL((k_batch_attn_mfma<TX, D, 2, 2>), grid, dim3(256), 0, s, a);
-    else if (a.block == KB)
-        hipLaunchKernelGGL((k_batch_attn_mfma<TX, D, 4, 1>), grid, dim3(256), 0, s, a);
-    else if constexpr (sizeof(TX) == 2) {
-        if (a.paged)
-            hipLaunchKernelGGL((k_batch_attn_wide<D, true>), grid, dim3(256), 0, s, a);
+    const dim3 grid((unsigned)(a.chunks ? a.chunks * a.n_kv_heads : a.slots * a.n_kv_heads * a.splits)), block(256);
+    if (a.tile == 16) {
+        if (a.chunks)
+            hipLaunchKernelGGL((k_batch_attn_few<TX, D, 1, true>), grid, block, 0, s, a);
         else
-            hipLaunchKernelGGL((k_batch_attn_wide<D, false>), grid, dim3(256), 0, s, a);
+            hipLaunchKernelGGL((k_batch_attn_few<TX, D, 1, false>), grid, block, 0, s, a);
+    } else if (a.tile == 32) {
+        if (a.chunks)
+            hipLaunchKernelGGL((k_batch_attn_few<TX, D, 2, true>), grid, block, 0, s, a);
+        else
+            hipLaunchKernelGGL((k_batch_attn_few<TX, D, 2, false>), grid, block, 0, s, a);
+    } else if (a.tile == 64) {
+        if (a.chunks)
+            hipLaunchKernelGGL((k_batch_attn_mfma<TX, D, 2, 2, STREAM>), grid, block, 0, s, a);
+        else if (a.paged)
+            hipLaunchKernelGGL((k_batch_attn_mfma<TX, D, 2, 2, PAGES>), grid, block, 0, s, a);
+        else
+            hipLaunchKernelGGL((k_batch_attn_mfma<TX, D, 2, 2, PACKED>), grid, block, 0, s, a);
+    } else if (a.chunks) {
+        hipLaunchKernelGGL((k_batch_attn_mfma<TX, D, 4, 1, STREAM>), grid, block, 0, s, a);
+    } else if constexpr (sizeof(TX) == 2) {
+        if (a.paged)
+            hipLaunchKernelGGL((k_batch_attn_wide<D, true>), grid, block, 0, s, a);
+        else
+            hipLaunchKernelGGL((k_batch_attn_wide<D, false>), grid, block, 0, s, a);
+    } else {
+        if (a.paged)
+            hipLaunchKernelGGL((k_batch_attn_mfma<TX, D, 4, 1, PAGES>), grid, block, 0, s, a);
+        else
+            hipLaunchKernelGGL((k_batch_attn_mfma<TX, D, 4, 1, PACKED>), grid, block, 0, s, a);
     }
 }
 template <typename TX>
