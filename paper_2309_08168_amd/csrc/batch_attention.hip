@@ -40,7 +40,8 @@ struct BatchAttnArgs {
     int32_t n, n_seqs, max_rows, max_length, n_pages, page_shift;
     int32_t n_heads, n_kv_heads, G;
     int32_t paged;                     // whether over pages
-    int32_t chunks, least, span;       // of the streams: chunks (0: no streams), spans of one at least, keys of a span
+    int32_t waves;                     // of a work-group
+    int32_t chunks, span;              // of the streams: chunks (0: no streams), keys of a span
     int32_t *spans;                    // [n_seqs + 2]: spans before each sequence, and of a chunk
     int32_t tile, slots, one_tile;     // rows of a tile; tiles at most; whether a sequence has at most one
     int32_t splits, per_split, block;  // shares of the keys; blocks of a share; keys of a block
@@ -75,6 +76,22 @@ __device__ __forceinline__ Tile tile_of(const BatchAttnArgs &a, int32_t t) {
     Tile w;
     int64_t before = 0;  // the slots of the sequences before
     w.seq = t;
+    if (!a.one_tile && a.starts && a.n_seqs < 64) {
+        // (one round trip: a lane's start, the next one's and its length)
+        const int lane = threadIdx.x & 63, j = min(lane, a.n_seqs);
+        const int32_t start = a.starts[j], length = a.lengths ? a.lengths[min(j, a.n_seqs - 1)] : 0;
+        const int64_t own = (int64_t)start * a.G / a.tile + j;
+        const int seq = min((int)__popcll(__ballot(lane >= 1 && lane <= a.n_seqs && own <= t)), a.n_seqs - 1);
+        w.seq = seq;
+        const int32_t first = __builtin_amdgcn_readlane(start, seq);
+        w.rows = seq_rows(first, __builtin_amdgcn_readlane(start, seq + 1), __builtin_amdgcn_readlane(length, seq), a.n,
+                          a.max_rows);
+        if (!a.lengths)
+            w.rows.past = 0;
+        const int64_t row0 = (t - ((int64_t)first * a.G / a.tile + seq)) * a.tile, most = (int64_t)w.rows.m * a.G;
+        w.row0 = (int32_t)(row0 < 0 || row0 > most ? most : row0);
+        return w;
+    }
     if (!a.one_tile) {
         const auto slot = [&](int32_t j) { return (int64_t)start_of(a, j) * a.G / a.tile + j; };
         w.seq = min(wave_count(a.n_seqs, t, slot), a.n_seqs - 1);
@@ -94,22 +111,22 @@ __device__ __forceinline__ Tile tile_of(const BatchAttnArgs &a, int32_t t) {
 // floats apart; (maximum, sum) [wave][row]) merged in wave order: the result, or with
 // part >= 0 that part's state, its rows adjacent there from `part` on, or by
 // packed row and head with a.chunks 0.
-template <typename TX, int D, int ROWS>
+template <typename TX, int D, int ROWS, int W>
 __device__ __forceinline__ void merge_waves(const BatchAttnArgs &a, const Tile &w, const float *o, int pitch,
                                             const float2 *ml, int g, int part) {
 #pragma unroll
-    for (int i = threadIdx.x; i < ROWS * D / 4; i += NW * 64) {
+    for (int i = threadIdx.x; i < ROWS * D / 4; i += W * 64) {
         const int rc = i / (D / 4), e = 4 * (i % (D / 4)), rr = w.row0 + rc;
         if (rr >= w.rows.m * a.G)
             break;  // i only grows
         float m = -INFINITY, L = 0.0f;
         f32x4_t O = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int v = 0; v < NW; ++v)
+        for (int v = 0; v < W; ++v)
             m = fmaxf(m, ml[v * ROWS + rc].x);
         const float mu = m == -INFINITY ? 0.0f : m;
 #pragma unroll
-        for (int v = 0; v < NW; ++v) {
+        for (int v = 0; v < W; ++v) {
             // (a wave without keys has weight zero, output zero)
             const float wt = __builtin_amdgcn_exp2f(ml[v * ROWS + rc].x - mu);
             L = fmaf(wt, ml[v * ROWS + rc].y, L);
@@ -140,19 +157,20 @@ __device__ __forceinline__ void merge_waves(const BatchAttnArgs &a, const Tile &
 constexpr int MAX_STREAM = 1024;  // sequences: every work-group adds up their spans
 
 struct Stream {
-    int32_t pre[MAX_STREAM + 1], wave[NW], first;
+    int32_t pre[MAX_STREAM + 1], wave[8], first;
 };
 // Spans of a sequence: one at least where it has rows, which get zeros.
 __device__ __forceinline__ int32_t spans_of(const BatchAttnArgs &a, const SeqRows &r) {
     return r.m == 0 ? 0 : max(1, (seen_from(r.past + r.m - 1, a.max_length) + a.span - 1) / a.span);
 }
 // The spans [at, end) of chunk c and the sequence that `at` is in; false: none.
+template <int W>  // waves
 __device__ __forceinline__ bool chunk_of(const BatchAttnArgs &a, Stream &st, int32_t c, int32_t *at, int32_t *end,
                                          int32_t *seq) {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, per = (a.n_seqs + NW * 64 - 1) / (NW * 64);
-    int32_t own[MAX_STREAM / (NW * 64)], sum = 0;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, per = (a.n_seqs + W * 64 - 1) / (W * 64);
+    int32_t own[MAX_STREAM / (W * 64)], sum = 0;
 #pragma unroll
-    for (int j = 0; j < MAX_STREAM / (NW * 64); ++j) {
+    for (int j = 0; j < MAX_STREAM / (W * 64); ++j) {
         const int s = tid * per + j;
         own[j] = j < per && s < a.n_seqs ? spans_of(a, rows_of(a, s)) : 0;
         sum += own[j];
@@ -168,15 +186,15 @@ __device__ __forceinline__ bool chunk_of(const BatchAttnArgs &a, Stream &st, int
     __syncthreads();
     int32_t before = upto - sum, total = 0;
 #pragma unroll
-    for (int v = 0; v < NW; ++v) {
+    for (int v = 0; v < W; ++v) {
         before += v < wave ? st.wave[v] : 0;
         total += st.wave[v];
     }
-    const int32_t len = max((total + a.chunks - 1) / a.chunks, a.least);
+    const int32_t len = max((total + a.chunks - 1) / a.chunks, 1);
     *at = c * len;
     *end = min(*at + len, total);
 #pragma unroll
-    for (int j = 0; j < MAX_STREAM / (NW * 64); ++j) {
+    for (int j = 0; j < MAX_STREAM / (W * 64); ++j) {
         const int s = tid * per + j;
         if (j < per && s < a.n_seqs) {
             st.pre[s] = before;
@@ -192,9 +210,10 @@ __device__ __forceinline__ bool chunk_of(const BatchAttnArgs &a, Stream &st, int
     return *at < *end;
 }
 // What the join reads, by one work-group.
+template <int W>
 __device__ __forceinline__ void keep_spans(const BatchAttnArgs &a, const Stream &st) {
-    const int32_t total = st.pre[a.n_seqs], len = max((total + a.chunks - 1) / a.chunks, a.least);
-    for (int s = threadIdx.x; s <= a.n_seqs; s += NW * 64)
+    const int32_t total = st.pre[a.n_seqs], len = max((total + a.chunks - 1) / a.chunks, 1);
+    for (int s = threadIdx.x; s <= a.n_seqs; s += W * 64)
         a.spans[s] = st.pre[s];
     if (threadIdx.x == 0)
         a.spans[a.n_seqs + 1] = len;
@@ -378,7 +397,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_batch_attn_f32(BatchAttnArgs a) 
     if (g4 == 0)
         ml[wave][c] = make_float2(m_run, l_run);
     __syncthreads();
-    merge_waves<TX, D, 16>(a, w, &tile[0][0], 16 * OP, &ml[0][0], g, a.splits > 1 ? split : -1);
+    merge_waves<TX, D, 16, NW>(a, w, &tile[0][0], 16 * OP, &ml[0][0], g, a.splits > 1 ? split : -1);
 }
 
 // ---------------------------------------------------------------------------
@@ -487,9 +506,9 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_batch_attn_mfma(BatchAttnAr
     __shared__ typename std::conditional<FROM == STREAM, Stream, int>::type stream;
     int32_t seq = 0, at = 0, end = 1;  // of a stream: the sequence, the spans left
     if constexpr (FROM == STREAM) {
-        const bool some = chunk_of(a, stream, rest, &at, &end, &seq);
+        const bool some = chunk_of<WAVES>(a, stream, rest, &at, &end, &seq);
         if (blockIdx.x == 0)
-            keep_spans(a, stream);
+            keep_spans<WAVES>(a, stream);
         if (!some)
             return;  // uniform
     }
@@ -1401,24 +1420,24 @@ __global__ __launch_bounds__(256, 2) void k_batch_attn_wide(BatchAttnArgs a) {
 // LDS lines are permuted for the reads here: eight rows, two adjacent chunks each.
 // A lane holds the table's entry for half a block of the wave, 32 blocks at a time.
 // A work-group takes a sequence whole, or the chunk of a stream.
-template <typename TX, int D, int QT, bool STREAMED>
-__global__ __launch_bounds__(256, QT == 1 || D < 128 ? 2 : 1) void k_batch_attn_few(BatchAttnArgs a) {
+template <typename TX, int D, int QT, int W, bool STREAMED>
+__global__ __launch_bounds__(64 * W, W == 8 ? 1 : QT == 1 || D < 128 ? 2 : 1) void k_batch_attn_few(BatchAttnArgs a) {
     constexpr bool EXACT = sizeof(TX) == 4;
     constexpr int T = EXACT ? X_TERMS : 1, ES = D < 32 ? 1 : D / 32, ET = D / 16, ROWS = 16 * QT, OP = D + 4;
     using L = FewLines<D>;
     constexpr int VB = KB_FEW * D;  // elements of a V block
     constexpr int WORDS = VB > ROWS * OP ? VB : ROWS * OP;
-    __shared__ __attribute__((aligned(1024))) uint32_t tile[NW][WORDS];  // two V blocks, or the outputs
-    __shared__ float2 ml[NW][ROWS];
+    __shared__ __attribute__((aligned(1024))) uint32_t tile[W][WORDS];  // two V blocks, or the outputs
+    __shared__ float2 ml[W][ROWS];
     __shared__ typename std::conditional<STREAMED, Stream, int>::type stream;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 15,
               grp = lane >> 4;
     const int g = blockIdx.x % a.n_kv_heads, chunk = blockIdx.x / a.n_kv_heads;
     int32_t seq = chunk, at = 0, end = 1;
     if constexpr (STREAMED) {
-        const bool some = chunk_of(a, stream, chunk, &at, &end, &seq);
+        const bool some = chunk_of<W>(a, stream, chunk, &at, &end, &seq);
         if (blockIdx.x == 0)
-            keep_spans(a, stream);
+            keep_spans<W>(a, stream);
         if (!some)
             return;  // uniform
     }
@@ -1430,12 +1449,12 @@ __global__ __launch_bounds__(256, QT == 1 || D < 128 ? 2 : 1) void k_batch_attn_
         all = __builtin_amdgcn_readfirstlane(stream.pre[seq + 1] - stream.pre[seq]);
         to = min(all, from + end - at);
     }
-    constexpr int BLOCKS = NW;  // of a span
+    constexpr int BLOCKS = W;  // of a span
     const int b0 = BLOCKS * from + wave;
     // the entries of this wave's blocks b .., of groups past the table none
     const int32_t *table = a.table + (int64_t)seq * a.ld_table;
     auto entries_from = [&](int b) {
-        const int64_t first = KB_FEW * ((int64_t)b + NW * (lane >> 1)) + 16 * (lane & 1);
+        const int64_t first = KB_FEW * ((int64_t)b + W * (lane >> 1)) + 16 * (lane & 1);
         return first < a.max_length ? table[first >> a.page_shift] : -1;
     };
     int entries = entries_from(b0);
@@ -1563,7 +1582,7 @@ __global__ __launch_bounds__(256, QT == 1 || D < 128 ? 2 : 1) void k_batch_attn_
     const char *vb = reinterpret_cast<const char *>(vt);
 
     int buf = 0;
-    for (; b < b1; b += NW, buf ^= 1) {
+    for (; b < b1; b += W, buf ^= 1) {
         const int first = KB_FEW * b;
         const Halves now = k;
         f32x4_t s[QT][2];
@@ -1581,14 +1600,14 @@ __global__ __launch_bounds__(256, QT == 1 || D < 128 ? 2 : 1) void k_batch_attn_
         // this block's V has landed (it was asked for before this block's K, or
         // just after), then the next block's loads
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        if (b + NW < b1) {
+        if (b + W < b1) {
             if (++slot == 32) {
                 slot = 0;
-                entries = entries_from(b + NW);
+                entries = entries_from(b + W);
             }
-            k = halves_of(b + NW, slot);
-            load_v(k, first + NW * KB_FEW, buf ^ 1);
-            load_k(k, first + NW * KB_FEW);
+            k = halves_of(b + W, slot);
+            load_v(k, first + W * KB_FEW, buf ^ 1);
+            load_k(k, first + W * KB_FEW);
         }
         const bool full = first + KB_FEW <= kall && now.ok == 3;  // every row sees every key
         // Infinities and NaN among values that some row does not see: it must not
@@ -1730,7 +1749,7 @@ __global__ __launch_bounds__(256, QT == 1 || D < 128 ? 2 : 1) void k_batch_attn_
     int part = -1;
     if constexpr (STREAMED)
         part = from == 0 && to == all ? -1 : 2 * (g * a.chunks + chunk) + (from == 0);
-    merge_waves<TX, D, ROWS>(a, w, reinterpret_cast<const float *>(tile), WORDS, &ml[0][0], g, part);
+    merge_waves<TX, D, ROWS, W>(a, w, reinterpret_cast<const float *>(tile), WORDS, &ml[0][0], g, part);
     if constexpr (!STREAMED) {
         return;
     } else {
@@ -1858,40 +1877,55 @@ __global__ __launch_bounds__(THREADS) void k_batch_join_stream(BatchAttnArgs a, 
            total == 0.0f ? f32x4_t{0.0f, 0.0f, 0.0f, 0.0f} : O / total);
 }
 
-// Tiles, and shares of the keys, from the sizes alone (what lies in device memory
-// is not known here).
-static int env(const char *n, int d) { const char *v = getenv(n); return v ? atoi(v) : d; }
-constexpr int FEW_ROWS = 32;
+// Tiles, and how the keys are shared out, from the sizes alone (what lies in device
+// memory is not known here).
+//   Streams (sequences of one tile) where work-groups of whole sequences would end
+// unevenly, or be too few: contexts past 512, past 1024 with a tile for every
+// CU, past 2048 with two.  us, streams and whole, a token of 250 .. 500 keys (40
+// heads, 8 sequences) 23.1 and 18.5, of 750 .. 1500 46.3 and 49.2; 64 heads on 8, 4
+// sequences of up to 700 11.5 and 13.1, 32 24.5 and 17.9, 128 72.6 and 61.2; chains of
+// 13, 16 sequences of up to 700 35.6 and 43.3, 8 of 40 heads 29.2 and 24.9.
+//   Eight waves a work-group for long ones: 60000 keys 57.7 -> 55.2 us, 64 sequences of
+// 500 .. 8000 197 -> 193; 8 sequences of 750 .. 1500 (40 heads) 46.6 -> 48.7.
+//   Packed tiles of 64 or 128 rows, us: 1023 rows of 40 heads (360 tiles) float32 51
+// and 68, bfloat16 31.8 and 35.5; 1000 of 64 heads on 8 (512) 72 and 71, 43 and 35.
+constexpr int FEW_ROWS = 32, CUS = 256, LONG = 2048, NARROW = 450;
 void plan(BatchAttnArgs *a, bool x_bf16, bool bf16, int D) {
     const int64_t most = (int64_t)a->max_rows * a->G;
     const bool few = bf16 && a->paged && most <= FEW_ROWS;
     const auto slots_of = [&](int tile) {
         return most <= tile ? (int64_t)a->n_seqs : (int64_t)a->n * a->G / tile + a->n_seqs;
     };
-    a->tile = !bf16 ? 16 : few ? (most <= 16 ? 16 : 32) : most <= 64 || (!a->paged && slots_of(128) * a->n_kv_heads <= env("BA_T64", 450)) ? 64 : 128;
+    const bool narrow = most <= 64 || (!a->paged && slots_of(128) * a->n_kv_heads <= NARROW);
+    a->tile = !bf16 ? 16 : few ? (most <= 16 ? 16 : 32) : narrow ? 64 : 128;
     a->one_tile = most <= a->tile;
     a->slots = (int32_t)slots_of(a->tile);
     const int64_t units = (int64_t)a->slots * a->n_kv_heads;
-    a->span = few ? NW * KB_FEW : KB;
-    const int64_t spans = (int64_t)a->n_seqs * ((a->max_length + a->span - 1) / a->span);
-    const bool stream = bf16 && a->paged && a->one_tile && a->max_length > env("BA_WHOLE", 512) && a->n_seqs <= MAX_STREAM &&
-                        spans <= 1 << 30;
-    a->block = few || (x_bf16 && bf16 && a->tile == 128 && !stream) ? KB_FEW : KB;
     a->splits = 1;
     a->chunks = 0;
+    a->waves = NW;
+    if (bf16 && a->paged && a->one_tile) {
+        const int whole = 512 * (int)std::max<int64_t>(1, std::min<int64_t>(4, units / (CUS / 2)));
+        const int waves = few && a->tile == 16 && a->max_length > LONG ? 8 : NW, span = few ? waves * KB_FEW : KB;
+        const int64_t spans = (int64_t)a->n_seqs * ((a->max_length + span - 1) / span);
+        if (a->max_length > whole && a->n_seqs <= MAX_STREAM && spans <= 1 << 30) {
+            // as many work-groups as run at once
+            const int at_once = waves == 8 || (a->tile == 32 && D == 128) ? CUS : 2 * CUS;
+            a->waves = waves;
+            a->span = span;
+            a->block = few ? KB_FEW : KB;
+            a->chunks = (int32_t)std::min<int64_t>(spans, std::max(1, at_once / a->n_kv_heads));
+            return;
+        }
+    }
+    a->block = few || (x_bf16 && bf16 && a->tile == 128) ? KB_FEW : KB;
     const int blocks = (a->max_length + a->block - 1) / a->block;
     a->per_split = blocks;
-    if (stream) {
-        const int groups = env("BA_GROUPS", a->tile == 32 && D == 128 ? 256 : 512);
-        a->chunks = (int32_t)std::min<int64_t>(spans, std::max(1, groups / a->n_kv_heads));
-        a->least = env("BA_LEAST", 1);
-        return;
+    if (a->paged && !few) {
+        const int want = (int)std::max<int64_t>(1, std::min<int64_t>((blocks + 7) / 8, 2 * CUS / units));
+        a->per_split = (blocks + want - 1) / want;
+        a->splits = (blocks + a->per_split - 1) / a->per_split;
     }
-    if (!a->paged || few)
-        return;
-    const int want = (int)std::max<int64_t>(1, std::min<int64_t>((blocks + 7) / 8, 512 / units));
-    a->per_split = (blocks + want - 1) / want;
-    a->splits = (blocks + a->per_split - 1) / a->per_split;
 }
 
 // What the workspace holds: outputs and states of the parts, and the spans.
@@ -1923,15 +1957,17 @@ template <typename TX, int D>
 void launch_mfma(const BatchAttnArgs &a, hipStream_t s) {
     const dim3 grid((unsigned)(a.chunks ? a.chunks * a.n_kv_heads : a.slots * a.n_kv_heads * a.splits)), block(256);
     if (a.tile == 16) {
-        if (a.chunks)
-            hipLaunchKernelGGL((k_batch_attn_few<TX, D, 1, true>), grid, block, 0, s, a);
+        if (a.waves == 8)
+            hipLaunchKernelGGL((k_batch_attn_few<TX, D, 1, 8, true>), grid, dim3(512), 0, s, a);
+        else if (a.chunks)
+            hipLaunchKernelGGL((k_batch_attn_few<TX, D, 1, NW, true>), grid, block, 0, s, a);
         else
-            hipLaunchKernelGGL((k_batch_attn_few<TX, D, 1, false>), grid, block, 0, s, a);
+            hipLaunchKernelGGL((k_batch_attn_few<TX, D, 1, NW, false>), grid, block, 0, s, a);
     } else if (a.tile == 32) {
         if (a.chunks)
-            hipLaunchKernelGGL((k_batch_attn_few<TX, D, 2, true>), grid, block, 0, s, a);
+            hipLaunchKernelGGL((k_batch_attn_few<TX, D, 2, NW, true>), grid, block, 0, s, a);
         else
-            hipLaunchKernelGGL((k_batch_attn_few<TX, D, 2, false>), grid, block, 0, s, a);
+            hipLaunchKernelGGL((k_batch_attn_few<TX, D, 2, NW, false>), grid, block, 0, s, a);
     } else if (a.tile == 64) {
         if (a.chunks)
             hipLaunchKernelGGL((k_batch_attn_mfma<TX, D, 2, 2, STREAM>), grid, block, 0, s, a);

@@ -12,6 +12,7 @@
 
 #include "host_api.h"
 #include "rope.h"
+#include "sd_internal.h"
 
 using namespace sdk;
 
@@ -114,9 +115,15 @@ __global__ __launch_bounds__(APPEND_THREADS) void k_paged_append(AppendArgs a) {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
                 sum = fmaf(p[j], p[j], fmaf(q[j], q[j], sum));
-            for (int o = 1; o < per; o <<= 1)
-                sum += __shfl_xor(sum, o, 64);
-            inv = 1.0f / sqrtf(sum / (float)D + a.eps);
+            // over the 2, 4, 8 or 16 lanes of the head
+            sum += dpp_mov<DPP_QUAD_XOR1>(sum);
+            if (per >= 4)
+                sum += dpp_mov<DPP_QUAD_XOR2>(sum);
+            if (per >= 8)
+                sum += dpp_mov<DPP_ROW_HALF_MIRROR>(sum);
+            if (per >= 16)
+                sum += dpp_mov<DPP_ROW_ROR8>(sum);
+            inv = rsqrtf(sum / (float)D + a.eps);
             if (key) {
                 np = np * inv * load4(norm + e0);
                 nq = nq * inv * load4(norm + e1);
