@@ -2006,7 +2006,7 @@ void launch_join_stream(const BatchAttnArgs &a, hipStream_t s) {
     const int rows = std::min(a.max_rows * a.G, a.tile);
     const dim3 grid((unsigned)(a.n_seqs * a.n_kv_heads * rows));
     // (parts of a sequence: one or two of many, or all of one)
-    if (a.chunks <= 4 * a.n_seqs)
+    if (a.chunks <= 8 * a.n_seqs)
         hipLaunchKernelGGL((k_batch_join_stream<TX, D, 64>), grid, dim3(64), 0, s, a, rows);
     else
         hipLaunchKernelGGL((k_batch_join_stream<TX, D, 256>), grid, dim3(256), 0, s, a, rows);
