@@ -1423,7 +1423,7 @@ __global__ __launch_bounds__(256, 2) void k_batch_attn_wide(BatchAttnArgs a) {
 template <typename TX, int D, int QT, int W, bool STREAMED>
 __global__ __launch_bounds__(64 * W, W == 8 ? 1 : QT == 1 || D < 128 ? 2 : 1) void k_batch_attn_few(BatchAttnArgs a) {
     constexpr bool EXACT = sizeof(TX) == 4;
-    constexpr int T = EXACT ? X_TERMS : 1, ES = D < 32 ? 1 : D / 32, ET = D / 16, ROWS = 16 * QT, OP = D + 4;
+    constexpr int T = EXACT ? X_TERMS : 1, TP = EXACT ? X_TERMS : 2, ES = D < 32 ? 1 : D / 32, ET = D / 16, ROWS = 16 * QT, OP = D + 4;
     using L = FewLines<D>;
     constexpr int VB = KB_FEW * D;  // elements of a V block
     constexpr int WORDS = VB > ROWS * OP ? VB : ROWS * OP;
@@ -1698,7 +1698,7 @@ __global__ __launch_bounds__(64 * W, W == 8 ? 1 : QT == 1 || D < 128 ? 2 : 1) vo
                     }
                 }
             }
-            u32x4_t pf[T];
+            u32x4_t pf[TP];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 if constexpr (EXACT) {
@@ -1709,6 +1709,8 @@ __global__ __launch_bounds__(64 * W, W == 8 ? 1 : QT == 1 || D < 128 ? 2 : 1) vo
                         pf[u][j] = t[u];
                 } else {
                     pf[0][j] = cvt_pk(p[2 * j], p[2 * j + 1]);
+                    pf[1][j] = cvt_pk(p[2 * j] - __uint_as_float(pf[0][j] << 16),
+                                      p[2 * j + 1] - __uint_as_float(pf[0][j] & 0xffff0000u));
                 }
             }
             // A operand V^T: column 16 et + col of keys 16 I + 4 grp + 0..3
@@ -1726,7 +1728,7 @@ __global__ __launch_bounds__(64 * W, W == 8 ? 1 : QT == 1 || D < 128 ? 2 : 1) vo
                     vf[2 * I + 1] = y[1];
                 }
 #pragma unroll
-                for (int u = 0; u < T; ++u)
+                for (int u = 0; u < TP; ++u)
                     o[i][et] = mfma16(vf, pf[u], o[i][et]);
             }
         }

@@ -595,3 +595,108 @@ def test_a_batch_does_not_change_its_neighbours_result():
     every = binding.paged_attention(q, c.k, c.v, binding.batch(gpu(c.table), gpu([300, 40, 77]), None, 1, 304))
     again = binding.paged_attention(q, c.k, c.v, binding.batch(gpu(c.table[[0, 2, 1]]), gpu([300, 0, 40]), None, 1, 304))
     assert torch.equal(every[0], again[0])
+
+
+# ----------------------------------------------------------------------------
+# tiles of 128 rows and streams: blocks in the middle of long contexts
+
+
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
+@pytest.mark.parametrize("page", [16, 32, 64])
+def test_paged_chunks_of_many_rows(x, d, page):
+    """Several tiles a sequence behind cached positions, ragged ends."""
+    check_paged([150, 1, 67], [700, 333, 67 + 590], 4, 2, d, x, "bf16", page)
+
+
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+def test_paged_bad_pages_inside_long_contexts(x, page):
+    """Pages missing in the middle and at the ends: of blocks that would be whole."""
+    def spoil(c):
+        for p in (0, 3, 5, 8):
+            if p < c.table.shape[1] - 2:
+                c.table[0, p] = (-1, c.n_pages, -2**31, 2**31 - 1)[p % 4]
+        c.table[1, 2] = c.n_pages
+
+    check_paged([140, 20, 1], [900, 620, 640], 4, 2, 64, x, "bf16", page, spoil=spoil)
+    check_paged([20, 20, 1], [900, 620, 640], 4, 2, 128, x, "bf16", page, spoil=spoil)
+
+
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [1, 20, 150])
+@pytest.mark.parametrize("at", [5, 200, 431])
+def test_paged_infinities_inside_long_contexts(x, rows, at):
+    """A value in a block that every row sees whole: infinite or NaN in its column for all of them, and nowhere else."""
+    rng = np.random.default_rng(77)
+    c = Cache(rng, [rows + 450], 1, 32, 64, "bf16")
+    q = torch.tensor(rng.standard_normal((rows, 2, 64)), dtype=TYPES[x], device="cuda")
+    batch = binding.batch(gpu(c.table), gpu([rows + 450]), None, rows)
+    want = binding.paged_attention(q, c.k, c.v, batch).clone()
+    c.v[int(c.table[0, at // 32]), :, at % 32, 9] = float("-inf")
+    got = binding.paged_attention(q, c.k, c.v, batch)
+    rest = [e for e in range(64) if e != 9]
+    assert torch.equal(got[..., rest], want[..., rest]) and not got[..., 9].isfinite().any()
+
+
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
+def test_prompt_steps_at_every_end(x, d):
+    """Tiles whose last block ends within the call's rows, and at them."""
+    for rows in ([161], [130, 31], [30, 192], [97, 95, 1]):
+        check_prompt(rows, 4, 1, d, x, "bf16")
+    check_prompt([400], 1, 1, d, x, "bf16", order="heads")
+
+
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+def test_prompt_large_enough_for_wide_tiles(x):
+    """More than 450 tiles of 128 rows, so that they are not cut to 64."""
+    rng = np.random.default_rng(6)
+    rows, heads, kvh, d = [370, 1, 130, 64, 300, 33], 64, 32, 64
+    starts, n = starts_of(rows), sum(rows)
+    kv = torch.tensor(rng.standard_normal((2, n, kvh, d)), dtype=torch.bfloat16, device="cuda")
+    q = torch.tensor(rng.standard_normal((n, heads, d)), dtype=TYPES[x], device="cuda")
+    got = binding.prompt_attention(q, kv[0].transpose(0, 1), kv[1].transpose(0, 1), gpu(starts))
+    q64, k64, v64 = (f64(t) for t in (q, kv[0], kv[1]))
+    for s, m in enumerate(rows):
+        for h in range(0, heads, 7):
+            a = slice(starts[s], starts[s] + m)
+            kk, vv, qq = k64[a, h // 2], v64[a, h // 2], q64[a, h]
+            z = np.where(np.tril(np.ones((m, m), bool)), qq @ kk.T / math.sqrt(d), -np.inf)
+            p = np.exp(z - z.max(axis=1, keepdims=True))
+            p /= p.sum(axis=1, keepdims=True)
+            want, spread = p @ vv, p @ np.abs(vv)
+            size = float((np.abs(qq) @ np.abs(kk).T).max() / math.sqrt(d))
+            tol = P.attention_tol(x, d, m, size, np.abs(vv).max(), want, spread)
+            assert (np.abs(f64(got[a, h]) - want) <= tol).all(), (s, h)
+
+
+@pytest.mark.parametrize("x,dtype", KINDS)
+@pytest.mark.parametrize("heads,kvh,rows", [(4, 1, 1), (8, 1, 4), (16, 2, 8), (16, 1, 8)])
+def test_streams_of_uneven_sequences(x, dtype, heads, kvh, rows):
+    """Chunks that hold several sequences, parts of one, and none: empty ones between, one much longer than the rest."""
+    rng = np.random.default_rng(14)
+    lengths = [0, 40, 3000, 0, 1, 130, 2047, 0, 64, 700, 129, 0]
+    m = [int(t) for t in rng.integers(0, rows + 1, len(lengths))]
+    m[2], m[5] = rows, 0
+    check_paged(m, lengths, heads, kvh, 32, x, dtype, 64)
+
+
+@pytest.mark.parametrize("n_seqs", [63, 64, 65, 257, 1024, 1025])
+def test_streams_of_many_sequences(n_seqs):
+    """As many as a work-group adds up the spans of, and more."""
+    rng = np.random.default_rng(n_seqs)
+    lengths = [int(t) for t in rng.integers(0, 40, n_seqs)]
+    lengths[n_seqs // 2] = 1500
+    check_paged([1] * n_seqs, lengths, 2, 1, 16, "f32", "bf16", 16)
+
+
+def test_streams_are_the_same_in_any_order():
+    """The whole result does not follow from where chunks are cut, but for the order of float32 sums."""
+    rng = np.random.default_rng(9)
+    lengths = [2500, 10, 900, 1700]
+    c = Cache(rng, lengths, 2, 16, 64, "bf16")
+    q = torch.tensor(rng.standard_normal((4, 8, 64)), dtype=torch.float32, device="cuda")
+    one = binding.paged_attention(q, c.k, c.v, binding.batch(gpu(c.table), gpu(lengths)))
+    back = binding.paged_attention(q.flip(0), c.k, c.v, binding.batch(gpu(c.table[::-1].copy()), gpu(lengths[::-1]))).flip(0)
+    assert (one - back).abs().max() <= 2.0 ** -20
