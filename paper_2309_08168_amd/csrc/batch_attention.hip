@@ -240,7 +240,8 @@ __global__ __launch_bounds__(NW * 64, 2) void k_batch_attn_f32(BatchAttnArgs a) 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, c = lane & 15,
               g4 = lane >> 4;
     const int g = blockIdx.x % a.n_kv_heads, split = blockIdx.y;
-    const Tile w = tile_of(a, blockIdx.x / a.n_kv_heads);
+    // (from the last tile, which has the most keys, to the first)
+    const Tile w = tile_of(a, a.slots - 1 - blockIdx.x / a.n_kv_heads);
     const int rows = w.rows.m * a.G;
     if (w.row0 >= rows)
         return;  // uniform
@@ -525,346 +526,346 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_batch_attn_mfma(BatchAttnAr
         off[i] = (uint32_t)(2 * ((int64_t)((s * L::RPL + p / L::C) & (one ? 63 : 15)) * a.row_stride + 8 * (p % L::C)));
     }
     for (;;) {
-    Tile w;
-    int b0, b1, part = 0;  // blocks of keys; the part of the result, or -1: all of it
-    int klen, kall, done = 0;
-    auto sees = [&](int rr) { return seen_from(w.rows.past + rr / a.G, a.max_length); };
-    if constexpr (FROM == STREAM) {
-        seq = __builtin_amdgcn_readfirstlane(seq);
-        w.seq = seq;
-        w.row0 = 0;
-        w.rows = rows_of(a, seq);
-    } else {
-        // (from the last tile, which has the most keys, to the first)
-        w = tile_of(a, a.slots - 1 - rest % a.slots);
-    }
-    const int rows = w.rows.m * a.G;
-    if (w.row0 >= rows)
-        return;  // uniform
-    klen = __builtin_amdgcn_readfirstlane(sees(min(w.row0 + 32 * NQ, rows) - 1));
-    kall = __builtin_amdgcn_readfirstlane(sees(w.row0));
-    if constexpr (FROM == STREAM) {
-        const int32_t from = at - stream.pre[seq], all = stream.pre[seq + 1] - stream.pre[seq];
-        done = min(all - from, end - at);
-        b0 = __builtin_amdgcn_readfirstlane(from);
-        b1 = __builtin_amdgcn_readfirstlane(from + done);
-        part = from == 0 && done == all ? -1 : 2 * (g * a.chunks + rest) + (from == 0);
-    } else if constexpr (FROM == PAGES) {
-        part = a.splits > 1 ? rest / a.slots : -1;
-        b0 = rest / a.slots * a.per_split;
-        b1 = b0 + a.per_split;
-    } else {
-        part = -1;
-        b0 = 0;
-        b1 = INT32_MAX;
-    }
-    b1 = min(b1, (klen + KB - 1) / KB);
-    if (FROM == PAGES && part >= 0 && b0 >= b1)
-        return;
-    const int r0 = w.row0 + wq * 32;
-    const bool live = r0 < rows;  // uniform over the wave: a wave without rows loads and waits with the others
-    const int row = min(r0 + col, rows - 1), node = row / a.G, head = g * a.G + row - node * a.G;
-    const int see = seen_from(w.rows.past + node, a.max_length);
-    auto load_block = [&](const Groups &k, int first, int buf) {
-        if (first + KB <= klen && near) {
-            const uint16_t *k0 = uniform(K + k.off[0]), *v0 = uniform(V + k.off[0]);
+        Tile w;
+        int b0, b1, part = 0;  // blocks of keys; the part of the result, or -1: all of it
+        int klen, kall, done = 0;
+        auto sees = [&](int rr) { return seen_from(w.rows.past + rr / a.G, a.max_length); };
+        if constexpr (FROM == STREAM) {
+            seq = __builtin_amdgcn_readfirstlane(seq);
+            w.seq = seq;
+            w.row0 = 0;
+            w.rows = rows_of(a, seq);
+        } else {
+            // (from the last tile, which has the most keys, to the first)
+            w = tile_of(a, a.slots - 1 - rest % a.slots);
+        }
+        const int rows = w.rows.m * a.G;
+        if (w.row0 >= rows)
+            return;  // uniform
+        klen = __builtin_amdgcn_readfirstlane(sees(min(w.row0 + 32 * NQ, rows) - 1));
+        kall = __builtin_amdgcn_readfirstlane(sees(w.row0));
+        if constexpr (FROM == STREAM) {
+            const int32_t from = at - stream.pre[seq], all = stream.pre[seq + 1] - stream.pre[seq];
+            done = min(all - from, end - at);
+            b0 = __builtin_amdgcn_readfirstlane(from);
+            b1 = __builtin_amdgcn_readfirstlane(from + done);
+            part = from == 0 && done == all ? -1 : 2 * (g * a.chunks + rest) + (from == 0);
+        } else if constexpr (FROM == PAGES) {
+            part = a.splits > 1 ? rest / a.slots : -1;
+            b0 = rest / a.slots * a.per_split;
+            b1 = b0 + a.per_split;
+        } else {
+            part = -1;
+            b0 = 0;
+            b1 = INT32_MAX;
+        }
+        b1 = min(b1, (klen + KB - 1) / KB);
+        if (FROM == PAGES && part >= 0 && b0 >= b1)
+            return;
+        const int r0 = w.row0 + wq * 32;
+        const bool live = r0 < rows;  // uniform over the wave: a wave without rows loads and waits with the others
+        const int row = min(r0 + col, rows - 1), node = row / a.G, head = g * a.G + row - node * a.G;
+        const int see = seen_from(w.rows.past + node, a.max_length);
+        auto load_block = [&](const Groups &k, int first, int buf) {
+            if (first + KB <= klen && near) {
+                const uint16_t *k0 = uniform(K + k.off[0]), *v0 = uniform(V + k.off[0]);
 #pragma unroll
-            for (int i = 0; i < NU; ++i) {
-                const int u = wave + WAVES * i;
-                if (L::C % WAVES == 0 || u < L::C) {  // uniform over the wave
-                    if (!one) {
-                        const int64_t o = row_at(k, false, ROWS * u / 16 * 16, a.row_stride);
-                        k0 = uniform(K + o);
-                        v0 = uniform(V + o);
+                for (int i = 0; i < NU; ++i) {
+                    const int u = wave + WAVES * i;
+                    if (L::C % WAVES == 0 || u < L::C) {  // uniform over the wave
+                        if (!one) {
+                            const int64_t o = row_at(k, false, ROWS * u / 16 * 16, a.row_stride);
+                            k0 = uniform(K + o);
+                            v0 = uniform(V + o);
+                        }
+                        load_to_lds16(k0, off[i], &kv[buf][0][u * 512]);
+                        load_to_lds16(v0, off[i], &kv[buf][1][u * 512]);
                     }
-                    load_to_lds16(k0, off[i], &kv[buf][0][u * 512]);
-                    load_to_lds16(v0, off[i], &kv[buf][1][u * 512]);
+                }
+            } else {
+#pragma unroll 1
+                for (int u = wave; u < L::C; u += WAVES) {
+                    const int s = 4 * u + (lane >> 4), p = (lane & 15) ^ L::swz(s);
+                    // rows past the last: that one
+                    const int64_t at = row_at(k, one, min(s * L::RPL + p / L::C, klen - 1 - first), a.row_stride) + 8 * (p % L::C);
+                    load_to_lds16(K + at, &kv[buf][0][u * 512]);
+                    load_to_lds16(V + at, &kv[buf][1][u * 512]);
                 }
             }
-        } else {
-#pragma unroll 1
-            for (int u = wave; u < L::C; u += WAVES) {
-                const int s = 4 * u + (lane >> 4), p = (lane & 15) ^ L::swz(s);
-                // rows past the last: that one
-                const int64_t at = row_at(k, one, min(s * L::RPL + p / L::C, klen - 1 - first), a.row_stride) + 8 * (p % L::C);
-                load_to_lds16(K + at, &kv[buf][0][u * 512]);
-                load_to_lds16(V + at, &kv[buf][1][u * 512]);
+        };
+        Entries entries = entries_of<PAGED>(a, w, KB * b0, klen);
+        // The queries are asked for before the first block: loads return in order.
+        const TX *qs = static_cast<const TX *>(a.q) + (int64_t)(w.rows.first + node) * a.ld_q + (int64_t)head * D + 8 * half;
+        u32x4_t qf[ES][T];
+        f32x4_t qx[EXACT ? ES : 1][2];
+#pragma unroll
+        for (int s = 0; s < ES; ++s) {
+            if constexpr (EXACT) {
+                qx[s][0] = load4(qs + 16 * s);
+                qx[s][1] = load4(qs + 16 * s + 4);
+            } else {
+                qf[s][0] = *reinterpret_cast<const u32x4_t *>(qs + 16 * s);
             }
         }
-    };
-    Entries entries = entries_of<PAGED>(a, w, KB * b0, klen);
-    // The queries are asked for before the first block: loads return in order.
-    const TX *qs = static_cast<const TX *>(a.q) + (int64_t)(w.rows.first + node) * a.ld_q + (int64_t)head * D + 8 * half;
-    u32x4_t qf[ES][T];
-    f32x4_t qx[EXACT ? ES : 1][2];
+        __builtin_amdgcn_sched_barrier(0);
+        Groups k = groups_of<PAGED>(a, w, entries, KB * b0, klen);
+        if (b0 < b1)
+            load_block(k, KB * b0, 0);
+        entries = entries_of<PAGED>(a, w, KB * (b0 + 1), klen);
+        // Rows past the last are zeros, which draw less power than copies of it.
+        const bool mine = r0 + col < rows;
 #pragma unroll
-    for (int s = 0; s < ES; ++s) {
-        if constexpr (EXACT) {
-            qx[s][0] = load4(qs + 16 * s);
-            qx[s][1] = load4(qs + 16 * s + 4);
-        } else {
-            qf[s][0] = *reinterpret_cast<const u32x4_t *>(qs + 16 * s);
-        }
-    }
-    __builtin_amdgcn_sched_barrier(0);
-    Groups k = groups_of<PAGED>(a, w, entries, KB * b0, klen);
-    if (b0 < b1)
-        load_block(k, KB * b0, 0);
-    entries = entries_of<PAGED>(a, w, KB * (b0 + 1), klen);
-    // Rows past the last are zeros, which draw less power than copies of it.
-    const bool mine = r0 + col < rows;
+        for (int s = 0; s < ES; ++s) {
+            if constexpr (EXACT) {
+                const float scale = mine ? a.scale : 0.0f;
+                query_terms(qx[s][0] * scale, qx[s][1] * scale, qf[s]);
+            } else {
+                // (a negative scale as one of q, so that the largest score stays the largest)
 #pragma unroll
-    for (int s = 0; s < ES; ++s) {
-        if constexpr (EXACT) {
-            const float scale = mine ? a.scale : 0.0f;
-            query_terms(qx[s][0] * scale, qx[s][1] * scale, qf[s]);
-        } else {
-            // (a negative scale as one of q, so that the largest score stays the largest)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                qf[s][0][j] = mine ? qf[s][0][j] ^ (a.scale < 0.0f ? 0x80008000u : 0u) : 0u;
-        }
-    }
-    // (a scale that float32 products would take for zero would make NaN of a masked score)
-    const float factor = EXACT ? 1.0f : fmaxf(fabsf(a.scale), 1.17549435e-38f);
-    // V^T reads: ds_read_b64_tr_b16 hands lane l of each 16-lane group element
-    // l % 4 of the 8 bytes that lanes l / 4 + 4 k (k = 0..3) point at, so lane l
-    // points at row 4 half + l / 4 % 4, columns 16 (l / 16 % 2) + 4 (l % 4) ...
-    // (head_dim 16: columns past it repeat the first, in output rows that
-    // nothing reads)
-    const int v_lane = 2 * (KB * D + L::at(4 * half + ((lane >> 2) & 3), (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) % L::C) +
-                            4 * (lane & 1));
-    const char *lds = reinterpret_cast<const char *>(kv);
-    float m_run = -INFINITY, l_run = 0.0f;
-    f32x16_t o[ET];
-#pragma unroll
-    for (int et = 0; et < ET; ++et)
-#pragma unroll
-        for (int v = 0; v < 16; ++v)
-            o[et][v] = 0.0f;
-
-    int buf = 0;
-    for (int b = b0; b < b1; ++b, buf ^= 1) {
-        const int first = KB * b;
-        const Groups now = k;
-        // this wave's loads of the block have landed, then everyone's; every
-        // read of the other buffer has returned
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (b + 1 < b1) {
-            k = groups_of<PAGED>(a, w, entries, first + KB, klen);
-            load_block(k, first + KB, buf ^ 1);
-            entries = entries_of<PAGED>(a, w, first + 2 * KB, klen);
-        }
-        const bool full = first + KB <= kall && now.ok == 15;  // every row sees every key
-        bool odd = false;
-        if (!full) {
-            // A row must not add 0 times an infinity or NaN of a value that it
-            // does not see: they are taken out here, and put where they belong
-            // beside the products.
-            uint16_t *vs = kv[buf][1];
-            for (int c = threadIdx.x; c < KB * D / 8; c += 64 * WAVES) {
-                u32x4_t x = reinterpret_cast<const u32x4_t *>(vs)[c];
-                bool hit = false;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t y = without_odd(x[j]);
-                    hit |= y != x[j];
-                    x[j] = y;
-                }
-                if (hit)
-                    reinterpret_cast<u32x4_t *>(vs)[c] = x;
-                odd |= hit;
+                for (int j = 0; j < 4; ++j)
+                    qf[s][0][j] = mine ? qf[s][0][j] ^ (a.scale < 0.0f ? 0x80008000u : 0u) : 0u;
             }
-            odd = __syncthreads_or(odd);
         }
-        const uint64_t visible = full ? ~0ull : seen_bits(see - first, now.ok);
-#pragma unroll 1
-        for (int h = wk; h < 2; h += NK) {
-            const uint32_t bits = h ? (uint32_t)(visible >> 32) : (uint32_t)visible;
-            if (!live || (!full && !__any(bits != 0)))
-                continue;  // uniform over the wave: no row of it sees these keys
-            f32x16_t s;
+        // (a scale that float32 products would take for zero would make NaN of a masked score)
+        const float factor = EXACT ? 1.0f : fmaxf(fabsf(a.scale), 1.17549435e-38f);
+        // V^T reads: ds_read_b64_tr_b16 hands lane l of each 16-lane group element
+        // l % 4 of the 8 bytes that lanes l / 4 + 4 k (k = 0..3) point at, so lane l
+        // points at row 4 half + l / 4 % 4, columns 16 (l / 16 % 2) + 4 (l % 4) ...
+        // (head_dim 16: columns past it repeat the first, in output rows that
+        // nothing reads)
+        const int v_lane = 2 * (KB * D + L::at(4 * half + ((lane >> 2) & 3), (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) % L::C) +
+                                4 * (lane & 1));
+        const char *lds = reinterpret_cast<const char *>(kv);
+        float m_run = -INFINITY, l_run = 0.0f;
+        f32x16_t o[ET];
+#pragma unroll
+        for (int et = 0; et < ET; ++et)
 #pragma unroll
             for (int v = 0; v < 16; ++v)
-                s[v] = 0.0f;
-            // byte addresses in LDS: rows 32 h + col, chunk 2 e + half at xk ^ 32 e.
-            // (Hidden from the compiler, which would keep every address of the
-            // loop in a register and spill.)
-            int xk = 2 * (buf * 2 * KB * D + 32 * h * D + L::at(col, half)), xv = 2 * (buf * 2 * KB * D + 32 * h * D) + v_lane;
-            asm volatile("" : "+v"(xk), "+v"(xv));
-            __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-            for (int e = 0; e < ES; ++e) {
-                const u32x4_t kf = *reinterpret_cast<const u32x4_t *>(lds + (xk ^ (32 * e)));
-#pragma unroll
-                for (int i = 0; i < T; ++i)
-                    s = mfma32(kf, qf[e][i], s);
+                o[et][v] = 0.0f;
+
+        int buf = 0;
+        for (int b = b0; b < b1; ++b, buf ^= 1) {
+            const int first = KB * b;
+            const Groups now = k;
+            // this wave's loads of the block have landed, then everyone's; every
+            // read of the other buffer has returned
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            if (b + 1 < b1) {
+                k = groups_of<PAGED>(a, w, entries, first + KB, klen);
+                load_block(k, first + KB, buf ^ 1);
+                entries = entries_of<PAGED>(a, w, first + 2 * KB, klen);
             }
-            __builtin_amdgcn_s_setprio(0);
+            const bool full = first + KB <= kall && now.ok == 15;  // every row sees every key
+            bool odd = false;
             if (!full) {
-                uint32_t own = bits >> (4 * half);
-                asm volatile("" : "+v"(own));  // (a branch, and not selects in every block)
+                // A row must not add 0 times an infinity or NaN of a value that it
+                // does not see: they are taken out here, and put where they belong
+                // beside the products.
+                uint16_t *vs = kv[buf][1];
+                for (int c = threadIdx.x; c < KB * D / 8; c += 64 * WAVES) {
+                    u32x4_t x = reinterpret_cast<const u32x4_t *>(vs)[c];
+                    bool hit = false;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t y = without_odd(x[j]);
+                        hit |= y != x[j];
+                        x[j] = y;
+                    }
+                    if (hit)
+                        reinterpret_cast<u32x4_t *>(vs)[c] = x;
+                    odd |= hit;
+                }
+                odd = __syncthreads_or(odd);
+            }
+            const uint64_t visible = full ? ~0ull : seen_bits(see - first, now.ok);
+#pragma unroll 1
+            for (int h = wk; h < 2; h += NK) {
+                const uint32_t bits = h ? (uint32_t)(visible >> 32) : (uint32_t)visible;
+                if (!live || (!full && !__any(bits != 0)))
+                    continue;  // uniform over the wave: no row of it sees these keys
+                f32x16_t s;
 #pragma unroll
                 for (int v = 0; v < 16; ++v)
-                    s[v] = (own >> (8 * (v >> 2) + (v & 3))) & 1 ? s[v] : -INFINITY;
-            }
-            float mx = s[0];
+                    s[v] = 0.0f;
+                // byte addresses in LDS: rows 32 h + col, chunk 2 e + half at xk ^ 32 e.
+                // (Hidden from the compiler, which would keep every address of the
+                // loop in a register and spill.)
+                int xk = 2 * (buf * 2 * KB * D + 32 * h * D + L::at(col, half)), xv = 2 * (buf * 2 * KB * D + 32 * h * D) + v_lane;
+                asm volatile("" : "+v"(xk), "+v"(xv));
+                __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-            for (int v = 1; v < 16; ++v)
-                mx = fmaxf(mx, s[v]);
-            {
-                const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-                mx = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-            }
-            if constexpr (!EXACT)
-                mx *= factor;
-            const bool grows = mx > m_run + SLACK;
-            if (__any(grows)) {
-                // (a row that has seen no key yet keeps zeros)
-                const float m_new = grows ? mx : m_run;
-                const float sc = m_run == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run - m_new);
-                l_run *= sc;
-#pragma unroll
-                for (int et = 0; et < ET; ++et)
-                    o[et] *= sc;
-                m_run = m_new;
-            }
-            const float m_use = m_run == -INFINITY ? 0.0f : m_run;
-            // (the running sum is rounded once for the 16 weights)
-            float p[16], sum = 0.0f;
-#pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                p[v] = __builtin_amdgcn_exp2f(EXACT ? s[v] - m_use : fmaf(s[v], factor, -m_use));
-                sum += p[v];
-            }
-            l_run += sum;
-            if (odd) {
-                // what was taken out, from memory: lane (col, half) holds
-                // elements 32 et + 8 (v / 4) + 4 half + v % 4 of row col
-#pragma unroll 1
-                for (int key = 0; key < 32; ++key) {
-                    float pk = 0.0f;
-                    const int own = 4 * (key >> 3) + (key & 3);
-#pragma unroll
-                    for (int v = 0; v < 16; ++v)
-                        pk = v == own ? p[v] : pk;
-                    pk = __shfl(pk, col + 32 * ((key >> 2) & 1), 64);
-                    const uint16_t *vr = V + row_at(now, one, min(32 * h + key, klen - 1 - first), a.row_stride);
-#pragma unroll
-                    for (int et = 0; et < ET; ++et)
-#pragma unroll
-                        for (int v = 0; v < 16; ++v) {
-                            const int e = 32 * et + 8 * (v >> 2) + 4 * half + (v & 3);
-                            const float x = e < D ? load1(vr + e) : 0.0f;
-                            if (pk != 0.0f && !finite(x))
-                                o[et][v] = fmaf(pk, x, o[et][v]);
-                        }
-                }
-            }
-            __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                u32x4_t pf[T];
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    if constexpr (EXACT) {
-                        uint32_t t[T];
-                        terms2(p[8 * j + 2 * u], p[8 * j + 2 * u + 1], t);
-#pragma unroll
-                        for (int i = 0; i < T; ++i)
-                            pf[i][u] = t[i];
-                    } else {
-                        pf[0][u] = cvt_pk(p[8 * j + 2 * u], p[8 * j + 2 * u + 1]);
-                    }
-                }
-                // A operand V^T: column 32 et + col of keys 16 j + 8 I + 4 half +
-                // 0..3, the row's chunks of et and I one exclusive or away
-#pragma unroll
-                for (int et = 0; et < ET; ++et) {
-                    u32x4_t vf;
-#pragma unroll
-                    for (int I = 0; I < 2; ++I) {
-                        const char *src = lds + (xv ^ (64 * et) ^ (I ? (D == 16 ? 16 : 32) : 0)) + 2 * (16 * j + 8 * I) * D;
-                        const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)src);
-                        const u32x2_t y = __builtin_bit_cast(u32x2_t, x);
-                        vf[2 * I] = y[0];
-                        vf[2 * I + 1] = y[1];
-                    }
+                for (int e = 0; e < ES; ++e) {
+                    const u32x4_t kf = *reinterpret_cast<const u32x4_t *>(lds + (xk ^ (32 * e)));
 #pragma unroll
                     for (int i = 0; i < T; ++i)
-                        o[et] = mfma32(vf, pf[i], o[et]);
+                        s = mfma32(kf, qf[e][i], s);
                 }
+                __builtin_amdgcn_s_setprio(0);
+                if (!full) {
+                    uint32_t own = bits >> (4 * half);
+                    asm volatile("" : "+v"(own));  // (a branch, and not selects in every block)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v)
+                        s[v] = (own >> (8 * (v >> 2) + (v & 3))) & 1 ? s[v] : -INFINITY;
+                }
+                float mx = s[0];
+#pragma unroll
+                for (int v = 1; v < 16; ++v)
+                    mx = fmaxf(mx, s[v]);
+                {
+                    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+                    mx = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+                }
+                if constexpr (!EXACT)
+                    mx *= factor;
+                const bool grows = mx > m_run + SLACK;
+                if (__any(grows)) {
+                    // (a row that has seen no key yet keeps zeros)
+                    const float m_new = grows ? mx : m_run;
+                    const float sc = m_run == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run - m_new);
+                    l_run *= sc;
+#pragma unroll
+                    for (int et = 0; et < ET; ++et)
+                        o[et] *= sc;
+                    m_run = m_new;
+                }
+                const float m_use = m_run == -INFINITY ? 0.0f : m_run;
+                // (the running sum is rounded once for the 16 weights)
+                float p[16], sum = 0.0f;
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    p[v] = __builtin_amdgcn_exp2f(EXACT ? s[v] - m_use : fmaf(s[v], factor, -m_use));
+                    sum += p[v];
+                }
+                l_run += sum;
+                if (odd) {
+                    // what was taken out, from memory: lane (col, half) holds
+                    // elements 32 et + 8 (v / 4) + 4 half + v % 4 of row col
+#pragma unroll 1
+                    for (int key = 0; key < 32; ++key) {
+                        float pk = 0.0f;
+                        const int own = 4 * (key >> 3) + (key & 3);
+#pragma unroll
+                        for (int v = 0; v < 16; ++v)
+                            pk = v == own ? p[v] : pk;
+                        pk = __shfl(pk, col + 32 * ((key >> 2) & 1), 64);
+                        const uint16_t *vr = V + row_at(now, one, min(32 * h + key, klen - 1 - first), a.row_stride);
+#pragma unroll
+                        for (int et = 0; et < ET; ++et)
+#pragma unroll
+                            for (int v = 0; v < 16; ++v) {
+                                const int e = 32 * et + 8 * (v >> 2) + 4 * half + (v & 3);
+                                const float x = e < D ? load1(vr + e) : 0.0f;
+                                if (pk != 0.0f && !finite(x))
+                                    o[et][v] = fmaf(pk, x, o[et][v]);
+                            }
+                    }
+                }
+                __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    u32x4_t pf[T];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        if constexpr (EXACT) {
+                            uint32_t t[T];
+                            terms2(p[8 * j + 2 * u], p[8 * j + 2 * u + 1], t);
+#pragma unroll
+                            for (int i = 0; i < T; ++i)
+                                pf[i][u] = t[i];
+                        } else {
+                            pf[0][u] = cvt_pk(p[8 * j + 2 * u], p[8 * j + 2 * u + 1]);
+                        }
+                    }
+                    // A operand V^T: column 32 et + col of keys 16 j + 8 I + 4 half +
+                    // 0..3, the row's chunks of et and I one exclusive or away
+#pragma unroll
+                    for (int et = 0; et < ET; ++et) {
+                        u32x4_t vf;
+#pragma unroll
+                        for (int I = 0; I < 2; ++I) {
+                            const char *src = lds + (xv ^ (64 * et) ^ (I ? (D == 16 ? 16 : 32) : 0)) + 2 * (16 * j + 8 * I) * D;
+                            const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)src);
+                            const u32x2_t y = __builtin_bit_cast(u32x2_t, x);
+                            vf[2 * I] = y[0];
+                            vf[2 * I + 1] = y[1];
+                        }
+#pragma unroll
+                        for (int i = 0; i < T; ++i)
+                            o[et] = mfma32(vf, pf[i], o[et]);
+                    }
+                }
+                __builtin_amdgcn_s_setprio(0);
             }
-            __builtin_amdgcn_s_setprio(0);
         }
-    }
-    {
-        const auto lr = __builtin_amdgcn_permlane32_swap(__float_as_uint(l_run), __float_as_uint(l_run), false, false);
-        l_run = __uint_as_float(lr[0]) + __uint_as_float(lr[1]);
-    }
-    if constexpr (NK == 2) {
-        // the second half of the keys joins the first: its states through LDS,
-        // 16 ET + 2 words a lane
-        static_assert(sizeof(kv) >= NQ * 64 * (16 * ET + 2) * 4 || D < 128, "LDS for the states");
-        __shared__ float st[D == 128 ? 1 : NQ * 64 * (16 * ET + 2)];
-        float *to = D == 128 ? reinterpret_cast<float *>(kv) : st;
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (wk == 1) {
+        {
+            const auto lr = __builtin_amdgcn_permlane32_swap(__float_as_uint(l_run), __float_as_uint(l_run), false, false);
+            l_run = __uint_as_float(lr[0]) + __uint_as_float(lr[1]);
+        }
+        if constexpr (NK == 2) {
+            // the second half of the keys joins the first: its states through LDS,
+            // 16 ET + 2 words a lane
+            static_assert(sizeof(kv) >= NQ * 64 * (16 * ET + 2) * 4 || D < 128, "LDS for the states");
+            __shared__ float st[D == 128 ? 1 : NQ * 64 * (16 * ET + 2)];
+            float *to = D == 128 ? reinterpret_cast<float *>(kv) : st;
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            if (wk == 1) {
+#pragma unroll
+                for (int et = 0; et < ET; ++et)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v)
+                        to[((16 * et + v) * NQ + wq) * 64 + lane] = o[et][v];
+                to[(16 * ET * NQ + wq) * 64 + lane] = m_run;
+                to[((16 * ET + 1) * NQ + wq) * 64 + lane] = l_run;
+            }
+            __syncthreads();
+            if (wk == 0) {
+            const float m2 = to[(16 * ET * NQ + wq) * 64 + lane], l2 = to[((16 * ET + 1) * NQ + wq) * 64 + lane];
+            const float m = fmaxf(m_run, m2), mu = m == -INFINITY ? 0.0f : m;
+            const float w1 = __builtin_amdgcn_exp2f(m_run - mu), w2 = __builtin_amdgcn_exp2f(m2 - mu);
+            m_run = m;
+            l_run = l_run * w1 + l2 * w2;
 #pragma unroll
             for (int et = 0; et < ET; ++et)
 #pragma unroll
                 for (int v = 0; v < 16; ++v)
-                    to[((16 * et + v) * NQ + wq) * 64 + lane] = o[et][v];
-            to[(16 * ET * NQ + wq) * 64 + lane] = m_run;
-            to[((16 * ET + 1) * NQ + wq) * 64 + lane] = l_run;
-        }
-        __syncthreads();
-        if (wk == 0) {
-        const float m2 = to[(16 * ET * NQ + wq) * 64 + lane], l2 = to[((16 * ET + 1) * NQ + wq) * 64 + lane];
-        const float m = fmaxf(m_run, m2), mu = m == -INFINITY ? 0.0f : m;
-        const float w1 = __builtin_amdgcn_exp2f(m_run - mu), w2 = __builtin_amdgcn_exp2f(m2 - mu);
-        m_run = m;
-        l_run = l_run * w1 + l2 * w2;
-#pragma unroll
-        for (int et = 0; et < ET; ++et)
-#pragma unroll
-            for (int v = 0; v < 16; ++v)
-                o[et][v] = o[et][v] * w1 + to[((16 * et + v) * NQ + wq) * 64 + lane] * w2;
-        }
-    }
-    if (mine && wk == 0) {
-        const int64_t packed = w.rows.first + node;
-        const int64_t slot = FROM == STREAM ? (int64_t)part * a.tile + 32 * wq + col : ((int64_t)part * a.n + packed) * a.n_heads + head;
-        TX *out = static_cast<TX *>(a.out) + packed * a.ld_out + (int64_t)head * D;
-        const float inv = part >= 0 ? 1.0f : l_run == 0.0f ? 0.0f : 1.0f / l_run;
-#pragma unroll
-        for (int et = 0; et < ET; ++et)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int e = 32 * et + 8 * q + 4 * half;
-                const f32x4_t y = f32x4_t{o[et][4 * q], o[et][4 * q + 1], o[et][4 * q + 2], o[et][4 * q + 3]} * inv;
-                if (e < D) {
-                    if (part < 0)
-                        store4(out + e, y);
-                    else
-                        store4(a.part_o + slot * D + e, y);
-                }
+                    o[et][v] = o[et][v] * w1 + to[((16 * et + v) * NQ + wq) * 64 + lane] * w2;
             }
-        if (part >= 0 && half == 0)
-            a.part_ml[slot] = make_float2(m_run, l_run);
-    }
-    if constexpr (FROM != STREAM) {
-        return;
-    } else {
-        at += done;
-        if (at >= end)
+        }
+        if (mine && wk == 0) {
+            const int64_t packed = w.rows.first + node;
+            const int64_t slot = FROM == STREAM ? (int64_t)part * a.tile + 32 * wq + col : ((int64_t)part * a.n + packed) * a.n_heads + head;
+            TX *out = static_cast<TX *>(a.out) + packed * a.ld_out + (int64_t)head * D;
+            const float inv = part >= 0 ? 1.0f : l_run == 0.0f ? 0.0f : 1.0f / l_run;
+#pragma unroll
+            for (int et = 0; et < ET; ++et)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int e = 32 * et + 8 * q + 4 * half;
+                    const f32x4_t y = f32x4_t{o[et][4 * q], o[et][4 * q + 1], o[et][4 * q + 2], o[et][4 * q + 3]} * inv;
+                    if (e < D) {
+                        if (part < 0)
+                            store4(out + e, y);
+                        else
+                            store4(a.part_o + slot * D + e, y);
+                    }
+                }
+            if (part >= 0 && half == 0)
+                a.part_ml[slot] = make_float2(m_run, l_run);
+        }
+        if constexpr (FROM != STREAM) {
             return;
-        // the next sequence that has spans
-        do
-            ++seq;
-        while (stream.pre[seq + 1] <= at);
-        __syncthreads();
-    }
+        } else {
+            at += done;
+            if (at >= end)
+                return;
+            // the next sequence that has spans
+            do
+                ++seq;
+            while (stream.pre[seq + 1] <= at);
+            __syncthreads();
+        }
     }
 }
 
@@ -1442,328 +1443,328 @@ __global__ __launch_bounds__(64 * W, W == 8 ? 1 : QT == 1 || D < 128 ? 2 : 1) vo
             return;  // uniform
     }
     for (;;) {
-    seq = __builtin_amdgcn_readfirstlane(seq);
-    int32_t from = 0, to = 0, all = 0;  // spans
-    if constexpr (STREAMED) {
-        from = __builtin_amdgcn_readfirstlane(at - stream.pre[seq]);
-        all = __builtin_amdgcn_readfirstlane(stream.pre[seq + 1] - stream.pre[seq]);
-        to = min(all, from + end - at);
-    }
-    constexpr int BLOCKS = W;  // of a span
-    const int b0 = BLOCKS * from + wave;
-    // the entries of this wave's blocks b .., of groups past the table none
-    const int32_t *table = a.table + (int64_t)seq * a.ld_table;
-    auto entries_from = [&](int b) {
-        const int64_t first = KB_FEW * ((int64_t)b + W * (lane >> 1)) + 16 * (lane & 1);
-        return first < a.max_length ? table[first >> a.page_shift] : -1;
-    };
-    int entries = entries_from(b0);
-    Tile w;
-    w.seq = seq;
-    w.row0 = 0;
-    w.rows = rows_of(a, seq);
-    const int rows = w.rows.m * a.G;
-    if (rows == 0)
-        return;  // uniform (no sequence of a stream's)
-    const int klen = __builtin_amdgcn_readfirstlane(seen_from(w.rows.past + w.rows.m - 1, a.max_length));
-    const int kall = __builtin_amdgcn_readfirstlane(seen_from(w.rows.past, a.max_length));
-    const int blocks = (klen + KB_FEW - 1) / KB_FEW, b1 = STREAMED ? min(BLOCKS * to, blocks) : blocks;
-    const uint16_t *K = static_cast<const uint16_t *>(a.k) + (int64_t)g * a.head_stride;
-    const uint16_t *V = static_cast<const uint16_t *>(a.v) + (int64_t)g * a.head_stride;
-    uint16_t *vt = reinterpret_cast<uint16_t *>(tile[wave]);
+        seq = __builtin_amdgcn_readfirstlane(seq);
+        int32_t from = 0, to = 0, all = 0;  // spans
+        if constexpr (STREAMED) {
+            from = __builtin_amdgcn_readfirstlane(at - stream.pre[seq]);
+            all = __builtin_amdgcn_readfirstlane(stream.pre[seq + 1] - stream.pre[seq]);
+            to = min(all, from + end - at);
+        }
+        constexpr int BLOCKS = W;  // of a span
+        const int b0 = BLOCKS * from + wave;
+        // the entries of this wave's blocks b .., of groups past the table none
+        const int32_t *table = a.table + (int64_t)seq * a.ld_table;
+        auto entries_from = [&](int b) {
+            const int64_t first = KB_FEW * ((int64_t)b + W * (lane >> 1)) + 16 * (lane & 1);
+            return first < a.max_length ? table[first >> a.page_shift] : -1;
+        };
+        int entries = entries_from(b0);
+        Tile w;
+        w.seq = seq;
+        w.row0 = 0;
+        w.rows = rows_of(a, seq);
+        const int rows = w.rows.m * a.G;
+        if (rows == 0)
+            return;  // uniform (no sequence of a stream's)
+        const int klen = __builtin_amdgcn_readfirstlane(seen_from(w.rows.past + w.rows.m - 1, a.max_length));
+        const int kall = __builtin_amdgcn_readfirstlane(seen_from(w.rows.past, a.max_length));
+        const int blocks = (klen + KB_FEW - 1) / KB_FEW, b1 = STREAMED ? min(BLOCKS * to, blocks) : blocks;
+        const uint16_t *K = static_cast<const uint16_t *>(a.k) + (int64_t)g * a.head_stride;
+        const uint16_t *V = static_cast<const uint16_t *>(a.v) + (int64_t)g * a.head_stride;
+        uint16_t *vt = reinterpret_cast<uint16_t *>(tile[wave]);
 
-    // Where the halves of a block start (elements), and whether they have a page.
-    struct Halves {
-        int64_t off[2];
-        int ok;
-    };
-    auto halves_of = [&](int b, int slot) {  // slot: among the entries
-        Halves h;
-        h.ok = 0;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            // (without a page: any rows, which are masked, and taken for finite)
-            const int page = __builtin_amdgcn_readlane(entries, 2 * slot + t);
-            const bool there = (uint32_t)page < (uint32_t)a.n_pages;
-            h.off[t] = (there ? page * a.page_stride : 0) +
-                       (int64_t)((KB_FEW * b + 16 * t) & ((1 << a.page_shift) - 1)) * a.row_stride;
-            h.ok |= there ? 1 << t : 0;
-        }
-        return h;
-    };
-    // Whole blocks: lane offsets that do not change, from a half's first row.
-    // (Of V's loads u, only the lane's place in odd and even ones differs.)
-    const bool near = D > 16 && near_rows(a.row_stride);
-    const uint32_t koff = (uint32_t)(2 * ((int64_t)col * a.row_stride + (8 * grp) % D));
-    uint32_t voff[2];
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-        const int s = 4 * u + (lane >> 4), p = (lane & 15) ^ L::swz(s);
-        voff[u] = (uint32_t)(2 * ((int64_t)((lane >> 4) * L::RPL + p / L::C) * a.row_stride + 8 * (p % L::C)));
-    }
-    u32x4_t kf[2][ES];
-    auto load_k = [&](const Halves &h, int first) {
-        const bool whole = first + KB_FEW <= klen && near;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            // keys past the last: that one, masked; head_dim 16: the upper slots are zeros of q
-            const int r = min(16 * t + col, klen - 1 - first);
-            const char *kp = whole ? reinterpret_cast<const char *>(K + h.off[t]) + koff
-                                   : reinterpret_cast<const char *>(K + (r < 16 ? h.off[0] : h.off[1]) +
-                                                                    (r & 15) * a.row_stride + (8 * grp) % D);
-#pragma unroll
-            for (int s = 0; s < ES; ++s)
-                kf[t][s] = *reinterpret_cast<const u32x4_t *>(kp + 64 * s);
-        }
-    };
-    auto load_v = [&](const Halves &h, int first, int buf) {
-        constexpr int LOAD_ROWS = 4 * L::RPL;
-        if (first + KB_FEW <= klen && near) {
-#pragma unroll
-            for (int u = 0; u < VB / 512; ++u)
-                load_to_lds16(V + h.off[LOAD_ROWS * u / 16] + (int64_t)(LOAD_ROWS * u % 16) * a.row_stride, voff[u & 1],
-                              vt + buf * VB + u * 512);
-        } else {
-#pragma unroll 1
-            for (int u = 0; u < VB / 512; ++u) {
-                const int s = 4 * u + (lane >> 4), p = (lane & 15) ^ L::swz(s);
-                const int r = min(s * L::RPL + p / L::C, klen - 1 - first);
-                load_to_lds16(V + (r < 16 ? h.off[0] : h.off[1]) + (r & 15) * a.row_stride + 8 * (p % L::C),
-                              vt + buf * VB + u * 512);
-            }
-        }
-    };
-    Halves k{};
-    int b = b0, slot = 0;
-    if (b < b1) {
-        k = halves_of(b, 0);
-        load_k(k, KB_FEW * b);
-        load_v(k, KB_FEW * b, 0);
-    }
-    int see[QT];
-    u32x4_t qf[QT][ES][T];
-#pragma unroll
-    for (int i = 0; i < QT; ++i) {
-        const int row = min(16 * i + col, rows - 1), node = row / a.G;
-        see[i] = seen_from(w.rows.past + node, a.max_length);
-        const TX *qs = static_cast<const TX *>(a.q) + (int64_t)(w.rows.first + node) * a.ld_q +
-                       (int64_t)(g * a.G + row - node * a.G) * D + (8 * grp) % D;
-        const bool none = (D < 32 && grp >= 2) || 16 * i + col >= rows;  // head_dim 16: the upper half of the reduction
-#pragma unroll
-        for (int s = 0; s < ES; ++s) {
-            if constexpr (EXACT) {
-                const float scale = a.scale;
-                f32x4_t x0 = load4(qs + 32 * s) * scale, x1 = load4(qs + 32 * s + 4) * scale;
-                if (none)
-                    x0 = x1 = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-                query_terms(x0, x1, qf[i][s]);
-            } else {
-                // (a negative scale as one of q, so that the largest score stays the largest)
-                const u32x4_t x = *reinterpret_cast<const u32x4_t *>(qs + 32 * s);
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    qf[i][s][0][j] = none ? 0u : x[j] ^ (a.scale < 0.0f ? 0x80008000u : 0u);
-            }
-        }
-    }
-    // (a scale that float32 products would take for zero would make NaN of a masked score)
-    const float factor = EXACT ? 1.0f : fmaxf(fabsf(a.scale), 1.17549435e-38f);
-    float m_run[QT], l_run[QT];
-    f32x4_t o[QT][ET];
-#pragma unroll
-    for (int i = 0; i < QT; ++i) {
-        m_run[i] = -INFINITY;
-        l_run[i] = 0.0f;
-#pragma unroll
-        for (int et = 0; et < ET; ++et)
-            o[i][et] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    }
-    const int v_lane = 2 * L::at(4 * grp + (col >> 2), (col & 3) >> 1) + 8 * (col & 1);
-    const char *vb = reinterpret_cast<const char *>(vt);
-
-    int buf = 0;
-    for (; b < b1; b += W, buf ^= 1) {
-        const int first = KB_FEW * b;
-        const Halves now = k;
-        f32x4_t s[QT][2];
-#pragma unroll
-        for (int i = 0; i < QT; ++i)
+        // Where the halves of a block start (elements), and whether they have a page.
+        struct Halves {
+            int64_t off[2];
+            int ok;
+        };
+        auto halves_of = [&](int b, int slot) {  // slot: among the entries
+            Halves h;
+            h.ok = 0;
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                s[i][t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int e = 0; e < ES; ++e)
-#pragma unroll
-                    for (int u = 0; u < T; ++u)
-                        s[i][t] = mfma16(kf[t][e], qf[i][e][u], s[i][t]);
+                // (without a page: any rows, which are masked, and taken for finite)
+                const int page = __builtin_amdgcn_readlane(entries, 2 * slot + t);
+                const bool there = (uint32_t)page < (uint32_t)a.n_pages;
+                h.off[t] = (there ? page * a.page_stride : 0) +
+                           (int64_t)((KB_FEW * b + 16 * t) & ((1 << a.page_shift) - 1)) * a.row_stride;
+                h.ok |= there ? 1 << t : 0;
             }
-        // this block's V has landed (it was asked for before this block's K, or
-        // just after), then the next block's loads
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        if (b + W < b1) {
-            if (++slot == 32) {
-                slot = 0;
-                entries = entries_from(b + W);
-            }
-            k = halves_of(b + W, slot);
-            load_v(k, first + W * KB_FEW, buf ^ 1);
-            load_k(k, first + W * KB_FEW);
+            return h;
+        };
+        // Whole blocks: lane offsets that do not change, from a half's first row.
+        // (Of V's loads u, only the lane's place in odd and even ones differs.)
+        const bool near = D > 16 && near_rows(a.row_stride);
+        const uint32_t koff = (uint32_t)(2 * ((int64_t)col * a.row_stride + (8 * grp) % D));
+        uint32_t voff[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int s = 4 * u + (lane >> 4), p = (lane & 15) ^ L::swz(s);
+            voff[u] = (uint32_t)(2 * ((int64_t)((lane >> 4) * L::RPL + p / L::C) * a.row_stride + 8 * (p % L::C)));
         }
-        const bool full = first + KB_FEW <= kall && now.ok == 3;  // every row sees every key
-        // Infinities and NaN among values that some row does not see: it must not
-        // add 0 times one.  They are taken out here, and put where they belong
-        // beside the products.
-        bool odd = false;
-        if (!full) {
-            u32x4_t *vw = reinterpret_cast<u32x4_t *>(vt + buf * VB);
-            for (int c = lane; c < VB / 8; c += 64) {
-                u32x4_t x = vw[c];
-                bool hit = false;
+        u32x4_t kf[2][ES];
+        auto load_k = [&](const Halves &h, int first) {
+            const bool whole = first + KB_FEW <= klen && near;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t y = without_odd(x[j]);
-                    hit |= y != x[j];
-                    x[j] = y;
+            for (int t = 0; t < 2; ++t) {
+                // keys past the last: that one, masked; head_dim 16: the upper slots are zeros of q
+                const int r = min(16 * t + col, klen - 1 - first);
+                const char *kp = whole ? reinterpret_cast<const char *>(K + h.off[t]) + koff
+                                       : reinterpret_cast<const char *>(K + (r < 16 ? h.off[0] : h.off[1]) +
+                                                                        (r & 15) * a.row_stride + (8 * grp) % D);
+#pragma unroll
+                for (int s = 0; s < ES; ++s)
+                    kf[t][s] = *reinterpret_cast<const u32x4_t *>(kp + 64 * s);
+            }
+        };
+        auto load_v = [&](const Halves &h, int first, int buf) {
+            constexpr int LOAD_ROWS = 4 * L::RPL;
+            if (first + KB_FEW <= klen && near) {
+#pragma unroll
+                for (int u = 0; u < VB / 512; ++u)
+                    load_to_lds16(V + h.off[LOAD_ROWS * u / 16] + (int64_t)(LOAD_ROWS * u % 16) * a.row_stride, voff[u & 1],
+                                  vt + buf * VB + u * 512);
+            } else {
+#pragma unroll 1
+                for (int u = 0; u < VB / 512; ++u) {
+                    const int s = 4 * u + (lane >> 4), p = (lane & 15) ^ L::swz(s);
+                    const int r = min(s * L::RPL + p / L::C, klen - 1 - first);
+                    load_to_lds16(V + (r < 16 ? h.off[0] : h.off[1]) + (r & 15) * a.row_stride + 8 * (p % L::C),
+                                  vt + buf * VB + u * 512);
                 }
-                if (hit)
-                    vw[c] = x;
-                odd |= hit;
             }
-            odd = __any(odd);
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        };
+        Halves k{};
+        int b = b0, slot = 0;
+        if (b < b1) {
+            k = halves_of(b, 0);
+            load_k(k, KB_FEW * b);
+            load_v(k, KB_FEW * b, 0);
         }
-        // (a tile's rows at a time: V again from LDS for the second costs less than
-        // the registers of both)
+        int see[QT];
+        u32x4_t qf[QT][ES][T];
 #pragma unroll
         for (int i = 0; i < QT; ++i) {
-            float p[8], mx = -INFINITY;
+            const int row = min(16 * i + col, rows - 1), node = row / a.G;
+            see[i] = seen_from(w.rows.past + node, a.max_length);
+            const TX *qs = static_cast<const TX *>(a.q) + (int64_t)(w.rows.first + node) * a.ld_q +
+                           (int64_t)(g * a.G + row - node * a.G) * D + (8 * grp) % D;
+            const bool none = (D < 32 && grp >= 2) || 16 * i + col >= rows;  // head_dim 16: the upper half of the reduction
 #pragma unroll
-            for (int u = 0; u < 8; ++u)
-                p[u] = s[i][u >> 2][u & 3];
-            if (!full) {
-                const int count = see[i] - first;
-                uint32_t own = count >= 32 ? ~0u : count <= 0 ? 0u : (1u << count) - 1;
-                own = (own & ((now.ok & 1 ? 0xffffu : 0u) | (now.ok & 2 ? 0xffff0000u : 0u))) >> (4 * grp);
-                asm volatile("" : "+v"(own));  // (a branch, and not selects in every block)
-#pragma unroll
-                for (int u = 0; u < 8; ++u)
-                    p[u] = (own >> (16 * (u >> 2) + (u & 3))) & 1 ? p[u] : -INFINITY;
-            }
-#pragma unroll
-            for (int u = 0; u < 8; ++u)
-                mx = fmaxf(mx, p[u]);
-            mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-            if constexpr (!EXACT)
-                mx *= factor;
-            const bool grows = mx > m_run[i] + SLACK;
-            if (__any(grows)) {
-                const float m_new = grows ? mx : m_run[i];
-                const float sc = m_run[i] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run[i] - m_new);
-                l_run[i] *= sc;
-#pragma unroll
-                for (int et = 0; et < ET; ++et)
-                    o[i][et] *= sc;
-                m_run[i] = m_new;
-            }
-            const float m_use = m_run[i] == -INFINITY ? 0.0f : m_run[i];
-            float sum = 0.0f;
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                p[u] = __builtin_amdgcn_exp2f(EXACT ? p[u] - m_use : fmaf(p[u], factor, -m_use));
-                sum += p[u];
-            }
-            l_run[i] += sum;
-            if (odd) {
-                // lane (col, grp) holds elements 16 et + 4 grp + u of row col
-#pragma unroll 1
-                for (int key = 0; key < KB_FEW; ++key) {
-                    float pk = 0.0f;
-                    const int own = 4 * (key >> 4) + (key & 3);
-#pragma unroll
-                    for (int u = 0; u < 8; ++u)
-                        pk = u == own ? p[u] : pk;
-                    pk = __shfl(pk, col + 16 * ((key >> 2) & 3), 64);
-                    const int r = min(key, klen - 1 - first);
-                    const uint16_t *vr = V + (r < 16 ? now.off[0] : now.off[1]) + (r & 15) * a.row_stride + 4 * grp;
-#pragma unroll
-                    for (int et = 0; et < ET; ++et) {
-#pragma unroll
-                        for (int u = 0; u < 4; ++u) {
-                            const float x = load1(vr + 16 * et + u);
-                            if (pk != 0.0f && !finite(x))
-                                o[i][et][u] = fmaf(pk, x, o[i][et][u]);
-                        }
-                        __builtin_amdgcn_sched_barrier(0);  // a few loads at a time: registers
-                    }
-                }
-            }
-            u32x4_t pf[TP];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int s = 0; s < ES; ++s) {
                 if constexpr (EXACT) {
-                    uint32_t t[T];
-                    terms2(p[2 * j], p[2 * j + 1], t);
-#pragma unroll
-                    for (int u = 0; u < T; ++u)
-                        pf[u][j] = t[u];
+                    const float scale = a.scale;
+                    f32x4_t x0 = load4(qs + 32 * s) * scale, x1 = load4(qs + 32 * s + 4) * scale;
+                    if (none)
+                        x0 = x1 = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+                    query_terms(x0, x1, qf[i][s]);
                 } else {
-                    pf[0][j] = cvt_pk(p[2 * j], p[2 * j + 1]);
-                    pf[1][j] = cvt_pk(p[2 * j] - __uint_as_float(pf[0][j] << 16),
-                                      p[2 * j + 1] - __uint_as_float(pf[0][j] & 0xffff0000u));
+                    // (a negative scale as one of q, so that the largest score stays the largest)
+                    const u32x4_t x = *reinterpret_cast<const u32x4_t *>(qs + 32 * s);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        qf[i][s][0][j] = none ? 0u : x[j] ^ (a.scale < 0.0f ? 0x80008000u : 0u);
                 }
-            }
-            // A operand V^T: column 16 et + col of keys 16 I + 4 grp + 0..3
-            int xv = v_lane + 2 * buf * VB;
-            asm volatile("" : "+v"(xv));
-#pragma unroll
-            for (int et = 0; et < ET; ++et) {
-                u32x4_t vf;
-#pragma unroll
-                for (int I = 0; I < 2; ++I) {
-                    const char *src = vb + (xv ^ (32 * et)) + 2 * 16 * I * D;
-                    const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)src);
-                    const u32x2_t y = __builtin_bit_cast(u32x2_t, x);
-                    vf[2 * I] = y[0];
-                    vf[2 * I + 1] = y[1];
-                }
-#pragma unroll
-                for (int u = 0; u < TP; ++u)
-                    o[i][et] = mfma16(vf, pf[u], o[i][et]);
             }
         }
-        // (every read of this block has returned before its buffer is filled again)
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    }
-    // the waves' states, merged in wave order
-    float *mine = reinterpret_cast<float *>(tile[wave]);
+        // (a scale that float32 products would take for zero would make NaN of a masked score)
+        const float factor = EXACT ? 1.0f : fmaxf(fabsf(a.scale), 1.17549435e-38f);
+        float m_run[QT], l_run[QT];
+        f32x4_t o[QT][ET];
 #pragma unroll
-    for (int i = 0; i < QT; ++i) {
-        l_run[i] += __shfl_xor(l_run[i], 16, 64);
-        l_run[i] += __shfl_xor(l_run[i], 32, 64);
+        for (int i = 0; i < QT; ++i) {
+            m_run[i] = -INFINITY;
+            l_run[i] = 0.0f;
 #pragma unroll
-        for (int et = 0; et < ET; ++et)
-            *reinterpret_cast<f32x4_t *>(mine + (16 * i + col) * OP + 16 * et + 4 * grp) = o[i][et];
-        if (grp == 0)
-            ml[wave][16 * i + col] = make_float2(m_run[i], l_run[i]);
-    }
-    __syncthreads();
-    int part = -1;
-    if constexpr (STREAMED)
-        part = from == 0 && to == all ? -1 : 2 * (g * a.chunks + chunk) + (from == 0);
-    merge_waves<TX, D, ROWS, W>(a, w, reinterpret_cast<const float *>(tile), WORDS, &ml[0][0], g, part);
-    if constexpr (!STREAMED) {
-        return;
-    } else {
-        at += to - from;
-        if (at >= end)
-            return;
-        // the next sequence that has spans
-        do
-            ++seq;
-        while (stream.pre[seq + 1] <= at);
+            for (int et = 0; et < ET; ++et)
+                o[i][et] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+        const int v_lane = 2 * L::at(4 * grp + (col >> 2), (col & 3) >> 1) + 8 * (col & 1);
+        const char *vb = reinterpret_cast<const char *>(vt);
+
+        int buf = 0;
+        for (; b < b1; b += W, buf ^= 1) {
+            const int first = KB_FEW * b;
+            const Halves now = k;
+            f32x4_t s[QT][2];
+#pragma unroll
+            for (int i = 0; i < QT; ++i)
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    s[i][t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int e = 0; e < ES; ++e)
+#pragma unroll
+                        for (int u = 0; u < T; ++u)
+                            s[i][t] = mfma16(kf[t][e], qf[i][e][u], s[i][t]);
+                }
+            // this block's V has landed (it was asked for before this block's K, or
+            // just after), then the next block's loads
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            if (b + W < b1) {
+                if (++slot == 32) {
+                    slot = 0;
+                    entries = entries_from(b + W);
+                }
+                k = halves_of(b + W, slot);
+                load_v(k, first + W * KB_FEW, buf ^ 1);
+                load_k(k, first + W * KB_FEW);
+            }
+            const bool full = first + KB_FEW <= kall && now.ok == 3;  // every row sees every key
+            // Infinities and NaN among values that some row does not see: it must not
+            // add 0 times one.  They are taken out here, and put where they belong
+            // beside the products.
+            bool odd = false;
+            if (!full) {
+                u32x4_t *vw = reinterpret_cast<u32x4_t *>(vt + buf * VB);
+                for (int c = lane; c < VB / 8; c += 64) {
+                    u32x4_t x = vw[c];
+                    bool hit = false;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t y = without_odd(x[j]);
+                        hit |= y != x[j];
+                        x[j] = y;
+                    }
+                    if (hit)
+                        vw[c] = x;
+                    odd |= hit;
+                }
+                odd = __any(odd);
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            }
+            // (a tile's rows at a time: V again from LDS for the second costs less than
+            // the registers of both)
+#pragma unroll
+            for (int i = 0; i < QT; ++i) {
+                float p[8], mx = -INFINITY;
+#pragma unroll
+                for (int u = 0; u < 8; ++u)
+                    p[u] = s[i][u >> 2][u & 3];
+                if (!full) {
+                    const int count = see[i] - first;
+                    uint32_t own = count >= 32 ? ~0u : count <= 0 ? 0u : (1u << count) - 1;
+                    own = (own & ((now.ok & 1 ? 0xffffu : 0u) | (now.ok & 2 ? 0xffff0000u : 0u))) >> (4 * grp);
+                    asm volatile("" : "+v"(own));  // (a branch, and not selects in every block)
+#pragma unroll
+                    for (int u = 0; u < 8; ++u)
+                        p[u] = (own >> (16 * (u >> 2) + (u & 3))) & 1 ? p[u] : -INFINITY;
+                }
+#pragma unroll
+                for (int u = 0; u < 8; ++u)
+                    mx = fmaxf(mx, p[u]);
+                mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+                mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+                if constexpr (!EXACT)
+                    mx *= factor;
+                const bool grows = mx > m_run[i] + SLACK;
+                if (__any(grows)) {
+                    const float m_new = grows ? mx : m_run[i];
+                    const float sc = m_run[i] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run[i] - m_new);
+                    l_run[i] *= sc;
+#pragma unroll
+                    for (int et = 0; et < ET; ++et)
+                        o[i][et] *= sc;
+                    m_run[i] = m_new;
+                }
+                const float m_use = m_run[i] == -INFINITY ? 0.0f : m_run[i];
+                float sum = 0.0f;
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    p[u] = __builtin_amdgcn_exp2f(EXACT ? p[u] - m_use : fmaf(p[u], factor, -m_use));
+                    sum += p[u];
+                }
+                l_run[i] += sum;
+                if (odd) {
+                    // lane (col, grp) holds elements 16 et + 4 grp + u of row col
+#pragma unroll 1
+                    for (int key = 0; key < KB_FEW; ++key) {
+                        float pk = 0.0f;
+                        const int own = 4 * (key >> 4) + (key & 3);
+#pragma unroll
+                        for (int u = 0; u < 8; ++u)
+                            pk = u == own ? p[u] : pk;
+                        pk = __shfl(pk, col + 16 * ((key >> 2) & 3), 64);
+                        const int r = min(key, klen - 1 - first);
+                        const uint16_t *vr = V + (r < 16 ? now.off[0] : now.off[1]) + (r & 15) * a.row_stride + 4 * grp;
+#pragma unroll
+                        for (int et = 0; et < ET; ++et) {
+#pragma unroll
+                            for (int u = 0; u < 4; ++u) {
+                                const float x = load1(vr + 16 * et + u);
+                                if (pk != 0.0f && !finite(x))
+                                    o[i][et][u] = fmaf(pk, x, o[i][et][u]);
+                            }
+                            __builtin_amdgcn_sched_barrier(0);  // a few loads at a time: registers
+                        }
+                    }
+                }
+                u32x4_t pf[TP];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if constexpr (EXACT) {
+                        uint32_t t[T];
+                        terms2(p[2 * j], p[2 * j + 1], t);
+#pragma unroll
+                        for (int u = 0; u < T; ++u)
+                            pf[u][j] = t[u];
+                    } else {
+                        pf[0][j] = cvt_pk(p[2 * j], p[2 * j + 1]);
+                        pf[1][j] = cvt_pk(p[2 * j] - __uint_as_float(pf[0][j] << 16),
+                                          p[2 * j + 1] - __uint_as_float(pf[0][j] & 0xffff0000u));
+                    }
+                }
+                // A operand V^T: column 16 et + col of keys 16 I + 4 grp + 0..3
+                int xv = v_lane + 2 * buf * VB;
+                asm volatile("" : "+v"(xv));
+#pragma unroll
+                for (int et = 0; et < ET; ++et) {
+                    u32x4_t vf;
+#pragma unroll
+                    for (int I = 0; I < 2; ++I) {
+                        const char *src = vb + (xv ^ (32 * et)) + 2 * 16 * I * D;
+                        const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)src);
+                        const u32x2_t y = __builtin_bit_cast(u32x2_t, x);
+                        vf[2 * I] = y[0];
+                        vf[2 * I + 1] = y[1];
+                    }
+#pragma unroll
+                    for (int u = 0; u < TP; ++u)
+                        o[i][et] = mfma16(vf, pf[u], o[i][et]);
+                }
+            }
+            // (every read of this block has returned before its buffer is filled again)
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
+        // the waves' states, merged in wave order
+        float *mine = reinterpret_cast<float *>(tile[wave]);
+#pragma unroll
+        for (int i = 0; i < QT; ++i) {
+            l_run[i] += __shfl_xor(l_run[i], 16, 64);
+            l_run[i] += __shfl_xor(l_run[i], 32, 64);
+#pragma unroll
+            for (int et = 0; et < ET; ++et)
+                *reinterpret_cast<f32x4_t *>(mine + (16 * i + col) * OP + 16 * et + 4 * grp) = o[i][et];
+            if (grp == 0)
+                ml[wave][16 * i + col] = make_float2(m_run[i], l_run[i]);
+        }
         __syncthreads();
-    }
+        int part = -1;
+        if constexpr (STREAMED)
+            part = from == 0 && to == all ? -1 : 2 * (g * a.chunks + chunk) + (from == 0);
+        merge_waves<TX, D, ROWS, W>(a, w, reinterpret_cast<const float *>(tile), WORDS, &ml[0][0], g, part);
+        if constexpr (!STREAMED) {
+            return;
+        } else {
+            at += to - from;
+            if (at >= end)
+                return;
+            // the next sequence that has spans
+            do
+                ++seq;
+            while (stream.pre[seq + 1] <= at);
+            __syncthreads();
+        }
     }
 }
 
@@ -1910,7 +1911,9 @@ void plan(BatchAttnArgs *a, bool x_bf16, bool bf16, int D) {
         const int whole = 512 * (int)std::max<int64_t>(1, std::min<int64_t>(4, units / (CUS / 2)));
         const int waves = few && a->tile == 16 && a->max_length > LONG ? 8 : NW, span = few ? waves * KB_FEW : KB;
         const int64_t spans = (int64_t)a->n_seqs * ((a->max_length + span - 1) / span);
-        if (a->max_length > whole && a->n_seqs <= MAX_STREAM && spans <= 1 << 30) {
+        // (the join has a work-group a row, and a launch at most 2^32 threads)
+        const int64_t joins = units * std::min<int64_t>(most, a->tile);
+        if (a->max_length > whole && a->n_seqs <= MAX_STREAM && spans <= 1 << 30 && joins <= 1 << 23) {
             // as many work-groups as run at once
             const int at_once = waves == 8 || (a->tile == 32 && D == 128) ? CUS : 2 * CUS;
             a->waves = waves;
@@ -1924,7 +1927,9 @@ void plan(BatchAttnArgs *a, bool x_bf16, bool bf16, int D) {
     const int blocks = (a->max_length + a->block - 1) / a->block;
     a->per_split = blocks;
     if (a->paged && !few) {
-        const int want = (int)std::max<int64_t>(1, std::min<int64_t>((blocks + 7) / 8, 2 * CUS / units));
+        // (shares of all n rows, also those of no sequence: at most 2^22 in all)
+        const int64_t most_shares = std::min<int64_t>(2 * CUS / units, (1 << 22) / ((int64_t)a->n * a->n_heads));
+        const int want = (int)std::max<int64_t>(1, std::min<int64_t>((blocks + 7) / 8, most_shares));
         a->per_split = (blocks + want - 1) / want;
         a->splits = (blocks + a->per_split - 1) / a->per_split;
     }

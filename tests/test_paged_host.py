@@ -150,6 +150,22 @@ def test_too_many_sequences_times_heads_are_refused():
     assert workspace(kv, batch(n_seqs=65536), n_heads=128) == 0
 
 
+def test_joins_stay_within_a_launch_and_a_workspace():
+    """A launch has at most 2^32 threads, and the join 256 a row and head: no parts
+    for more rows than that, also where most rows are of no sequence."""
+    kv = pages(n_kv_heads=128, page_stride=128 * 16 * 128)
+    chains = batch(n_seqs=1024, max_rows=128, max_length=0, table_pages=320, ld_table=320)
+    assert workspace(kv, chains, n_heads=128, n=131072) == 0
+    kv = pages(n_kv_heads=64, page_stride=64 * 16 * 128)
+    assert workspace(kv, chains, n_heads=64, n=131072) > 0  # 2^23 of them
+    one = batch(n_seqs=1, max_length=0, table_pages=4000, ld_table=4000)
+    for n, shares in ((6, None), (1 << 18, 4), (1 << 20, 1)):
+        need = workspace(pages(dtype=binding.SD_F32), one, n_heads=4, n=n)
+        assert need <= (1 << 22) * (128 * 4 + 8)
+        if shares:
+            assert need == (0 if shares == 1 else shares * n * 4 * (128 * 4 + 8))
+
+
 def test_workspace_is_asked_for():
     b = batch(n_seqs=1, table_pages=1000, ld_table=1000, max_length=16000, max_rows=1)
     for x in (0, 1):
