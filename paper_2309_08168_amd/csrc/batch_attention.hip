@@ -1892,7 +1892,14 @@ __global__ __launch_bounds__(THREADS) void k_batch_join_stream(BatchAttnArgs a, 
 // 500 .. 8000 197 -> 193; 8 sequences of 750 .. 1500 (40 heads) 46.6 -> 48.7.
 //   Packed tiles of 64 or 128 rows, us: 1023 rows of 40 heads (360 tiles) float32 51
 // and 68, bfloat16 31.8 and 35.5; 1000 of 64 heads on 8 (512) 72 and 71, 43 and 35.
-constexpr int FEW_ROWS = 32, CUS = 256, LONG = 2048, NARROW = 450;
+//   One wave a work-group for short ones, where more than four times as many then run
+// at once (four waves and one): a token of 32 sequences (40 heads, float32) of up to 30
+// keys 18.7 and 9.8 us, 100 22.4 and 16.9, 250 34.0 and 32.5, 500 55.3 and 55.0; 64
+// sequences of 500 93 and 101; 256 (64 heads on 8, bfloat16) of 100 29.2 and 20.7, 500 77.9 and
+// 79.8; 16 of 30 11.8 and 6.9, 8 of 100 9.6 and 11.7.  27 rows each of 14 sequences, 100 keys
+// 30.7 and 23.7, 400 48.8 and 43.9; 2 to 4 rows of 64 heads on 8, 40 sequences of 100 (320
+// work-groups) 19.0 and 21.9.
+constexpr int FEW_ROWS = 32, CUS = 256, SHORT = 256, LONG = 2048, NARROW = 450;
 void plan(BatchAttnArgs *a, bool x_bf16, bool bf16, int D) {
     const int64_t most = (int64_t)a->max_rows * a->G;
     const bool few = bf16 && a->paged && most <= FEW_ROWS;
@@ -1923,6 +1930,8 @@ void plan(BatchAttnArgs *a, bool x_bf16, bool bf16, int D) {
             return;
         }
     }
+    if (few && units > 2 * CUS && a->max_length <= (a->tile == 16 ? SHORT : 2 * SHORT))
+        a->waves = 1;
     a->block = few || (x_bf16 && bf16 && a->tile == 128) ? KB_FEW : KB;
     const int blocks = (a->max_length + a->block - 1) / a->block;
     a->per_split = blocks;
@@ -1968,11 +1977,15 @@ void launch_mfma(const BatchAttnArgs &a, hipStream_t s) {
             hipLaunchKernelGGL((k_batch_attn_few<TX, D, 1, 8, true>), grid, dim3(512), 0, s, a);
         else if (a.chunks)
             hipLaunchKernelGGL((k_batch_attn_few<TX, D, 1, NW, true>), grid, block, 0, s, a);
+        else if (a.waves == 1)
+            hipLaunchKernelGGL((k_batch_attn_few<TX, D, 1, 1, false>), grid, dim3(64), 0, s, a);
         else
             hipLaunchKernelGGL((k_batch_attn_few<TX, D, 1, NW, false>), grid, block, 0, s, a);
     } else if (a.tile == 32) {
         if (a.chunks)
             hipLaunchKernelGGL((k_batch_attn_few<TX, D, 2, NW, true>), grid, block, 0, s, a);
+        else if (a.waves == 1)
+            hipLaunchKernelGGL((k_batch_attn_few<TX, D, 2, 1, false>), grid, dim3(64), 0, s, a);
         else
             hipLaunchKernelGGL((k_batch_attn_few<TX, D, 2, NW, false>), grid, block, 0, s, a);
     } else if (a.tile == 64) {

@@ -700,3 +700,43 @@ def test_streams_are_the_same_in_any_order():
     one = binding.paged_attention(q, c.k, c.v, binding.batch(gpu(c.table), gpu(lengths)))
     back = binding.paged_attention(q.flip(0), c.k, c.v, binding.batch(gpu(c.table[::-1].copy()), gpu(lengths[::-1]))).flip(0)
     assert (one - back).abs().max() <= 2.0 ** -20
+
+
+# ----------------------------------------------------------------------------
+# many short sequences: a wave each
+
+
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
+@pytest.mark.parametrize("rows,heads", [(1, 86), (3, 129), (18, 43)])
+def test_many_short_sequences(x, d, rows, heads):
+    """More than 512 work-groups of at most 32 rows, contexts of zero to several blocks, pages that are not there."""
+    def spoil(c):
+        c.table[0, 0] = -1
+        c.table[4, 1], c.table[5, 2] = c.n_pages, -2**31
+
+    lengths = [100, rows, 33, 0, 64, 250, 31, 32, 20, 129, 16, 65]
+    m = [min(rows, n) for n in lengths]
+    m[8] = 0
+    check_paged(m, lengths, heads, 43, d, x, "bf16", 16, spoil=spoil, gap=1)
+    check_paged(m, lengths, heads, 43, d, x, "bf16", 64, order="rows")
+
+
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [2, 20])
+def test_many_short_sequences_and_values_that_are_infinite(x, rows):
+    """What a row sees arrives in its column; what it does not, changes no bit of it."""
+    rng = np.random.default_rng(78)
+    lengths, kvh = [40 + 5 * s for s in range(40)], 16
+    c = Cache(rng, lengths, kvh, 16, 32, "bf16")
+    q = torch.tensor(rng.standard_normal((40 * rows, kvh, 32)), dtype=TYPES[x], device="cuda")
+    batch = binding.batch(gpu(c.table), gpu(lengths), None, rows, max(lengths))
+    want = binding.paged_attention(q, c.k, c.v, batch).clone()
+    s, at = 11, lengths[11] - 1  # of its rows only the last sees it
+    c.v[int(c.table[s, at // 16]), :, at % 16, 9] = float("inf")
+    got = binding.paged_attention(q, c.k, c.v, batch)
+    last = (s + 1) * rows - 1
+    others = [r for r in range(40 * rows) if r != last]
+    rest = [e for e in range(32) if e != 9]
+    assert torch.equal(got[others], want[others]) and torch.equal(got[last][:, rest], want[last][:, rest])
+    assert not got[last, :, 9].isfinite().any()
