@@ -1770,10 +1770,9 @@ __global__ __launch_bounds__(64 * W, W == 8 ? 1 : QT == 1 || D < 128 ? 2 : 1) vo
 
 // The shares of a (row, head) joined: a work-group each.  D / 4 lanes hold a row, the
 // groups of lanes take the shares in turn and add up in order.
-constexpr int JOIN_THREADS = 256;
-template <typename TX, int D>
-__global__ __launch_bounds__(JOIN_THREADS) void k_batch_join(BatchAttnArgs a) {
-    constexpr int LANES = D / 4, NG = JOIN_THREADS / LANES;
+template <typename TX, int D, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_batch_join(BatchAttnArgs a) {
+    constexpr int LANES = D / 4, NG = THREADS / LANES;
     __shared__ f32x4_t red[NG][LANES];
     const int64_t slots = (int64_t)a.n * a.n_heads, slot = blockIdx.x;
     const int lane = threadIdx.x & 63, e = threadIdx.x % LANES, gi = threadIdx.x / LANES;
@@ -1906,7 +1905,9 @@ void plan(BatchAttnArgs *a, bool x_bf16, bool bf16, int D) {
     const auto slots_of = [&](int tile) {
         return most <= tile ? (int64_t)a->n_seqs : (int64_t)a->n * a->G / tile + a->n_seqs;
     };
-    const bool narrow = most <= 64 || (!a->paged && slots_of(128) * a->n_kv_heads <= NARROW);
+    const int64_t wide = slots_of(128) * a->n_kv_heads;
+    const bool narrow = most <= 64 || (wide <= NARROW && (!a->paged || (wide > CUS && (!x_bf16 || (int64_t)a->n * a->G <=
+                                                                                             512 * (int64_t)a->n_seqs))));
     a->tile = !bf16 ? 16 : few ? (most <= 16 ? 16 : 32) : narrow ? 64 : 128;
     a->one_tile = most <= a->tile;
     a->slots = (int32_t)slots_of(a->tile);
@@ -2032,28 +2033,32 @@ void launch_join_stream(const BatchAttnArgs &a, hipStream_t s) {
         hipLaunchKernelGGL((k_batch_join_stream<TX, D, 256>), grid, dim3(256), 0, s, a, rows);
 }
 
+template <typename TX, int D>
+void launch_join_shares(const BatchAttnArgs &a, hipStream_t s) {
+    const dim3 grid((unsigned)(a.n * a.n_heads));
+    if (a.splits <= 8)
+        hipLaunchKernelGGL((k_batch_join<TX, D, 64>), grid, dim3(64), 0, s, a);
+    else
+        hipLaunchKernelGGL((k_batch_join<TX, D, 256>), grid, dim3(256), 0, s, a);
+}
+
+template <typename TX, int D>
+void launch_join(const BatchAttnArgs &a, hipStream_t s) {
+    if (a.chunks)
+        launch_join_stream<TX, D>(a, s);
+    else
+        launch_join_shares<TX, D>(a, s);
+}
 template <typename TX>
 void launch_join(const BatchAttnArgs &a, int D, hipStream_t s) {
-    if (a.chunks) {
-        if (D == 16)
-            launch_join_stream<TX, 16>(a, s);
-        else if (D == 32)
-            launch_join_stream<TX, 32>(a, s);
-        else if (D == 64)
-            launch_join_stream<TX, 64>(a, s);
-        else
-            launch_join_stream<TX, 128>(a, s);
-        return;
-    }
-    const dim3 grid((unsigned)(a.n * a.n_heads)), block(JOIN_THREADS);
     if (D == 16)
-        hipLaunchKernelGGL((k_batch_join<TX, 16>), grid, block, 0, s, a);
+        launch_join<TX, 16>(a, s);
     else if (D == 32)
-        hipLaunchKernelGGL((k_batch_join<TX, 32>), grid, block, 0, s, a);
+        launch_join<TX, 32>(a, s);
     else if (D == 64)
-        hipLaunchKernelGGL((k_batch_join<TX, 64>), grid, block, 0, s, a);
+        launch_join<TX, 64>(a, s);
     else
-        hipLaunchKernelGGL((k_batch_join<TX, 128>), grid, block, 0, s, a);
+        launch_join<TX, 128>(a, s);
 }
 
 // What both entry points take besides their keys.
