@@ -496,11 +496,12 @@ sd_status sd_paged_append(const sd_rope *rope, const void *qkv, int64_t ld_qkv, 
  * positions 0 .. p of its sequence (its own and those of the rows before it
  * are in the pages already).  q and out [n][n_heads head_dim] (x_dtype, rows
  * ld_q and ld_out apart, not overlapping); scores are scaled by scale (0: 1 /
- * sqrt(head_dim); scale log2(e) is finite); scores and sums are float32 (with
- * bfloat16 queries the softmax weights may be rounded to bfloat16 for their
- * products).  A row that sees nothing gives zeros; what a row does not see
+ * sqrt(head_dim); scale log2(e) is finite); scores and sums are float32 (of
+ * bfloat16 queries and pages the softmax weights are rounded to bfloat16 for their
+ * products, but for max_rows times query heads of a kv head up to 32).  A row that sees nothing gives zeros; what a row does not see
  * changes no bit of its result, whatever it holds, and neither do the other
- * rows' queries; what it sees is finite, or its result may be NaN.  workspace
+ * rows' queries (the sizes of the call and the lengths of its sequences may, in
+ * the order of float32 sums); what it sees is finite, or its result may be NaN.  workspace
  * (16-byte aligned) holds at least sd_paged_attention_workspace() bytes for
  * these sizes and belongs to the call until it has run.  Errors: INVALID_ARG, DEVICE. */
 sd_status sd_paged_attention(const sd_kv_pages *kv, const sd_batch *batch, const void *q, int64_t ld_q, int32_t x_dtype,

@@ -6,7 +6,13 @@
 // of a kv head share its keys: its m G rows (row = i G + head) are cut into tiles,
 // and the keys of a tile into shares, each leaving an unnormalised output with its
 // maximum and sum, which a second kernel joins in order; a single share is
-// normalised at once.
+// normalised at once.  One pass over the keys: a running maximum m and sum l of a row,
+// which, with o, are multiplied by exp(m - m') where m rises to m'.
+//
+// A call reads the keys and values of its sequences, q, and writes out; it computes 4 D
+// flops a (row, head, key).  Tokens and short chains are bound by the read (k_batch_attn_few,
+// streams), chunks and prompts by the matrix cores (k_batch_attn_wide for bfloat16 queries,
+// k_batch_attn_mfma), float32 caches by either (k_batch_attn_f32).
 #include "paged.h"
 
 #include <algorithm>
@@ -230,6 +236,15 @@ __device__ __forceinline__ void keep_spans(const BatchAttnArgs &a, const Stream 
 // elements of row 4 g + v are a lane's operands of four tiles.  V is asked for before
 // the scores and the next block's K after them.  The waves keep states of their
 // own and merge at the end.  A wave's 16 keys lie in one page.
+//
+// Tokens: bound by the read (8 sequences of 700 to 1500 keys, 40 heads of 128, 88 us, 4.5
+// TB/s).  Prompts: four of 3115 rows, 4 heads of 64, 285 us, 70 of the 154 TFLOP/s that a
+// large float32 product reaches; 700 rows, 64 heads on 8 of 128, 126 us, 64.  Float32
+// products and vector operations take turns (32 products 1035 cycles of a SIMD, 128
+// multiply-adds 364, both 1351), but a softmax left out gains 2 to 7%, and loads left out 11
+// to 24: the rest is the start and the merge of tiles of 16 rows, few blocks each.  Tiles of
+// 32 rows: 136 -> 124 us at 64 heads, 81 -> 93 at 4.  K by whole rows, lane offsets kept,
+// chains of products cut in four, a maximum that may lag: none faster, or slower by 5%.
 
 template <typename TX, int D>
 __global__ __launch_bounds__(NW * 64, 2) void k_batch_attn_f32(BatchAttnArgs a) {
@@ -420,6 +435,11 @@ __global__ __launch_bounds__(NW * 64, 2) void k_batch_attn_f32(BatchAttnArgs a) 
 // V read over all banks; the loads permute the chunks of a line on the way in.
 // The 16 rows of a group lie in one page, so a load of a group's rows (heads of 32 and
 // more) has one base.
+//
+// Bound by the matrix cores: 1023 float32 rows, 40 heads of 128, 39.6 us, 0.81 PFLOP/s issued
+// (three terms), where a large product of random operands reaches 1.42.  A weight of a bfloat16
+// call is rounded to bfloat16 for its product with V, by 2^-8 of it at most; a second term would take half again as many products (the few rows of
+// k_batch_attn_few have it, where the read hides it).
 
 // Where the four 16-key groups of a block start: elements from a head's first, and
 // whether there are keys (a bit each).
@@ -587,7 +607,8 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_batch_attn_mfma(BatchAttnAr
                 for (int u = wave; u < L::C; u += WAVES) {
                     const int s = 4 * u + (lane >> 4), p = (lane & 15) ^ L::swz(s);
                     // rows past the last: that one
-                    const int64_t at = row_at(k, one, min(s * L::RPL + p / L::C, klen - 1 - first), a.row_stride) + 8 * (p % L::C);
+                    const int r = min(s * L::RPL + p / L::C, klen - 1 - first);
+                    const int64_t at = row_at(k, one, r, a.row_stride) + 8 * (p % L::C);
                     load_to_lds16(K + at, &kv[buf][0][u * 512]);
                     load_to_lds16(V + at, &kv[buf][1][u * 512]);
                 }
@@ -595,7 +616,8 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_batch_attn_mfma(BatchAttnAr
         };
         Entries entries = entries_of<PAGED>(a, w, KB * b0, klen);
         // The queries are asked for before the first block: loads return in order.
-        const TX *qs = static_cast<const TX *>(a.q) + (int64_t)(w.rows.first + node) * a.ld_q + (int64_t)head * D + 8 * half;
+        const TX *qs =
+            static_cast<const TX *>(a.q) + (int64_t)(w.rows.first + node) * a.ld_q + (int64_t)head * D + 8 * half;
         u32x4_t qf[ES][T];
         f32x4_t qx[EXACT ? ES : 1][2];
 #pragma unroll
@@ -691,7 +713,8 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_batch_attn_mfma(BatchAttnAr
                 // byte addresses in LDS: rows 32 h + col, chunk 2 e + half at xk ^ 32 e.
                 // (Hidden from the compiler, which would keep every address of the
                 // loop in a register and spill.)
-                int xk = 2 * (buf * 2 * KB * D + 32 * h * D + L::at(col, half)), xv = 2 * (buf * 2 * KB * D + 32 * h * D) + v_lane;
+                int xk = 2 * (buf * 2 * KB * D + 32 * h * D + L::at(col, half));
+                int xv = 2 * (buf * 2 * KB * D + 32 * h * D) + v_lane;
                 asm volatile("" : "+v"(xk), "+v"(xv));
                 __builtin_amdgcn_s_setprio(1);
 #pragma unroll
@@ -821,21 +844,22 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_batch_attn_mfma(BatchAttnAr
             }
             __syncthreads();
             if (wk == 0) {
-            const float m2 = to[(16 * ET * NQ + wq) * 64 + lane], l2 = to[((16 * ET + 1) * NQ + wq) * 64 + lane];
-            const float m = fmaxf(m_run, m2), mu = m == -INFINITY ? 0.0f : m;
-            const float w1 = __builtin_amdgcn_exp2f(m_run - mu), w2 = __builtin_amdgcn_exp2f(m2 - mu);
-            m_run = m;
-            l_run = l_run * w1 + l2 * w2;
+                const float m2 = to[(16 * ET * NQ + wq) * 64 + lane], l2 = to[((16 * ET + 1) * NQ + wq) * 64 + lane];
+                const float m = fmaxf(m_run, m2), mu = m == -INFINITY ? 0.0f : m;
+                const float w1 = __builtin_amdgcn_exp2f(m_run - mu), w2 = __builtin_amdgcn_exp2f(m2 - mu);
+                m_run = m;
+                l_run = l_run * w1 + l2 * w2;
 #pragma unroll
-            for (int et = 0; et < ET; ++et)
+                for (int et = 0; et < ET; ++et)
 #pragma unroll
-                for (int v = 0; v < 16; ++v)
-                    o[et][v] = o[et][v] * w1 + to[((16 * et + v) * NQ + wq) * 64 + lane] * w2;
+                    for (int v = 0; v < 16; ++v)
+                        o[et][v] = o[et][v] * w1 + to[((16 * et + v) * NQ + wq) * 64 + lane] * w2;
             }
         }
         if (mine && wk == 0) {
             const int64_t packed = w.rows.first + node;
-            const int64_t slot = FROM == STREAM ? (int64_t)part * a.tile + 32 * wq + col : ((int64_t)part * a.n + packed) * a.n_heads + head;
+            const int64_t slot = FROM == STREAM ? (int64_t)part * a.tile + 32 * wq + col
+                                                : ((int64_t)part * a.n + packed) * a.n_heads + head;
             TX *out = static_cast<TX *>(a.out) + packed * a.ld_out + (int64_t)head * D;
             const float inv = part >= 0 ? 1.0f : l_run == 0.0f ? 0.0f : 1.0f / l_run;
 #pragma unroll
@@ -878,6 +902,13 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_batch_attn_mfma(BatchAttnAr
 // a part of the softmax at a time.  K comes four blocks ahead and V two, in rings
 // of four.  The running maximum of block t rescales the sums when block t - 1 is in
 // them.  Blocks that some row does not see whole take their parts one after another.
+//
+// Heads of 128, us: 8000 rows of 32 heads 534 (0.98 PFLOP/s), 1000 rows of 64 heads on 8
+// behind 15111 positions 541 (0.94), 16 ragged prompts of 64 heads on 8 378 (0.70: 5 to 6 us of
+// start and end a tile).  With k_batch_attn_mfma, whose blocks of 64 keys take their parts
+// one after another, 579, 622 and 398.  The 8000 rows of zeros take 383: power holds the clock at 2.07 GHz
+// with random operands, and the matrix cores are busy 45% of the time.  Loads cost 13% of
+// a step, its barrier 2 to 4.  64-key steps need more registers than there are.
 struct Halves {  // where the 16-key halves of a block start (elements), and which have a page
     int64_t off[2];
     int ok;
@@ -1421,10 +1452,17 @@ __global__ __launch_bounds__(256, 2) void k_batch_attn_wide(BatchAttnArgs a) {
 // LDS lines are permuted for the reads here: eight rows, two adjacent chunks each.
 // A lane holds the table's entry for half a block of the wave, 32 blocks at a time.
 // A work-group takes a sequence whole, or the chunk of a stream.
+//
+// Bound by the read, 6.15 TB/s at most for pages in any order: 64 sequences of 500 to 8000
+// keys, 64 heads on 8, 193 us, 5.6 TB/s; one of 60002 49 us, 5.0 (55 in a captured graph of
+// such calls).  So weights of bfloat16 calls are two bfloat16 terms, off by 2^-16,
+// for products that wait for the read in any case (float32 three, off by less than the
+// float32 sums).  Loads that bypass the caches: 229 -> 238 us, 56.7 -> 55.0.
 template <typename TX, int D, int QT, int W, bool STREAMED>
 __global__ __launch_bounds__(64 * W, W == 8 ? 1 : QT == 1 || D < 128 ? 2 : 1) void k_batch_attn_few(BatchAttnArgs a) {
     constexpr bool EXACT = sizeof(TX) == 4;
-    constexpr int T = EXACT ? X_TERMS : 1, TP = EXACT ? X_TERMS : 2, ES = D < 32 ? 1 : D / 32, ET = D / 16, ROWS = 16 * QT, OP = D + 4;
+    constexpr int T = EXACT ? X_TERMS : 1, TP = EXACT ? X_TERMS : 2;  // of q and of the weights
+    constexpr int ES = D < 32 ? 1 : D / 32, ET = D / 16, ROWS = 16 * QT, OP = D + 4;
     using L = FewLines<D>;
     constexpr int VB = KB_FEW * D;  // elements of a V block
     constexpr int WORDS = VB > ROWS * OP ? VB : ROWS * OP;
@@ -1769,7 +1807,8 @@ __global__ __launch_bounds__(64 * W, W == 8 ? 1 : QT == 1 || D < 128 ? 2 : 1) vo
 }
 
 // The shares of a (row, head) joined: a work-group each.  D / 4 lanes hold a row, the
-// groups of lanes take the shares in turn and add up in order.
+// groups of lanes take the shares in turn and add up in order.  One wave where there are at
+// most eight shares: 12800 rows of four joined with attention 58 us, 68 with four waves.
 template <typename TX, int D, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_batch_join(BatchAttnArgs a) {
     constexpr int LANES = D / 4, NG = THREADS / LANES;
@@ -1821,7 +1860,7 @@ __global__ __launch_bounds__(THREADS) void k_batch_join(BatchAttnArgs a) {
 }
 
 // The parts of a sequence joined, of a stream's chunks: a work-group a row of a
-// (sequence, kv head).
+// (sequence, kv head).  4 to 5 us, of which about 2.5 are a launch's.
 template <typename TX, int D, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_batch_join_stream(BatchAttnArgs a, int rows_most) {
     constexpr int LANES = D / 4, NG = THREADS / LANES;
@@ -1891,6 +1930,15 @@ __global__ __launch_bounds__(THREADS) void k_batch_join_stream(BatchAttnArgs a, 
 // 500 .. 8000 197 -> 193; 8 sequences of 750 .. 1500 (40 heads) 46.6 -> 48.7.
 //   Packed tiles of 64 or 128 rows, us: 1023 rows of 40 heads (360 tiles) float32 51
 // and 68, bfloat16 31.8 and 35.5; 1000 of 64 heads on 8 (512) 72 and 71, 43 and 35.
+//   Over pages, where tiles of 128 rows are too many for shares (more than 256) and too few
+// to fill the last round (at most 450): 15 chains of 26 rows, 64 heads on 8, 26.9 and 36.3,
+// float32 39.6 and 56.9; five chunks of up to 358 rows of 32 heads 40.7 and 55.5, 58.8 and 76.4; 1000
+// rows of 40 heads behind 2000 positions 126 and 96, 187 and 187; six of 100 rows, 64 heads
+// on 8, behind up to 8000 264 and 258, 367 and 497: float32 always, bfloat16 where
+// sequences are short, whose last tiles are a large part.
+//   Shares for two work-groups a CU (three, four): 200 rows of 64 heads on 8 behind 4000 positions
+// 58 (64, 78) us, 1000 of 40 heads behind 2000 97 (121, 122), 13 of 64 heads on 8 behind 2000,
+// float32, 46 (40, 40).
 //   One wave a work-group for short ones, where more than four times as many then run
 // at once (four waves and one): a token of 32 sequences (40 heads, float32) of up to 30
 // keys 18.7 and 9.8 us, 100 22.4 and 16.9, 250 34.0 and 32.5, 500 55.3 and 55.0; 64
@@ -1906,8 +1954,8 @@ void plan(BatchAttnArgs *a, bool x_bf16, bool bf16, int D) {
         return most <= tile ? (int64_t)a->n_seqs : (int64_t)a->n * a->G / tile + a->n_seqs;
     };
     const int64_t wide = slots_of(128) * a->n_kv_heads;
-    const bool narrow = most <= 64 || (wide <= NARROW && (!a->paged || (wide > CUS && (!x_bf16 || (int64_t)a->n * a->G <=
-                                                                                             512 * (int64_t)a->n_seqs))));
+    const bool brief = !x_bf16 || (int64_t)a->n * a->G <= 512 * (int64_t)a->n_seqs;
+    const bool narrow = most <= 64 || (wide <= NARROW && (!a->paged || (wide > CUS && brief)));
     a->tile = !bf16 ? 16 : few ? (most <= 16 ? 16 : 32) : narrow ? 64 : 128;
     a->one_tile = most <= a->tile;
     a->slots = (int32_t)slots_of(a->tile);
