@@ -51,6 +51,7 @@ struct BatchAttnArgs {
     int32_t *spans;                    // [n_seqs + 2]: spans before each sequence, and of a chunk
     int32_t tile, slots, one_tile;     // rows of a tile; tiles at most; whether a sequence has at most one
     int32_t splits, per_split, block;  // shares of the keys; blocks of a share; keys of a block
+    int32_t wide;                      // whether k_batch_attn_wide takes it
 };
 
 // An address that is the same in every lane, in scalar registers.
@@ -1936,6 +1937,12 @@ __global__ __launch_bounds__(THREADS) void k_batch_join_stream(BatchAttnArgs a, 
 // rows of 40 heads behind 2000 positions 126 and 96, 187 and 187; six of 100 rows, 64 heads
 // on 8, behind up to 8000 264 and 258, 367 and 497: float32 always, bfloat16 where
 // sequences are short, whose last tiles are a large part.
+//   k_batch_attn_wide for bfloat16 queries, or k_batch_attn_mfma where blocks that a row sees
+// in part, which the first takes without overlap, and the start are much of it: 39 chunks
+// of up to 77 rows over up to 96 positions, 32 heads, 42.3 and 28.7; 20 of up to 128 over 428 52.3 and
+// 42.9, over 728 96.3 and 93.7, over 1128 123 and 127; 10 of 100 of 64 heads on 8 over 700 55.8 and
+// 61.6.  Prompts of 32 heads, 16 of 400 rows 94 and 79, 1200 343 and 315, one of 3001 108 and
+// 105, of 8000 534 and 579; of 64 heads on 8, 8 of 400 61.6 and 60.3, 800 145 and 151.
 //   Shares for two work-groups a CU (three, four): 200 rows of 64 heads on 8 behind 4000 positions
 // 58 (64, 78) us, 1000 of 40 heads behind 2000 97 (121, 122), 13 of 64 heads on 8 behind 2000,
 // float32, 46 (40, 40).
@@ -1953,9 +1960,9 @@ void plan(BatchAttnArgs *a, bool x_bf16, bool bf16, int D) {
     const auto slots_of = [&](int tile) {
         return most <= tile ? (int64_t)a->n_seqs : (int64_t)a->n * a->G / tile + a->n_seqs;
     };
-    const int64_t wide = slots_of(128) * a->n_kv_heads;
+    const int64_t tiles = slots_of(128) * a->n_kv_heads;
     const bool brief = !x_bf16 || (int64_t)a->n * a->G <= 512 * (int64_t)a->n_seqs;
-    const bool narrow = most <= 64 || (wide <= NARROW && (!a->paged || (wide > CUS && brief)));
+    const bool narrow = most <= 64 || (tiles <= NARROW && (!a->paged || (tiles > CUS && brief)));
     a->tile = !bf16 ? 16 : few ? (most <= 16 ? 16 : 32) : narrow ? 64 : 128;
     a->one_tile = most <= a->tile;
     a->slots = (int32_t)slots_of(a->tile);
@@ -1981,7 +1988,9 @@ void plan(BatchAttnArgs *a, bool x_bf16, bool bf16, int D) {
     }
     if (few && units > 2 * CUS && a->max_length <= (a->tile == 16 ? SHORT : 2 * SHORT))
         a->waves = 1;
-    a->block = few || (x_bf16 && bf16 && a->tile == 128) ? KB_FEW : KB;
+    a->wide = x_bf16 && bf16 && a->tile == 128 &&
+              (a->paged ? a->max_length > 512 : (int64_t)a->n * a->G > 4096 * (int64_t)a->n_seqs);
+    a->block = few || a->wide ? KB_FEW : KB;
     const int blocks = (a->max_length + a->block - 1) / a->block;
     a->per_split = blocks;
     if (a->paged && !few) {
@@ -2046,7 +2055,7 @@ void launch_mfma(const BatchAttnArgs &a, hipStream_t s) {
             hipLaunchKernelGGL((k_batch_attn_mfma<TX, D, 2, 2, PACKED>), grid, block, 0, s, a);
     } else if (a.chunks) {
         hipLaunchKernelGGL((k_batch_attn_mfma<TX, D, 4, 1, STREAM>), grid, block, 0, s, a);
-    } else if constexpr (sizeof(TX) == 2) {
+    } else if (a.wide) {
         if (a.paged)
             hipLaunchKernelGGL((k_batch_attn_wide<D, true>), grid, block, 0, s, a);
         else

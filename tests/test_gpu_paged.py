@@ -740,3 +740,42 @@ def test_many_short_sequences_and_values_that_are_infinite(x, rows):
     rest = [e for e in range(32) if e != 9]
     assert torch.equal(got[others], want[others]) and torch.equal(got[last][:, rest], want[last][:, rest])
     assert not got[last, :, 9].isfinite().any()
+
+
+# ----------------------------------------------------------------------------
+# prompts of many tiles a sequence
+
+
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
+@pytest.mark.parametrize("rows,heads,kvh", [([150, 129, 161, 1, 200], 120, 3), ([577], 128, 16), ([300, 90, 511], 128, 16),
+                                            ([40] * 12, 64, 64)])
+def test_prompts_of_many_tiles(x, d, rows, heads, kvh):
+    """More than 450 tiles of 128 rows, of sequences of many tiles and of one each."""
+    rng = np.random.default_rng(60 + d)
+    starts, n, G = starts_of(rows), sum(rows), heads // kvh
+    kv = torch.tensor(rng.standard_normal((2, n + 3, kvh, d)), dtype=torch.bfloat16, device="cuda")
+    kv[:, n:] = float("nan")
+    q = torch.tensor(rng.standard_normal((n, heads, d)), dtype=TYPES[x], device="cuda")
+    got = binding.prompt_attention(q, kv[0].transpose(0, 1), kv[1].transpose(0, 1), gpu(starts))
+    q64, k64, v64 = (f64(t) for t in (q, kv[0], kv[1]))
+    for s, m in enumerate(rows):
+        for h in range(s % 3, heads, 11):
+            a = slice(starts[s], starts[s] + m)
+            kk, vv, qq = k64[a, h // G], v64[a, h // G], q64[a, h]
+            z = np.where(np.tril(np.ones((m, m), bool)), qq @ kk.T / math.sqrt(d), -np.inf)
+            p = np.exp(z - z.max(axis=1, keepdims=True))
+            p /= p.sum(axis=1, keepdims=True)
+            want, spread = p @ vv, p @ np.abs(vv)
+            size = float((np.abs(qq) @ np.abs(kk).T).max() / math.sqrt(d))
+            tol = P.attention_tol(x, d, m, size, np.abs(vv).max(), want, spread)
+            assert (np.abs(f64(got[a, h]) - want) <= tol).all(), (s, h)
+
+
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
+@pytest.mark.parametrize("page", [16, 32, 64])
+def test_paged_chunks_of_short_and_long_contexts(x, d, page):
+    """Tiles of 128 rows over at most 512 positions and over more."""
+    check_paged([150, 0, 67, 129], [500, 333, 67, 129], 4, 2, d, x, "bf16", page, max_length=512)
+    check_paged([150, 0, 67, 129], [500, 333, 67, 129], 4, 2, d, x, "bf16", page, max_length=513, max_rows=151, gap=2)
