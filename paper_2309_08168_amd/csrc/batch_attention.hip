@@ -2274,6 +2274,22 @@ sd_status sd_paged_attention(const sd_kv_pages *kv, const sd_batch *batch, const
                                     workspace_bytes, reinterpret_cast<hipStream_t>(hip_stream));)
 }
 
+// For the tests: how a call over pages is shared out: rows of a tile and how many tiles at
+// most, chunks of the streams and keys of a span, shares of the keys, waves of a work-group, and whether
+// k_batch_attn_wide takes it.
+sd_status sdk_paged_plan(const sd_kv_pages *kv, const sd_batch *batch, int32_t x_dtype, int32_t n_heads, int32_t n,
+                         int32_t out[7]) {
+    BatchAttnArgs a{};
+    sd_status st = paged_sizes(kv, batch, n_heads, n, false, &a);
+    if (st != SD_OK || (st = check_call(nullptr, 0, x_dtype, n_heads, n, a.n_seqs, a.n_kv_heads, kv->head_dim, nullptr, 0,
+                                        nullptr)) != SD_OK)
+        return st;
+    plan(&a, x_dtype == SD_BF16, kv->dtype == SD_BF16, kv->head_dim);
+    const int32_t of[7] = {a.tile, a.slots, a.chunks, a.span, a.splits, a.waves, a.wide};
+    std::copy(of, of + 7, out);
+    return SD_OK;
+}
+
 sd_status sd_prompt_attention(const sd_kv_layer *kv, const int32_t *starts, int32_t n_seqs, const void *q, int64_t ld_q,
                               int32_t x_dtype, int32_t n_heads, int32_t n, float scale, void *out, int64_t ld_out,
                               void *hip_stream) {

@@ -1,0 +1,76 @@
+"""paged_attention by every way a call is shared out, against float64: streams of many
+spans, tiles over pages with and without shares, many sequences.
+
+Tolerances count roundings: see the helpers.  What a row must not see holds NaN throughout.
+"""
+
+import numpy as np
+import pytest
+
+from tests import paged_routes as R
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from tests.test_gpu_paged import TYPES, Cache, _gpu, f64, gpu, starts_of  # noqa: E402,F401
+
+if torch.cuda.is_available():
+    from paper_2309_08168_amd import binding
+
+
+def check(call, d, x, dtype, want_plan=None, max_length=0, gap=0, heads_of=None, spoil=None, seed=0):
+    """One call, on some kv heads (all of a few) against float64.  want_plan: what its plan has to hold."""
+    rng = np.random.default_rng(seed + 31 * sum(call.rows) + sum(call.lengths) + d)
+    rows, lengths, kvh, heads = call.rows, call.lengths, call.kvh, call.heads
+    c = Cache(rng, lengths, kvh, call.page, d, dtype)
+    if spoil is not None:
+        spoil(c)
+    starts, G = starts_of(rows, gap), heads // kvh
+    n = int(starts[-1]) + gap
+    q = torch.tensor(rng.standard_normal((n, heads, d)), dtype=TYPES[x], device="cuda")
+    out = torch.full((n, heads, d), 5.0, dtype=TYPES[x], device="cuda")
+    batch = binding.batch(gpu(c.table), gpu(lengths), gpu(starts), call.max_rows, max_length)
+    p = R.plan(binding.kv_pages(c.k, c.v), batch, x, heads, n)
+    for name, value in (want_plan or {}).items():
+        assert getattr(p, name) == value, (name, p)
+    got, q64 = f64(binding.paged_attention(q, c.k, c.v, batch, out=out)), f64(q)
+    limit = max_length or c.table.shape[1] * call.page
+    of_heads = range(kvh) if kvh <= 4 else sorted({0, 1, kvh // 2, kvh - 1}) if heads_of is None else heads_of
+    vmax = max(np.abs(v).max() for v in c.v64 if v.size)
+    live = np.zeros(n, bool)
+    for s, (m, length) in enumerate(zip(rows, lengths)):
+        at, take = starts[s], min(m, call.max_rows)
+        live[at:at + take] = True
+        pages = c.table[s, np.arange(length) // call.page]
+        there = (pages >= 0) & (pages < c.n_pages)
+        for g in of_heads if m else ():
+            hs = slice(g * G, (g + 1) * G)
+            want, size, spread = R.attention(q64[at:at + m, hs], c.k64[s][:, g], c.v64[s][:, g], length, take, limit,
+                                             R.scale_of(d), there)
+            tol = R.tolerance(x, R.weight_of(p, dtype), d, max(length, 1), size, vmax, want, spread)
+            off = np.abs(got[at:at + take, hs] - want)
+            assert (off <= tol).all(), (s, g, float(np.nanmax(off / tol)))
+    assert np.isfinite(got).all() and (got[~live] == 5.0).all()
+    return p
+
+
+# ----------------------------------------------------------------------------
+# streams
+
+
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [16, 64, 128])
+@pytest.mark.parametrize("kind", R.STREAMS, ids=str)
+def test_chunks_of_several_spans(kind, d, x):
+    """Chunks that hold several sequences, parts of them, and one whose middle is all of it."""
+    p = check(R.STREAMS[kind], d, x, "bf16", dict(tile=kind[0], waves=kind[1]))
+    assert p.chunks and R.layout(R.STREAMS[kind], p)[1] > 1
+
+
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [16, 64, 128])
+@pytest.mark.parametrize("kind", R.MANY_PARTS, ids=str)
+def test_sequences_of_many_parts(kind, d, x):
+    """More parts than a wave has lanes, joined by one wave and by four."""
+    p = check(R.MANY_PARTS[kind], d, x, "bf16", dict(tile=kind[0]))
+    assert p.chunks and R.parts(R.MANY_PARTS[kind], p) > 64

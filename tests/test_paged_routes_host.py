@@ -1,0 +1,32 @@
+"""That the calls of the GPU tests are shared out as those say (no GPU is needed)."""
+
+import pytest
+
+from tests import paged_routes as R
+
+
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [16, 64, 128])
+@pytest.mark.parametrize("kind", R.STREAMS, ids=str)
+def test_chunks_of_several_spans(kind, d, x):
+    """Every way in which a sequence can lie in a chunk."""
+    c = R.STREAMS[kind]
+    p = R.plan_of(c, d, x, "bf16")
+    chunks, step = R.layout(c, p)
+    assert (p.tile, p.waves) == kind and 1 < p.chunks < sum(k[-1][-1] for k in chunks if k) and step > 1
+    ends = [[(first == 0, end == spans) for _, first, end, spans in k] for k in chunks]
+    assert any(len(k) > 2 for k in ends)
+    assert any((True, True) in k and len(k) > 1 for k in ends)  # a sequence whole beside another
+    assert any((False, True) in k and (True, False) in k for k in ends)  # the end of one and the beginning of another
+    assert any(k == [(False, False)] for k in ends)  # nothing but the middle of one
+    assert any(first == 0 and 1 < end == spans for k in chunks for _, first, end, spans in k)  # whole, of several spans
+
+
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [16, 64, 128])
+@pytest.mark.parametrize("kind", R.MANY_PARTS, ids=str)
+def test_sequences_of_many_parts(kind, d, x):
+    c = R.MANY_PARTS[kind]
+    p = R.plan_of(c, d, x, "bf16")
+    assert p.tile == kind[0] and R.parts(c, p) > 64
+    assert (p.chunks <= 8 * len(c.rows)) == (kind[1] == 64)
