@@ -115,3 +115,19 @@ MANY_PARTS = {
     (128, 256): Call([2, 16], [300, 20000], 8, 1, 32, 16),
     (128, 64): Call([16] + [1] * 70, [9000] + [70] * 70, 8, 1, 32, 16),
 }
+
+
+# Around as many sequences as a work-group of a stream adds up the spans of (1024), several hundred of
+# more than one span, by (sequences, rows of a tile): two or four sequences a thread.
+def many_sequences(n, tile):
+    rng = np.random.default_rng(n + tile)
+    most = {16: 1, 32: 3, 64: 8, 128: 16}[tile]
+    heads = 2 if tile == 16 else 8
+    lengths = [int(t) for t in rng.integers(0, 700, n)]
+    lengths[n // 3], lengths[n - 1] = 2100, 1500
+    rows = [int(t) for t in rng.integers(0, most + 1, n)]
+    rows[0], rows[n - 1] = most, 1
+    return Call(rows, lengths, heads, 1, 64, most)
+
+
+MANY = [(n, tile) for n in (513, 1023, 1024, 1025) for tile in (16, 32, 64, 128)]

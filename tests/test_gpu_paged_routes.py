@@ -74,3 +74,11 @@ def test_sequences_of_many_parts(kind, d, x):
     """More parts than a wave has lanes, joined by one wave and by four."""
     p = check(R.MANY_PARTS[kind], d, x, "bf16", dict(tile=kind[0]))
     assert p.chunks and R.parts(R.MANY_PARTS[kind], p) > 64
+
+
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+@pytest.mark.parametrize("n,tile", R.MANY)
+def test_streams_of_a_thousand_sequences(n, tile, x):
+    """As many as a work-group adds up the spans of, and one more, which takes them whole."""
+    p = check(R.many_sequences(n, tile), 32, x, "bf16", dict(tile=tile))
+    assert (p.chunks > 0) == (n <= 1024)

@@ -30,3 +30,14 @@ def test_sequences_of_many_parts(kind, d, x):
     p = R.plan_of(c, d, x, "bf16")
     assert p.tile == kind[0] and R.parts(c, p) > 64
     assert (p.chunks <= 8 * len(c.rows)) == (kind[1] == 64)
+
+
+@pytest.mark.parametrize("n,tile", R.MANY)
+def test_streams_of_a_thousand_sequences(n, tile):
+    """Streams up to 1024 sequences, whole ones past that."""
+    c = R.many_sequences(n, tile)
+    for x in ("f32", "bf16"):
+        p = R.plan_of(c, 32, x, "bf16")
+        assert (p.tile, p.chunks > 0) == (tile, n <= 1024)
+        if p.chunks:
+            assert R.layout(c, p)[1] > 1 and sum(k > p.span for k in c.lengths) > 200
