@@ -131,3 +131,27 @@ def many_sequences(n, tile):
 
 
 MANY = [(n, tile) for n in (513, 1023, 1024, 1025) for tile in (16, 32, 64, 128)]
+
+# Tiles over pages, whole and in shares, of few and of many sequences.
+CHUNKS, BEHIND = [200, 1, 130, 90, 64], [700, 300, 130, 500, 1000]
+_rng = np.random.default_rng(70)
+SEVENTY = [int(t) for t in _rng.integers(0, 71, 70)]
+SEVENTY[5] = 70
+AFTER = [m + int(t) for m, t in zip(SEVENTY, _rng.integers(0, 500, 70))]
+TILES = {
+    # (name, type of the queries): (Call, tile, shares or 0: more than one, whether by k_batch_attn_wide)
+    ("five chunks, 64-row tiles", "f32"): (Call(CHUNKS, BEHIND, 64, 32, 64, 200), 64, 1, 0),
+    ("five chunks, 64-row tiles", "bf16"): (Call(CHUNKS, BEHIND, 64, 32, 16, 200), 64, 1, 0),
+    ("five chunks, tiles for every CU", "f32"): (Call(CHUNKS, BEHIND, 80, 40, 16, 200), 128, 1, 0),
+    ("five chunks, tiles for every CU", "bf16"): (Call(CHUNKS, BEHIND, 80, 40, 64, 200), 128, 1, 1),
+    ("five chunks, small pages", "bf16"): (Call(CHUNKS, BEHIND, 80, 40, 16, 190), 128, 1, 1),
+    ("one chunk", "f32"): (Call([700], [1111], 64, 32, 32, 700), 64, 1, 0),
+    ("one chunk", "bf16"): (Call([700], [1111], 64, 32, 32, 700), 128, 1, 1),
+    ("one chunk, no past", "bf16"): (Call([700], [700], 64, 32, 128, 700), 128, 1, 1),
+    ("70 sequences, shares", "f32"): (Call(SEVENTY, AFTER, 4, 2, 64, 70), 128, 0, 0),
+    ("70 sequences, shares", "bf16"): (Call(SEVENTY, AFTER, 4, 2, 16, 70), 128, 0, 1),
+    ("70 sequences, 64-row tiles", "f32"): (Call(SEVENTY, AFTER, 8, 4, 16, 70), 64, 1, 0),
+    ("70 sequences, 64-row tiles", "bf16"): (Call(SEVENTY, AFTER, 8, 4, 64, 70), 64, 1, 0),
+    ("70 sequences, tiles for every CU", "f32"): (Call(SEVENTY, AFTER, 12, 6, 64, 70), 128, 1, 0),
+    ("70 sequences, tiles for every CU", "bf16"): (Call(SEVENTY, AFTER, 12, 6, 32, 69), 128, 1, 1),
+}

@@ -82,3 +82,29 @@ def test_streams_of_a_thousand_sequences(n, tile, x):
     """As many as a work-group adds up the spans of, and one more, which takes them whole."""
     p = check(R.many_sequences(n, tile), 32, x, "bf16", dict(tile=tile))
     assert (p.chunks > 0) == (n <= 1024)
+
+
+# ----------------------------------------------------------------------------
+# tiles
+
+
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
+@pytest.mark.parametrize("kind", R.TILES, ids=str)
+def test_tiles_over_pages(kind, d):
+    """Sequences of several tiles, some of them short, rows of no sequence around them and pages that are not there."""
+    def spoil(c):
+        c.table[0, 1], c.table[3, 0], c.table[2, 1 if c.table.shape[1] > 2 else 0] = -1, c.n_pages, -2**31
+
+    call, tile, shares, wide = R.TILES[kind]
+    p = check(call, d, kind[1], "bf16", dict(tile=tile, chunks=0, wide=wide), gap=3)
+    assert p.splits == shares if shares else p.splits > 1
+    if len(call.rows) > 1:
+        check(call, d, kind[1], "bf16", dict(tile=tile, chunks=0, wide=wide), spoil=spoil, seed=1)
+
+
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
+@pytest.mark.parametrize("name", ["five chunks, 64-row tiles", "one chunk", "70 sequences, shares"])
+def test_tiles_over_float32_pages(name, d, x):
+    call = R.TILES[name, x][0]
+    check(call._replace(heads=call.heads // (call.kvh // 2), kvh=2), d, x, "f32", dict(tile=16, chunks=0), gap=1)

@@ -41,3 +41,13 @@ def test_streams_of_a_thousand_sequences(n, tile):
         assert (p.tile, p.chunks > 0) == (tile, n <= 1024)
         if p.chunks:
             assert R.layout(c, p)[1] > 1 and sum(k > p.span for k in c.lengths) > 200
+
+
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
+@pytest.mark.parametrize("kind", R.TILES, ids=str)
+def test_tiles_over_pages(kind, d):
+    """Sequences of several tiles each."""
+    c, tile, shares, wide = R.TILES[kind]
+    p = R.plan_of(c, d, kind[1], "bf16")
+    assert (p.tile, p.chunks, p.wide) == (tile, 0, wide) and (p.splits == shares if shares else p.splits > 1)
+    assert c.max_rows * c.heads // c.kvh > tile
