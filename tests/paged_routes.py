@@ -72,7 +72,7 @@ def attention(q, k, v, length, rows, limit, scale, there=None):
     top = np.where(see.any(axis=1), z.max(axis=1, initial=-np.inf), 0.0)
     w = np.exp(z - top[:, None])
     w /= np.maximum(w.sum(axis=1, keepdims=True), 1e-300)
-    size = float((np.abs(x).max(axis=0) @ np.abs(k).max(axis=0) if length else 0.0) * abs(scale))
+    size = float((np.abs(x) @ np.abs(k).T).max(initial=0.0) * abs(scale))
     return (w @ v).reshape(rows, G, d), size, (w @ np.abs(v)).reshape(rows, G, d)
 
 
@@ -154,4 +154,12 @@ TILES = {
     ("70 sequences, 64-row tiles", "bf16"): (Call(SEVENTY, AFTER, 8, 4, 64, 70), 64, 1, 0),
     ("70 sequences, tiles for every CU", "f32"): (Call(SEVENTY, AFTER, 12, 6, 64, 70), 128, 1, 0),
     ("70 sequences, tiles for every CU", "bf16"): (Call(SEVENTY, AFTER, 12, 6, 32, 69), 128, 1, 1),
+}
+
+# Up to 32 rows of a kv head without streams, by (rows of a tile, waves): Call.
+FEW = {
+    (16, 4): Call([1, 3, 2, 4, 0, 1], [300, 40, 333, 64, 7, 1], 16, 4, 32, 4),
+    (32, 4): Call([5, 8, 1, 7], [250, 33, 410, 7], 16, 4, 16, 8),
+    (16, 1): Call([1, 2, 0, 2] * 4, [100, 33, 5, 200] * 4, 344, 43, 16, 2),
+    (32, 1): Call([4, 2, 3, 1] * 4, [100, 33, 5, 401] * 4, 344, 43, 16, 4),
 }

@@ -108,3 +108,15 @@ def test_tiles_over_pages(kind, d):
 def test_tiles_over_float32_pages(name, d, x):
     call = R.TILES[name, x][0]
     check(call._replace(heads=call.heads // (call.kvh // 2), kvh=2), d, x, "f32", dict(tile=16, chunks=0), gap=1)
+
+
+# ----------------------------------------------------------------------------
+# few rows
+
+
+@pytest.mark.parametrize("x,dtype", [("f32", "bf16"), ("bf16", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
+@pytest.mark.parametrize("kind", R.FEW, ids=str)
+def test_few_rows_hold_their_weights(kind, d, x, dtype):
+    """Two bfloat16 terms of a softmax weight, and all of it over float32 pages: the tolerance has no room for one term."""
+    check(R.FEW[kind], d, x, dtype, dict(tile=kind[0], waves=kind[1], chunks=0) if dtype == "bf16" else dict(tile=16), gap=1)

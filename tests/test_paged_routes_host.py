@@ -1,5 +1,6 @@
 """That the calls of the GPU tests are shared out as those say (no GPU is needed)."""
 
+import numpy as np
 import pytest
 
 from tests import paged_routes as R
@@ -51,3 +52,35 @@ def test_tiles_over_pages(kind, d):
     p = R.plan_of(c, d, kind[1], "bf16")
     assert (p.tile, p.chunks, p.wide) == (tile, 0, wide) and (p.splits == shares if shares else p.splits > 1)
     assert c.max_rows * c.heads // c.kvh > tile
+
+
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", R.FEW, ids=str)
+def test_few_rows(kind, x):
+    p = R.plan_of(R.FEW[kind], 64, x, "bf16")
+    assert (p.tile, p.waves) == kind and p.chunks == 0
+
+
+@pytest.mark.parametrize("d", [16, 64, 128])
+def test_tolerance_of_two_terms_does_not_take_one(d):
+    """Weights rounded to one bfloat16 term, in the oracle, are outside the tolerance of two: what calls of few
+    rows promise would not be lost unseen.  Two terms are within it."""
+    torch = pytest.importorskip("torch")
+
+    def rounded(t):
+        return torch.tensor(t, dtype=torch.float64).to(torch.bfloat16).double().numpy()
+
+    rng = np.random.default_rng(d)
+    rows, length = 32, 60
+    q, k, v = (rounded(rng.standard_normal(s)) for s in ((rows, 1, d), (length, d), (length, d)))
+    want, size, spread = R.attention(q, k, v, length, rows, length, R.scale_of(d))
+    tol = R.tolerance("bf16", "two", d, length, size, np.abs(v).max(), want, spread)
+    off = {"one": np.zeros(want.shape), "two": np.zeros(want.shape)}
+    for i in range(rows):
+        z = k[:length - rows + i + 1] @ q[i, 0] * R.scale_of(d)
+        w = np.exp(z - z.max())
+        one = rounded(w)
+        for name, terms in (("one", one), ("two", one + rounded(w - one))):
+            off[name][i, 0] = np.abs(rounded(terms @ v[:len(z)] / w.sum()) - want[i, 0])
+    assert (off["two"] <= tol).all() and (off["one"] > tol).mean() > 0.01
+    assert (off["one"] <= R.tolerance("bf16", "one", d, length, size, np.abs(v).max(), want, spread)).all()
