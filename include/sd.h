@@ -494,7 +494,9 @@ sd_status sd_paged_append(const sd_rope *rope, const void *qkv, int64_t ld_qkv, 
 
 /* Attention of a batch's rows over the pages: the row at position p sees the
  * positions 0 .. p of its sequence (its own and those of the rows before it
- * are in the pages already).  q and out [n][n_heads head_dim] (x_dtype, rows
+ * are in the pages already).  1 <= n <= 2^20, n_heads at most 4096, n n_heads at most
+ * 2^26 and n_seqs n_kv_heads at most 2^22: a larger call is refused, and is two of
+ * some of the sequences.  q and out [n][n_heads head_dim] (x_dtype, rows
  * ld_q and ld_out apart, not overlapping); scores are scaled by scale (0: 1 /
  * sqrt(head_dim); scale log2(e) is finite); scores and sums are float32 (of
  * bfloat16 queries and pages the softmax weights are rounded to bfloat16 for their
@@ -507,8 +509,9 @@ sd_status sd_paged_append(const sd_rope *rope, const void *qkv, int64_t ld_qkv, 
 sd_status sd_paged_attention(const sd_kv_pages *kv, const sd_batch *batch, const void *q, int64_t ld_q, int32_t x_dtype,
                              int32_t n_heads, int32_t n, float scale, void *out, int64_t ld_out, void *workspace,
                              size_t workspace_bytes, void *hip_stream);
-/* Bytes of workspace for these sizes (0 where none is needed, or for sizes
- * that sd_paged_attention refuses); batch's pointers are not read. */
+/* Bytes of workspace for these sizes (0 where none is needed, and for sizes
+ * that sd_paged_attention refuses, with the reason in sd_last_error()); of batch's
+ * pointers only whether starts is NULL counts. */
 size_t sd_paged_attention_workspace(const sd_kv_pages *kv, const sd_batch *batch, int32_t x_dtype, int32_t n_heads,
                                     int32_t n);
 
@@ -517,7 +520,8 @@ size_t sd_paged_attention_workspace(const sd_kv_pages *kv, const sd_batch *batch
  * sequence of n rows, n_seqs 1) of q, and the same positions of the layer hold
  * its keys and values (capacity >= n; a packed [rows][kv heads][head_dim] tensor
  * is a layer with row_stride n_kv_heads head_dim).  Row i of a sequence sees its
- * rows 0 .. i.  The rest as in sd_paged_attention.  Errors: INVALID_ARG, CAPACITY, DEVICE. */
+ * rows 0 .. i.  The rest, its bounds of n, n_heads and n_seqs among it, as in
+ * sd_paged_attention.  Errors: INVALID_ARG, CAPACITY, DEVICE. */
 sd_status sd_prompt_attention(const sd_kv_layer *kv, const int32_t *starts, int32_t n_seqs, const void *q, int64_t ld_q,
                               int32_t x_dtype, int32_t n_heads, int32_t n, float scale, void *out, int64_t ld_out,
                               void *hip_stream);

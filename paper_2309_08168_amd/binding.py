@@ -890,7 +890,7 @@ def paged_attention(q, k, v, batch: sd_batch, scale: float = 0.0, out=None, work
 
 def paged_attention_workspace(k, v, batch: sd_batch, n_heads: int, n: int, bf16: bool = False) -> int:
     """Bytes of workspace paged_attention needs for these sizes (bf16: for bfloat16
-    queries)."""
+    queries); 0 also for sizes that it refuses."""
     _int32(n_heads, n)
     return int(load().sd_paged_attention_workspace(kv_pages(k, v), batch, SD_BF16 if bf16 else SD_F32, n_heads, n))
 

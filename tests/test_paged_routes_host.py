@@ -3,6 +3,7 @@
 import numpy as np
 import pytest
 
+from paper_2309_08168_amd import binding
 from tests import paged_routes as R
 
 
@@ -84,3 +85,37 @@ def test_tolerance_of_two_terms_does_not_take_one(d):
             off[name][i, 0] = np.abs(rounded(terms @ v[:len(z)] / w.sum()) - want[i, 0])
     assert (off["two"] <= tol).all() and (off["one"] > tol).mean() > 0.01
     assert (off["one"] <= R.tolerance("bf16", "one", d, length, size, np.abs(v).max(), want, spread)).all()
+
+
+# ----------------------------------------------------------------------------
+# the bounds of a call
+
+AT = 1 << 20  # an aligned address that nothing reads
+
+
+def refusal(n, heads, seqs, kvh, prompt):
+    """What sd_last_error() says of a call of these sizes without queries."""
+    lib, kv = binding.load(), binding.sd_kv_pages(AT, AT, kvh * 256, 256, 16, kvh, 4, 16, 16, 1)
+    batch = binding.sd_batch(AT, AT, AT, 4, seqs, 4, n, 0)
+    ld = heads * 16
+    if prompt:
+        layer = binding.sd_kv_layer(AT, AT, 16, kvh * 16, kvh, 1 << 20, 16, 1)
+        status = lib.sd_prompt_attention(layer, AT, seqs, None, ld, 0, heads, n, 0.0, AT, ld, None)
+    else:
+        status = lib.sd_paged_attention(kv, batch, None, ld, 0, heads, n, 0.0, AT, ld, AT, 1 << 40, None)
+    assert status == binding.SD_ERR_INVALID_ARG
+    said = lib.sd_last_error()
+    if not prompt and b"q and out" not in said:
+        assert lib.sd_paged_attention_workspace(kv, batch, 0, heads, n) == 0 and lib.sd_last_error() == said
+    return said
+
+
+@pytest.mark.parametrize("prompt", [False, True])
+@pytest.mark.parametrize("n,heads,seqs,kvh,fits", [
+    (1 << 20, 64, 3, 8, True), (1 << 20, 65, 3, 5, False), (1 << 20, 128, 3, 8, False), (1 << 14, 4096, 3, 8, True),
+    ((1 << 14) + 1, 4096, 3, 8, False), (1 << 16, 64, 1 << 16, 64, True), (1 << 16, 65, 1 << 16, 65, False),
+    (1 << 16, 128, 1 << 15, 128, True), (1 << 16, 128, (1 << 15) + 1, 128, False)])
+def test_rows_times_heads_and_sequences_times_kv_heads(n, heads, seqs, kvh, fits, prompt):
+    """2^26 and 2^22 are taken (refused only further on: without queries), one more of either is not."""
+    said = refusal(n, heads, seqs, kvh, prompt)
+    assert (b"q and out" in said) == fits and (b"2^26" in said and b"2^22" in said) != fits
