@@ -119,3 +119,13 @@ def test_rows_times_heads_and_sequences_times_kv_heads(n, heads, seqs, kvh, fits
     """2^26 and 2^22 are taken (refused only further on: without queries), one more of either is not."""
     said = refusal(n, heads, seqs, kvh, prompt)
     assert (b"q and out" in said) == fits and (b"2^26" in said and b"2^22" in said) != fits
+
+
+def test_pages_that_reach_past_64_bits():
+    """Refused for that, and not for a stride that is no multiple of 16 bytes."""
+    lib, far = binding.load(), dict(page_stride=1 << 40, head_stride=0, row_stride=128, n_kv_heads=1, page_size=16, head_dim=128)
+    batch = binding.sd_batch(AT, AT, AT, 4, 1, 4, 1, 0)
+    for n_pages, fits in ((1 << 22, True), ((1 << 22) + 2, False), (2**31 - 1, False)):
+        kv = binding.sd_kv_pages(k=AT, v=AT, n_pages=n_pages, dtype=0, **far)
+        assert lib.sd_paged_attention(kv, batch, None, 128, 0, 1, 1, 0.0, AT, 128, AT, 1 << 40, None) == binding.SD_ERR_INVALID_ARG
+        assert (b"past 64 bits" in lib.sd_last_error()) != fits
