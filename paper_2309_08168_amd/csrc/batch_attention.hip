@@ -1929,8 +1929,8 @@ __global__ __launch_bounds__(THREADS) void k_batch_join_stream(BatchAttnArgs a, 
 // 13, 16 sequences of up to 700 35.6 and 43.3, 8 of 40 heads 29.2 and 24.9.
 //   Eight waves a work-group for long ones: 60000 keys 57.7 -> 55.2 us, 64 sequences of
 // 500 .. 8000 197 -> 193; 8 sequences of 750 .. 1500 (40 heads) 46.6 -> 48.7.
-//   Packed tiles of 64 or 128 rows, us: 1023 rows of 40 heads (360 tiles) float32 51
-// and 68, bfloat16 31.8 and 35.5; 1000 of 64 heads on 8 (512) 72 and 71, 43 and 35.
+//   Packed tiles of 64 or 128 rows, us: 1023 rows of 40 heads (320 tiles) float32 51
+// and 68, bfloat16 31.8 and 35.5; 1000 of 64 heads on 8 (504) 72 and 71, 43 and 35.
 //   Over pages, where tiles of 128 rows are too many for shares (more than 256) and too few
 // to fill the last round (at most 450): 15 chains of 26 rows, 64 heads on 8, 26.9 and 36.3,
 // float32 39.6 and 56.9; five chunks of up to 358 rows of 32 heads 40.7 and 55.5, 58.8 and 76.4; 1000
@@ -2193,6 +2193,17 @@ sd_status paged_sizes(const sd_kv_pages *kv, const sd_batch *batch, int32_t n_he
     return SD_OK;
 }
 
+// The plan of a call over pages, from its sizes alone.
+sd_status paged_plan(const sd_kv_pages *kv, const sd_batch *batch, int32_t x_dtype, int32_t n_heads, int32_t n,
+                     BatchAttnArgs *a) {
+    sd_status st = paged_sizes(kv, batch, n_heads, n, false, a);
+    if (st != SD_OK || (st = check_call(nullptr, 0, x_dtype, n_heads, n, a->n_seqs, a->n_kv_heads, kv->head_dim, nullptr, 0,
+                                        nullptr)) != SD_OK)
+        return st;
+    plan(a, x_dtype == SD_BF16, kv->dtype == SD_BF16, kv->head_dim);
+    return SD_OK;
+}
+
 sd_status paged_attention(const sd_kv_pages *kv, const sd_batch *batch, const void *q, int64_t ld_q, int32_t x_dtype,
                           int32_t n_heads, int32_t n, float scale, void *out, int64_t ld_out, void *workspace,
                           size_t workspace_bytes, hipStream_t s) {
@@ -2258,13 +2269,11 @@ sd_status prompt_attention(const sd_kv_layer *kv, const int32_t *starts, int32_t
 extern "C" {
 
 size_t sd_paged_attention_workspace(const sd_kv_pages *kv, const sd_batch *batch, int32_t x_dtype, int32_t n_heads,
-                                    int32_t n) {
+                                    int32_t n) try {
     BatchAttnArgs a{};
-    if (paged_sizes(kv, batch, n_heads, n, false, &a) != SD_OK ||
-        check_call(nullptr, 0, x_dtype, n_heads, n, a.n_seqs, a.n_kv_heads, kv->head_dim, nullptr, 0, nullptr) != SD_OK)
-        return 0;
-    plan(&a, x_dtype == SD_BF16, kv->dtype == SD_BF16, kv->head_dim);
-    return space_of(a, kv->head_dim).bytes();
+    return paged_plan(kv, batch, x_dtype, n_heads, n, &a) == SD_OK ? space_of(a, kv->head_dim).bytes() : 0;
+} catch (...) {  // (a refusal's message is allocated)
+    return 0;
 }
 
 sd_status sd_paged_attention(const sd_kv_pages *kv, const sd_batch *batch, const void *q, int64_t ld_q, int32_t x_dtype,
@@ -2279,15 +2288,11 @@ sd_status sd_paged_attention(const sd_kv_pages *kv, const sd_batch *batch, const
 // k_batch_attn_wide takes it.
 sd_status sdk_paged_plan(const sd_kv_pages *kv, const sd_batch *batch, int32_t x_dtype, int32_t n_heads, int32_t n,
                          int32_t out[7]) {
-    BatchAttnArgs a{};
-    sd_status st = paged_sizes(kv, batch, n_heads, n, false, &a);
-    if (st != SD_OK || (st = check_call(nullptr, 0, x_dtype, n_heads, n, a.n_seqs, a.n_kv_heads, kv->head_dim, nullptr, 0,
-                                        nullptr)) != SD_OK)
-        return st;
-    plan(&a, x_dtype == SD_BF16, kv->dtype == SD_BF16, kv->head_dim);
-    const int32_t of[7] = {a.tile, a.slots, a.chunks, a.span, a.splits, a.waves, a.wide};
-    std::copy(of, of + 7, out);
-    return SD_OK;
+    SD_GUARD(BatchAttnArgs a{};
+             const sd_status st = paged_plan(kv, batch, x_dtype, n_heads, n, &a);
+             if (st != SD_OK) return st;
+             const int32_t of[7] = {a.tile, a.slots, a.chunks, a.span, a.splits, a.waves, a.wide};
+             std::copy(of, of + 7, out); return SD_OK;)
 }
 
 sd_status sd_prompt_attention(const sd_kv_layer *kv, const int32_t *starts, int32_t n_seqs, const void *q, int64_t ld_q,

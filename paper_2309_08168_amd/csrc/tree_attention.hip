@@ -1103,8 +1103,10 @@ size_t tree_attention_bytes(const sd_kv_layer *kv, int32_t n_heads, int32_t n, i
 
 extern "C" {
 
-size_t sd_tree_attention_workspace(const sd_kv_layer *kv, int32_t n_heads, int32_t n, int32_t prefix) {
+size_t sd_tree_attention_workspace(const sd_kv_layer *kv, int32_t n_heads, int32_t n, int32_t prefix) try {
     return tree_attention_bytes(kv, n_heads, n, n, prefix);
+} catch (...) {  // (a refusal's message is allocated)
+    return 0;
 }
 
 sd_status sd_tree_attention(const sd_kv_layer *kv, const float *q, int64_t ld_q, int32_t n_heads, int32_t n,
