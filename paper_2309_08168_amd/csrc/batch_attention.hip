@@ -907,8 +907,9 @@ __global__ __launch_bounds__(64 * NQ * NK, 2) void k_batch_attn_mfma(BatchAttnAr
 // Heads of 128, us: 8000 rows of 32 heads 534 (0.98 PFLOP/s), 1000 rows of 64 heads on 8
 // behind 15111 positions 541 (0.94), 16 ragged prompts of 64 heads on 8 378 (0.70: 5 to 6 us of
 // start and end a tile).  With k_batch_attn_mfma, whose blocks of 64 keys take their parts
-// one after another, 579, 622 and 398.  The 8000 rows of zeros take 383: power holds the clock at 2.07 GHz
-// with random operands, and the matrix cores are busy 45% of the time.  Loads cost 13% of
+// one after another, 579, 622 and 398.  Of the cycles of a SIMD the products take 57% and the vector operations
+// 51%: its two waves nearly take turns.  Rows of zeros take as many cycles (907 thousand) in 383 us: power holds
+// the clock, 1.74 GHz with random operands and 2.18 with zeros under the profiler (522 and 415 us).  Loads cost 13% of
 // a step, its barrier 2 to 4.  64-key steps need more registers than there are.
 struct Halves {  // where the 16-key halves of a block start (elements), and which have a page
     int64_t off[2];
