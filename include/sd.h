@@ -467,8 +467,10 @@ typedef struct {
  * the call would write for them is left as it was), and positions below
  * max_length (at most table_pages * page_size, which 0 stands for; positions
  * from there on are neither stored nor seen).  Both only bound what the call
- * prepares for: a tight bound is a faster call.  An entry of the table outside [0, n_pages) holds no
- * positions: nothing is stored there, and nothing of it is seen. */
+ * prepares for: a tight bound is a faster call.  Long sequences of one row beside
+ * others of many are faster as two batches of some of the sequences each (table + s
+ * ld_table, lengths + s, starts + s) over the same rows.  An entry of the table outside
+ * [0, n_pages) holds no positions: nothing is stored there, and nothing of it is seen. */
 typedef struct {
     const int32_t *table, *lengths, *starts;
     int64_t ld_table;

@@ -771,8 +771,10 @@ def batch(table, lengths, starts=None, max_rows: int = 1, max_length: int = 0) -
     """A batch of sequences (sd_batch) over int32 tensors: table [n_seqs, pages], the
     page of each page_size positions; lengths [n_seqs], positions with the new rows;
     starts [n_seqs + 1], the packed rows of each sequence, or None: max_rows rows a
-    sequence.  max_rows and max_length (0: all that the table holds) bound them.  The
-    tensors live on with the batch and may change between calls."""
+    sequence.  max_rows and max_length (0: all that the table holds) bound them; long
+    sequences of one row beside others of many are faster as two batches over the same
+    rows (slices of the three tensors).  The tensors live on with the batch and may
+    change between calls."""
     if _torch is None:
         _use_torch()
     shape, stride = table.shape, table.stride()

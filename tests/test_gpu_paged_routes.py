@@ -189,3 +189,43 @@ def test_large_pages(rows, heads, x, dtype, page):
 @pytest.mark.parametrize("x,dtype", [("f32", "bf16"), ("bf16", "bf16"), ("f32", "f32")])
 def test_append_to_large_pages(x, dtype):
     assert check_append([5, 3, 1], [65538, 65536, 7], 2, 1, 16, x, dtype, dict(rotary_dim=16), 65536) == 9
+
+
+# ----------------------------------------------------------------------------
+# batches of some of the sequences
+
+
+@pytest.mark.parametrize("x,dtype", [("f32", "bf16"), ("bf16", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("cut", [0, 1, 5, 8])
+def test_a_step_as_two_batches(cut, x, dtype):
+    """Tokens and a chunk: one call and two over slices of the same tensors, appends too; each writes its own rows."""
+    rng = np.random.default_rng(cut)
+    rows, past, heads, kvh, d, page = [1] * 5 + [3, 1, 1, 130], [700, 0, 1500, 40, 63, 10, 2000, 1, 300], 8, 2, 64, 32
+    lengths, starts, n = [m + p for m, p in zip(rows, past)], starts_of(rows), sum(rows)
+    c = Cache(rng, lengths, kvh, page, d, dtype)
+    table, at, begin = gpu(c.table), gpu(lengths), gpu(starts)
+    qkv = torch.tensor(rng.standard_normal((n, (heads + 2 * kvh) * d)), dtype=TYPES[x], device="cuda")
+    form = binding.rope(rotary_dim=d)
+    halves = [slice(0, cut), slice(cut, len(rows))]
+    batches = [binding.batch(table[h], at[h], begin[h.start:h.stop + 1], max(rows[h]), max(lengths[h])) for h in halves if rows[h]]
+    k, v = c.k.clone(), c.v.clone()
+    whole = binding.batch(table, at, begin, max(rows))
+    q = binding.paged_append(form, qkv, c.k, c.v, whole, heads)
+    q2 = torch.full_like(q, 3.0)
+    for b in batches:
+        binding.paged_append(form, qkv, k, v, b, heads, q_out=q2)
+    assert torch.equal(q, q2) and torch.equal(k.nan_to_num(7.0), c.k.nan_to_num(7.0)) and torch.equal(v.nan_to_num(7.0), c.v.nan_to_num(7.0))
+    out = torch.full_like(q, 3.0)
+    for b in batches:
+        binding.paged_attention(q, k, v, b, out=out)
+    one = binding.paged_attention(q, k, v, whole)
+    q64, k64, v64 = f64(q), f64(k), f64(v)
+    for s, (m, length) in enumerate(zip(rows, lengths)):
+        pos = np.arange(length)
+        pages, place = c.table[s, pos // page], pos % page
+        for g in range(kvh):
+            a, hs = slice(starts[s], starts[s] + m), slice(g * heads // kvh, (g + 1) * heads // kvh)
+            kk, vv = k64[pages, g, place], v64[pages, g, place]
+            want, size, spread = R.attention(q64[a, hs], kk, vv, length, m, length, R.scale_of(d))
+            tol = R.tolerance(x, "float32" if dtype == "f32" else "one", d, length, size, np.abs(vv).max(), want, spread)
+            assert (np.abs(f64(out[a, hs]) - want) <= tol).all() and (np.abs(f64(one[a, hs]) - want) <= tol).all(), (s, g)
