@@ -482,7 +482,7 @@ typedef struct {
  * sd_dtype, rows ld_qkv elements apart: n_heads query heads, then the pages' kv
  * heads of K, then of V).  q_norm and k_norm (dtype of the pages, [head_dim],
  * both or neither): each head x of Q and of K becomes x_e w_e / sqrt(mean(x^2) +
- * eps) before it is rotated.  The rotary position is positions[r] (int32 [n]), or
+ * eps) before it is rotated (squares and mean in float32).  The rotary position is positions[r] (int32 [n]), or
  * the row's position in the cache when positions is NULL.  Rotated queries to
  * q_out [n][n_heads head_dim] (x_dtype, rows ld_q apart, not overlapping qkv; of
  * rows that no sequence has nothing is written), K and V to the row's
@@ -500,12 +500,15 @@ sd_status sd_paged_append(const sd_rope *rope, const void *qkv, int64_t ld_qkv, 
  * 2^26 and n_seqs n_kv_heads at most 2^22: a larger call is refused, and is two of
  * some of the sequences.  q and out [n][n_heads head_dim] (x_dtype, rows
  * ld_q and ld_out apart, not overlapping); scores are scaled by scale (0: 1 /
- * sqrt(head_dim); scale log2(e) is finite); scores and sums are float32 (of
- * bfloat16 queries and pages the softmax weights are rounded to bfloat16 for their
- * products, but for max_rows times query heads of a kv head up to 32).  A row that sees nothing gives zeros; what a row does not see
- * changes no bit of its result, whatever it holds, and neither do the other
- * rows' queries (the sizes of the call and the lengths of its sequences may, in
- * the order of float32 sums); what it sees is finite, or its result may be NaN.  workspace
+ * sqrt(head_dim); scale log2(e) is finite); scores and sums are float32.  Softmax weights
+ * enter their products with V as they are, but for bfloat16 queries over bfloat16
+ * keys: rounded to bfloat16 (by 2^-8 of a weight at most), or, over pages where max_rows
+ * times the query heads of a kv head is up to 32, as two bfloat16 terms (2^-16).  Float32
+ * queries are the choice where that is too much.  A row that sees nothing gives zeros;
+ * what a row does not see changes no bit of its result, whatever it holds, and
+ * neither do the other rows' queries (the sizes of the call and the lengths of its
+ * sequences may, in the order of float32 sums); what it sees is finite, or its
+ * result may be NaN.  workspace
  * (16-byte aligned) holds at least sd_paged_attention_workspace() bytes for
  * these sizes and belongs to the call until it has run.  Errors: INVALID_ARG, DEVICE. */
 sd_status sd_paged_attention(const sd_kv_pages *kv, const sd_batch *batch, const void *q, int64_t ld_q, int32_t x_dtype,
