@@ -152,7 +152,7 @@ def host_cpu() -> dict:
 def oracle_decode_rates(cfg, weights, prompt, wl, skip, prefix=8, n_tokens=4) -> dict:
     """The oracle at the workload's model shape, decode separated from prefill.
 
-    The prefill of prompt[:prefix] is timed alone; each generate call
+    The prefill of prompt[:prefix] is timed alone, at its shortest; each generate call
     (prefill + n_tokens) is timed whole and the prefill time subtracted,
     which leaves the decode-only time of n_tokens greedy autoregressive
     tokens and of n_tokens self-speculative tokens (same mask, K_max and
@@ -165,11 +165,16 @@ def oracle_decode_rates(cfg, weights, prompt, wl, skip, prefix=8, n_tokens=4) ->
 
     om = oracle.Model(cfg, weights)
     pr = np.asarray(prompt[:prefix], np.int32)
-    c = om.cache(prefix)
-    t0 = time.perf_counter()
-    om.forward(c, pr[:-1], want_logits=False)
-    t_pf = time.perf_counter() - t0
-    del c
+    # (the shortest of up to five within two seconds: the first starts threads and touches the
+    # weights, and a small model's decode is shorter than that)
+    t_pf, spent, turn = float("inf"), 0.0, 0
+    while turn < 5 and spent < 2.0:
+        c = om.cache(prefix)
+        t0 = time.perf_counter()
+        om.forward(c, pr[:-1], want_logits=False)
+        t = time.perf_counter() - t0
+        t_pf, spent, turn = min(t_pf, t), spent + t, turn + 1
+        del c
     t0 = time.perf_counter()
     om.generate_ar(pr, n_tokens)
     t_ar = time.perf_counter() - t0 - t_pf
@@ -186,7 +191,7 @@ def oracle_decode_rates(cfg, weights, prompt, wl, skip, prefix=8, n_tokens=4) ->
         "sd_stages": int(sd["n_stages"]), "sd_drafted": int(sd["n_drafted"]),
         "context": f"{prefix - 1}..{prefix - 2 + n_tokens} positions",
         "attn_share_at_workload_ctx": round(macs_attn / (macs_w + macs_attn), 4),
-        "threads": oracle.num_threads(), "seconds": round(t_pf * 3 + t_ar + t_sd, 1),
+        "threads": oracle.num_threads(), "seconds": round(spent + t_pf * 2 + t_ar + t_sd, 1),
     }
 
 
